@@ -11,8 +11,11 @@
  *      Sec. 4.3); PE heads by a gamma-cumsum over pooled scores  (Alg. 4)
  *   4. causal softmax attention restricted to that set           (Eq. 1, Sec. 2.1)
  *
- * Conventions shared by every entry point
- * ---------------------------------------
+ * Behind the prefill it keeps K and V in an 8-bit paged cache and attends to it: the
+ * crisp_cache_* and crisp_pool_* entry points, whose layouts stand with them below.
+ *
+ * Conventions of the prefill entry points (ownership, execution and errors: of all)
+ * ----------------------------------------------------------------------------------
  * Tensors are contiguous, row-major, on the device, bf16 (raw bits):
  *   q [H_q, n, d], k and v [H_kv, n, d], o [H_q, n, d];  d = head_dim = 128.
  * GQA: query head h reads KV head h / (H_q / H_kv).  Batch is 1 (one layer of
@@ -49,7 +52,8 @@
  * it.  These checks launch their own kernels and wait for the stream (the one place
  * where the library synchronises), and its attention kernels run their tile pipeline
  * serialised (same arithmetic, same results as the release build, bit for bit), so
- * the debug build is for testing, not timing.
+ * the debug build is for testing, not timing.  The cache's entry points are the same in
+ * both builds.
  */
 #ifndef CRISP_H
 #define CRISP_H
@@ -67,7 +71,7 @@ typedef void* crisp_stream;   /* hipStream_t */
 typedef enum {
   CRISP_OK = 0,
   CRISP_EINVAL = 1,       /* bad shape, parameter, null/misaligned pointer, capacity or workspace too small */
-  CRISP_EUNSUPPORTED = 2, /* head_dim != 128 or block not in {64, 128} */
+  CRISP_EUNSUPPORTED = 2, /* head_dim != 128, block not in {64, 128}, or a size above a limit */
   CRISP_EHIP = 3          /* a HIP launch failed; see crisp_last_error() */
 } crisp_status;
 
@@ -267,6 +271,132 @@ crisp_status crisp_prefill_workspace_size(const crisp_shape* shape, size_t* byte
 crisp_status crisp_dense_attn(const crisp_shape* shape, float softmax_scale,
                               const crisp_bf16* q, const crisp_bf16* k, const crisp_bf16* v,
                               crisp_bf16* o, crisp_stream stream);
+
+/* ---------------------------------------------------------------------------------------
+ * The K/V cache: what follows a layer's prefill.  K and V of many sequences are kept in 8 bits in
+ * pages, and new rows attend to them: one row a sequence (decoding), a few (drafted tokens),
+ * or a chunk of a prompt.
+ *
+ * A page holds `block` tokens of all KV heads, codes and one scale a KV head and tensor:
+ *   pages   uint8[n_pages][H_kv][block / 64][2][8192]   tiles of 64 tokens, K (0) then V (1)
+ *   scales  float[n_pages][H_kv][2]                     a power of two, 2^-64 .. 2^122
+ * A cached value is its code times its scale; codes are e4m3 (finite, largest 448) or int8 (-127 ..
+ * 127).  Within a tile, with token t and element e of the head (0 .. 127):
+ *   K at ((t / 4 % 4 * 2 + e / 16 % 2) * 64 + e / 32 * 16 + t / 16 * 4 + t % 4) * 16 + e % 16
+ *   V at (e / 16 * 64 + t / 16 * 16 + e % 16) * 16 + t % 16
+ * (the order in which a wave of the attention takes them as matrix operands).
+ *
+ * Sequences: table int32[n_seqs][max_pages] lists each sequence's pages, position j in page
+ * table[s][j / block]; -1, or any value outside [0, n_pages), is no page.  seq_len int32[n_seqs]
+ * is the number of tokens held BEFORE the call, the same for the append and the attention of
+ * one step; rows row_ptr[s] .. row_ptr[s + 1] (int32[n_seqs + 1]) of the packed tensors are
+ * sequence s's, at positions seq_len[s], seq_len[s] + 1, ...; none is allowed.  Rows that row_ptr
+ * does not cover are not read, and in an output left as they were.  Device values out of range
+ * (lengths, offsets, pages) are brought into range or skipped: no value of theirs leads out
+ * of a buffer.  A page that two sequences of one append write to, or overlapping rows, give
+ * undefined contents.
+ * Packed tensors are bf16 [heads][n_rows][128] with strides in elements, multiples of 8; the 128
+ * elements of a row are contiguous.  Inputs may repeat heads or rows (stride 0).
+ * All entry points can be captured into a HIP graph; what they do then follows the device
+ * values at each replay. */
+enum { CRISP_CACHE_E4M3 = 0, CRISP_CACHE_INT8 = 1 };
+
+/* n_pages in [1, 2^24], n_kv_heads >= 1, head_dim == 128, block in {64, 128}. */
+typedef struct {
+  int32_t n_pages;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t block;
+  int32_t format;
+} crisp_cache_shape;
+
+/* n_seqs, max_pages, n_rows >= 0; max_pages * block <= 2^30, n_seqs * max_pages < 2^31, n_rows <= 2^24.
+ * Without sequences or rows a call returns CRISP_OK and launches nothing. */
+typedef struct {
+  int32_t n_seqs;
+  int32_t max_pages;
+  int32_t n_rows;
+} crisp_cache_batch;
+
+/* Host only.  Bytes of `pages` (16-byte aligned) and `scales` (4-byte aligned).  Neither needs any
+ * contents before the first append. */
+crisp_status crisp_cache_bytes(const crisp_cache_shape* cache, size_t* page_bytes, size_t* scale_bytes);
+
+/* K and V rows into the pages behind each sequence's tokens.  For a page, KV head and tensor that
+ * the call writes to, with MAX = 448 or 127:
+ *   e = max(-64, the smallest e with |x| <= MAX 2^e for the call's finite rows x in the page,
+ *           the page's exponent so far if it holds older tokens of the sequence)
+ *   code = x 2^-e rounded to nearest even; where e has grown, every other code of the page
+ *   becomes code 2^(e_old - e), rounded to nearest even.
+ * NaN is stored as 0 and an infinity as the largest code; neither moves e.  Positions that have
+ * no page are dropped. */
+crisp_status crisp_cache_append(const crisp_cache_shape* cache, const crisp_cache_batch* batch, uint8_t* pages,
+                                float* scales, const int32_t* table, const int32_t* seq_len, const int32_t* row_ptr,
+                                const crisp_bf16* k, int64_t k_head_stride, int64_t k_row_stride,
+                                const crisp_bf16* v, int64_t v_head_stride, int64_t v_row_stride,
+                                crisp_stream stream);
+
+/* Host only.  Bytes of workspace (256-byte aligned, any contents) of crisp_cache_attn. */
+crisp_status crisp_cache_attn_workspace_size(const crisp_cache_shape* cache, const crisp_cache_batch* batch,
+                                             int32_t n_q_heads, size_t* bytes);
+
+/* Attention of each sequence's rows over its cached tokens, the row's own position included:
+ *   o[h][r] = sum_{j <= t} softmax_j(softmax_scale q[h][r] . k_j) v_j,  t = seq_len[s] + r - row_ptr[s],
+ * over the positions j that have a page; a row that sees none gets 0.  Query head h reads KV
+ * head h / (H_q / H_kv).  softmax_scale 0 means 1/sqrt(128).  The work is split evenly over the GPU
+ * whatever the lengths, also along a sequence; partial results are joined in a fixed order, so
+ * that a call with the same arguments gives the same bits. */
+crisp_status crisp_cache_attn(const crisp_cache_shape* cache, const crisp_cache_batch* batch, int32_t n_q_heads,
+                              float softmax_scale, const uint8_t* pages, const float* scales, const int32_t* table,
+                              const int32_t* seq_len, const int32_t* row_ptr, const crisp_bf16* q,
+                              int64_t q_head_stride, int64_t q_row_stride, crisp_bf16* o, int64_t o_head_stride,
+                              int64_t o_row_stride, void* workspace, size_t workspace_bytes, crisp_stream stream);
+
+/* Page copies: pairs int32[n_pairs][2] of (from, to), of which the first *count_or_null (device;
+ * all if null) count.  A pair with a page outside [0, n_pages) moves nothing.  The pages written
+ * to must be distinct and none of them read by another pair. */
+crisp_status crisp_cache_copy(const crisp_cache_shape* cache, uint8_t* pages, float* scales, const int32_t* pairs,
+                              int32_t n_pairs, const int32_t* count_or_null, crisp_stream stream);
+
+/* The pages' bookkeeping, on the device and for the caches of all layers at once: pool holds the uses of
+ * each page (int32[n_pages]) and one bit a page in use (ceil(n_pages / 32) words, lowest page first).
+ * The same calls give the same pages: requests are served in order, with the lowest free pages.
+ * These calls must not overlap in time on one pool or table.  n_seqs <= 4096 in reserve and fork. */
+
+/* Host only.  int32 words of a pool; -1 on a bad n_pages. */
+int64_t crisp_pool_words(int32_t n_pages);
+
+/* No page in use. */
+crisp_status crisp_pool_init(int32_t n_pages, int32_t* pool, crisp_stream stream);
+
+/* Room for counts[s] more tokens behind seq_len[s]: the slots seq_len / block .. ceil((seq_len + count) /
+ * block) - 1 of row s that have no page (a negative entry) get one.  granted[s] = counts[s], or 0 where the
+ * row is too short or the free pages do not cover what the sequences up to and with s ask for: such a
+ * sequence gets none.  seq_len stays as it is. */
+crisp_status crisp_pool_reserve(int32_t n_pages, int32_t block, int32_t n_seqs, int32_t max_pages, int32_t* pool,
+                                int32_t* table, const int32_t* seq_len, const int32_t* counts, int32_t* granted,
+                                crisp_stream stream);
+
+/* Sequence dst[i] becomes a copy of src[i] (i < n <= 4096): it shares the full pages, and a partial last
+ * page is copied to a free one.  copies int32[n][2] receives that pair for crisp_cache_copy (to be run
+ * on every layer's cache), (-1, -1) if there is none, (-2, -2) if the fork is refused: an index out of
+ * range, src == dst, a dst that is not empty (seq_len 0 and no page in its first slot) or that an
+ * earlier fork of the call names, no free page, or a source whose last page is missing.  Lengths are
+ * those before the call. */
+crisp_status crisp_pool_fork(int32_t n_pages, int32_t block, int32_t n_seqs, int32_t max_pages, int32_t* pool,
+                             int32_t* table, int32_t* seq_len, const int32_t* src, const int32_t* dst, int32_t n,
+                             int32_t* copies, crisp_stream stream);
+
+/* Sequences ids[0 .. n) end: each page of their rows loses one use, the rows become -1, the lengths 0.
+ * Ids out of range are skipped, repeated ones count once. */
+crisp_status crisp_pool_free(int32_t n_pages, int32_t n_seqs, int32_t max_pages, int32_t* pool, int32_t* table,
+                             int32_t* seq_len, const int32_t* ids, int32_t n, crisp_stream stream);
+
+/* Gathers the U pages in use at [0, U): the k-th free page below U takes the k-th page in use from U on.
+ * moves int32[max(1, n_pages / 2)][2] receives the pairs for crisp_cache_copy, -1 behind the last, *count
+ * their number; table (all rows that name pages of the pool) and pool follow. */
+crisp_status crisp_pool_compact(int32_t n_pages, int32_t n_seqs, int32_t max_pages, int32_t* pool, int32_t* table,
+                                int32_t* moves, int32_t* count, crisp_stream stream);
 
 /* Static name of a status code. */
 const char* crisp_status_string(crisp_status status);

@@ -36,7 +36,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}", f"-I{CSRC}", "-Wall", "-
 # results (scores, read by the softmax every tile, and the output accumulators) in
 # VGPRs; left to itself the compiler places them in AGPRs and copies every score out
 # again.
-EXTRA = {"attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "estimate.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+EXTRA = {"attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "estimate.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+         "cache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def hipcc() -> str:

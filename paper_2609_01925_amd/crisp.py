@@ -37,6 +37,15 @@ class CrispParams(ctypes.Structure):
                 ("tau_jsd", ctypes.c_float), ("floor_mode", ctypes.c_int32), ("dense_below_len", ctypes.c_int32)]
 
 
+class CrispCacheShape(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("block", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class CrispCacheBatch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_rows", ctypes.c_int32)]
+
+
 class CrispError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{msg} (status {status})")
@@ -49,6 +58,7 @@ def _load(path: str = _LIB_PATH):
     lib = ctypes.CDLL(path)
     P, F, I32, I64, SZ = ctypes.c_void_p, ctypes.c_float, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     sh, pa = ctypes.POINTER(CrispShape), ctypes.POINTER(CrispParams)
+    cs, cb = ctypes.POINTER(CrispCacheShape), ctypes.POINTER(CrispCacheBatch)
     sig = {
         "crisp_params_default": (None, [pa]),
         "crisp_col_capacity": (I64, [sh]),
@@ -62,6 +72,17 @@ def _load(path: str = _LIB_PATH):
         "crisp_sparse_attn_noalloc": (ctypes.c_int, [sh, F, P, P, P, P, P, I64, P, P]),
         "crisp_prefill_attn": (ctypes.c_int, [sh, pa, P, P, P, P, P, P, P, P, SZ, P]),
         "crisp_dense_attn": (ctypes.c_int, [sh, F, P, P, P, P, P]),
+        "crisp_cache_bytes": (ctypes.c_int, [cs, ctypes.POINTER(SZ), ctypes.POINTER(SZ)]),
+        "crisp_cache_append": (ctypes.c_int, [cs, cb, P, P, P, P, P, P, I64, I64, P, I64, I64, P]),
+        "crisp_cache_attn_workspace_size": (ctypes.c_int, [cs, cb, I32, ctypes.POINTER(SZ)]),
+        "crisp_cache_attn": (ctypes.c_int, [cs, cb, I32, F, P, P, P, P, P, P, I64, I64, P, I64, I64, P, SZ, P]),
+        "crisp_cache_copy": (ctypes.c_int, [cs, P, P, P, I32, P, P]),
+        "crisp_pool_words": (I64, [I32]),
+        "crisp_pool_init": (ctypes.c_int, [I32, P, P]),
+        "crisp_pool_reserve": (ctypes.c_int, [I32, I32, I32, I32, P, P, P, P, P, P]),
+        "crisp_pool_fork": (ctypes.c_int, [I32, I32, I32, I32, P, P, P, P, P, I32, P, P]),
+        "crisp_pool_free": (ctypes.c_int, [I32, I32, I32, P, P, P, P, I32, P]),
+        "crisp_pool_compact": (ctypes.c_int, [I32, I32, I32, P, P, P, P, P]),
         "crisp_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "crisp_last_error": (ctypes.c_char_p, []),
     }
@@ -75,12 +96,17 @@ def _load(path: str = _LIB_PATH):
 lib = _load()
 EXPORTED = ("crisp_params_default", "crisp_col_capacity", "crisp_workspace_size", "crisp_prefill_workspace_size",
             "crisp_sparse_workspace_size", "crisp_estimate", "crisp_jsd", "crisp_route_select", "crisp_sparse_attn",
-            "crisp_sparse_attn_noalloc", "crisp_prefill_attn", "crisp_dense_attn", "crisp_status_string", "crisp_last_error")
+            "crisp_sparse_attn_noalloc", "crisp_prefill_attn", "crisp_dense_attn", "crisp_status_string", "crisp_last_error",
+            "crisp_cache_bytes", "crisp_cache_append", "crisp_cache_attn_workspace_size", "crisp_cache_attn",
+            "crisp_cache_copy", "crisp_pool_words", "crisp_pool_init", "crisp_pool_reserve", "crisp_pool_fork",
+            "crisp_pool_free", "crisp_pool_compact")
 
 # route_mode / vs_mode values (include/crisp.h)
 ROUTE_BY_CSTRUCT, ROUTE_BY_JSD = 0, 1
 VS_FLOOR, VS_GAMMA = 0, 1
 FLOOR_MEAN, FLOOR_MEDIAN = 0, 1
+# cache formats
+CACHE_E4M3, CACHE_INT8 = 0, 1
 
 
 def _check(status: int, what: str):
@@ -314,3 +340,217 @@ def crisp_prefill_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, params
                                   _ptr(route), _ptr(row_ptr), _ptr(col_idx), _ptr(ws), ws.numel(), _stream(dev)),
                     "crisp_prefill_attn")
     return (o, route, row_ptr, col_idx) if return_lists else o
+
+
+# ---------------------------------------------------------------- the 8-bit paged K/V cache
+
+
+class Cache:
+    """One layer's K and V: pages uint8 [n_pages, H_kv, block / 64, 2, 8192] and scales float32
+    [n_pages, H_kv, 2] on one GPU, in the layout of include/crisp.h.  Neither needs contents."""
+
+    def __init__(self, pages: torch.Tensor, scales: torch.Tensor, fmt: int = CACHE_E4M3):
+        _tensor(pages, "pages", torch.uint8, (None, None, None, 2, 8192), pages.device)
+        _tensor(scales, "scales", torch.float32, (pages.shape[0], pages.shape[1], 2), pages.device)
+        self.pages, self.scales, self.fmt = pages, scales, fmt
+        self.n_pages, self.n_kv_heads, self.block = pages.shape[0], pages.shape[1], 64 * pages.shape[2]
+        self.shape = CrispCacheShape(self.n_pages, self.n_kv_heads, 128, self.block, fmt)
+        crisp_cache_bytes(self.shape)  # raises on a size or format that the library does not take
+
+
+def make_cache(n_pages: int, n_kv_heads: int, block: int = 64, fmt: int = CACHE_E4M3, device="cuda") -> Cache:
+    """A cache without contents."""
+    crisp_cache_bytes(CrispCacheShape(n_pages, n_kv_heads, 128, block, fmt))
+    return Cache(torch.empty(n_pages, n_kv_heads, block // 64, 2, 8192, dtype=torch.uint8, device=device),
+                 torch.empty(n_pages, n_kv_heads, 2, dtype=torch.float32, device=device), fmt)
+
+
+def crisp_cache_bytes(shape: CrispCacheShape) -> Tuple[int, int]:
+    """Bytes of (pages, scales)."""
+    a, b = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib.crisp_cache_bytes(ctypes.byref(shape), ctypes.byref(a), ctypes.byref(b)), "crisp_cache_bytes")
+    return int(a.value), int(b.value)
+
+
+def _i32(t: torch.Tensor, name: str, dims: int, device):
+    if not (t.dtype == torch.int32 and t.dim() == dims and t.device == device and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dims}-d int32 tensor on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _batch(cache: Cache, table, seq_len, row_ptr, n_rows: int) -> CrispCacheBatch:
+    dev = cache.pages.device
+    _i32(table, "table", 2, dev)
+    _i32(seq_len, "seq_len", 1, dev)
+    _i32(row_ptr, "row_ptr", 1, dev)
+    n = table.shape[0]
+    if seq_len.shape[0] != n or row_ptr.shape[0] != n + 1:
+        raise ValueError(f"table {tuple(table.shape)}, seq_len {tuple(seq_len.shape)} and row_ptr "
+                         f"{tuple(row_ptr.shape)} must be [n, pages], [n] and [n + 1]")
+    return CrispCacheBatch(n, table.shape[1], n_rows)
+
+
+def _rows(t: torch.Tensor, name: str, heads: Optional[int], device) -> Tuple[int, int]:
+    """A packed tensor [heads, n_rows, 128] of any head and row stride -> those strides.  A stride that no
+    second head or row uses does not matter and is passed as 0 (128 would be as good)."""
+    if not (t.dtype == torch.bfloat16 and t.dim() == 3 and t.device == device and t.shape[2] == 128
+            and t.stride(2) == 1 and (heads is None or t.shape[0] == heads)):
+        raise ValueError(f"{name} must be a bf16 tensor [{heads or 'heads'}, n_rows, 128] on {device} whose rows are "
+                         f"contiguous, got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
+    return (t.stride(0) if t.shape[0] > 1 else 0), (t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def crisp_cache_append(cache: Cache, table: torch.Tensor, seq_len: torch.Tensor, row_ptr: torch.Tensor,
+                       k: torch.Tensor, v: torch.Tensor) -> None:
+    """K and V rows [H_kv, n_rows, 128] (any head and row strides that are multiples of 8) quantised into the
+    pages behind each sequence's seq_len tokens."""
+    dev = cache.pages.device
+    kh, kr = _rows(k, "k", cache.n_kv_heads, dev)
+    vh, vr = _rows(v, "v", cache.n_kv_heads, dev)
+    if v.shape != k.shape:
+        raise ValueError(f"v {tuple(v.shape)} must have k's shape {tuple(k.shape)}")
+    b = _batch(cache, table, seq_len, row_ptr, k.shape[1])
+    with torch.cuda.device(dev):
+        _check(lib.crisp_cache_append(ctypes.byref(cache.shape), ctypes.byref(b), cache.pages.data_ptr(),
+                                      cache.scales.data_ptr(), table.data_ptr(), seq_len.data_ptr(), row_ptr.data_ptr(),
+                                      k.data_ptr(), kh, kr, v.data_ptr(), vh, vr, _stream(dev)), "crisp_cache_append")
+
+
+def crisp_cache_attn_workspace_size(cache: Cache, n_q_heads: int, n_seqs: int, max_pages: int, n_rows: int) -> int:
+    n = ctypes.c_size_t()
+    b = CrispCacheBatch(n_seqs, max_pages, n_rows)
+    _check(lib.crisp_cache_attn_workspace_size(ctypes.byref(cache.shape), ctypes.byref(b), n_q_heads, ctypes.byref(n)),
+           "crisp_cache_attn_workspace_size")
+    return int(n.value)
+
+
+def cache_workspace(cache: Cache, n_q_heads: int, n_seqs: int, n_rows: int, max_pages: Optional[int] = None) -> torch.Tensor:
+    """A workspace for crisp_cache_attn; without max_pages one that is enough for any table width."""
+    wide = (1 << 30) // cache.block if max_pages is None else max_pages
+    if max_pages is None and n_seqs:
+        wide = min(wide, ((1 << 31) - 1) // n_seqs)
+    nbytes = crisp_cache_attn_workspace_size(cache, n_q_heads, n_seqs, wide, n_rows)
+    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=cache.pages.device)
+
+
+def crisp_cache_attn(cache: Cache, table: torch.Tensor, seq_len: torch.Tensor, row_ptr: torch.Tensor, q: torch.Tensor,
+                     softmax_scale: float = 0.0, ws: Optional[torch.Tensor] = None,
+                     out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of rows q [H_q, n_rows, 128] over the cached tokens (the rows' own appended before)
+    -> o bf16 [H_q, n_rows, 128]; rows that row_ptr does not cover are left as they were in out."""
+    dev = cache.pages.device
+    qh, qr = _rows(q, "q", None, dev)
+    if out is None:
+        o = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+    else:
+        o = out
+        if o.shape != q.shape:
+            raise ValueError(f"out {tuple(o.shape)} must have q's shape {tuple(q.shape)}")
+    oh, orow = _rows(o, "out", None, dev)
+    b = _batch(cache, table, seq_len, row_ptr, q.shape[1])
+    if ws is None:
+        ws = cache_workspace(cache, q.shape[0], b.n_seqs, b.n_rows, b.max_pages)
+    else:
+        _ws(ws, dev)
+    with torch.cuda.device(dev):
+        _check(lib.crisp_cache_attn(ctypes.byref(cache.shape), ctypes.byref(b), q.shape[0], softmax_scale,
+                                    cache.pages.data_ptr(), cache.scales.data_ptr(), table.data_ptr(),
+                                    seq_len.data_ptr(), row_ptr.data_ptr(), q.data_ptr(), qh, qr, o.data_ptr(), oh, orow,
+                                    ws.data_ptr(), ws.numel(), _stream(dev)), "crisp_cache_attn")
+    return o
+
+
+def crisp_cache_copy(cache: Cache, pairs: torch.Tensor, count: Optional[torch.Tensor] = None) -> None:
+    """Page copies: pairs int32 [n, 2] of (from, to), of which the first count[0] count (all without it)."""
+    dev = cache.pages.device
+    _tensor(pairs, "pairs", torch.int32, (None, 2), dev)
+    if count is not None:
+        _tensor(count, "count", torch.int32, (1,), dev)
+    with torch.cuda.device(dev):
+        _check(lib.crisp_cache_copy(ctypes.byref(cache.shape), cache.pages.data_ptr(), cache.scales.data_ptr(),
+                                    pairs.data_ptr(), pairs.shape[0], None if count is None else count.data_ptr(),
+                                    _stream(dev)), "crisp_cache_copy")
+
+
+def crisp_pool_words(n_pages: int) -> int:
+    n = int(lib.crisp_pool_words(n_pages))
+    if n < 0:
+        raise CrispError(CRISP_EINVAL, lib.crisp_last_error().decode())
+    return n
+
+
+def crisp_pool_init(n_pages: int, device="cuda") -> torch.Tensor:
+    """A pool of n_pages pages, none in use: int32 [crisp_pool_words(n_pages)]; pool[:n_pages] are the uses."""
+    if torch.device(device).type != "cuda":
+        raise ValueError(f"a pool lives on a GPU, got device {device}")
+    pool = torch.empty(crisp_pool_words(n_pages), dtype=torch.int32, device=device)
+    with torch.cuda.device(pool.device):
+        _check(lib.crisp_pool_init(n_pages, pool.data_ptr(), _stream(pool.device)), "crisp_pool_init")
+    return pool
+
+
+def pool_pages(pool: torch.Tensor) -> int:
+    """The number of pages that a pool tensor is for."""
+    words = pool.numel()
+    n = words * 32 // 33
+    if n < 1 or n + (n + 31) // 32 != words:
+        raise ValueError(f"{words} words are no pool")
+    return n
+
+
+def _pool(pool: torch.Tensor, table: torch.Tensor, seq_len: Optional[torch.Tensor]) -> int:
+    dev = pool.device
+    _tensor(pool, "pool", torch.int32, (None,), dev)
+    _i32(table, "table", 2, dev)
+    if seq_len is not None:
+        _tensor(seq_len, "seq_len", torch.int32, (table.shape[0],), dev)
+    return pool_pages(pool)
+
+
+def crisp_pool_reserve(pool: torch.Tensor, block: int, table: torch.Tensor, seq_len: torch.Tensor,
+                       counts: torch.Tensor) -> torch.Tensor:
+    """Pages for counts[s] more tokens of each sequence -> granted int32 [n_seqs] (counts[s] or 0)."""
+    n = _pool(pool, table, seq_len)
+    _tensor(counts, "counts", torch.int32, (table.shape[0],), pool.device)
+    granted = torch.empty_like(counts)
+    with torch.cuda.device(pool.device):
+        _check(lib.crisp_pool_reserve(n, block, table.shape[0], table.shape[1], pool.data_ptr(), table.data_ptr(),
+                                      seq_len.data_ptr(), counts.data_ptr(), granted.data_ptr(), _stream(pool.device)),
+               "crisp_pool_reserve")
+    return granted
+
+
+def crisp_pool_fork(pool: torch.Tensor, block: int, table: torch.Tensor, seq_len: torch.Tensor, src: torch.Tensor,
+                    dst: torch.Tensor) -> torch.Tensor:
+    """Sequences dst[i] become copies of src[i] -> copies int32 [n, 2], the page pairs for crisp_cache_copy."""
+    n = _pool(pool, table, seq_len)
+    _tensor(src, "src", torch.int32, (None,), pool.device)
+    _tensor(dst, "dst", torch.int32, (src.shape[0],), pool.device)
+    copies = torch.empty(src.shape[0], 2, dtype=torch.int32, device=pool.device)
+    with torch.cuda.device(pool.device):
+        _check(lib.crisp_pool_fork(n, block, table.shape[0], table.shape[1], pool.data_ptr(), table.data_ptr(),
+                                   seq_len.data_ptr(), src.data_ptr(), dst.data_ptr(), src.shape[0], copies.data_ptr(),
+                                   _stream(pool.device)), "crisp_pool_fork")
+    return copies
+
+
+def crisp_pool_free(pool: torch.Tensor, table: torch.Tensor, seq_len: torch.Tensor, ids: torch.Tensor) -> None:
+    """Sequences ids[i] end: their pages lose a use, their rows become -1, their lengths 0."""
+    n = _pool(pool, table, seq_len)
+    _tensor(ids, "ids", torch.int32, (None,), pool.device)
+    with torch.cuda.device(pool.device):
+        _check(lib.crisp_pool_free(n, table.shape[0], table.shape[1], pool.data_ptr(), table.data_ptr(),
+                                   seq_len.data_ptr(), ids.data_ptr(), ids.shape[0], _stream(pool.device)),
+               "crisp_pool_free")
+
+
+def crisp_pool_compact(pool: torch.Tensor, table: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The pages in use gathered at the front -> (moves int32 [max(1, n_pages // 2), 2], count int32 [1]) for
+    crisp_cache_copy; pool and table follow."""
+    n = _pool(pool, table, None)
+    moves = torch.empty(max(1, n // 2), 2, dtype=torch.int32, device=pool.device)
+    count = torch.empty(1, dtype=torch.int32, device=pool.device)
+    with torch.cuda.device(pool.device):
+        _check(lib.crisp_pool_compact(n, table.shape[0], table.shape[1], pool.data_ptr(), table.data_ptr(),
+                                      moves.data_ptr(), count.data_ptr(), _stream(pool.device)), "crisp_pool_compact")
+    return moves, count

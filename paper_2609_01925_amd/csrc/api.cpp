@@ -29,6 +29,13 @@ crisp_status fail(crisp_status s, const char* fmt, ...) {
   return s;
 }
 
+}  // namespace
+
+// The message of a failing call of the other host layers (cache_api.cpp).
+void set_error(const char* msg) { snprintf(g_err, sizeof(g_err), "%s", msg); }
+
+namespace {
+
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
