@@ -355,6 +355,7 @@ class Cache:
         self.pages, self.scales, self.fmt = pages, scales, fmt
         self.n_pages, self.n_kv_heads, self.block = pages.shape[0], pages.shape[1], 64 * pages.shape[2]
         self.shape = CrispCacheShape(self.n_pages, self.n_kv_heads, 128, self.block, fmt)
+        self._ref, self._gpu = ctypes.byref(self.shape), pages.get_device()
         crisp_cache_bytes(self.shape)  # raises on a size or format that the library does not take
 
 
@@ -372,48 +373,62 @@ def crisp_cache_bytes(shape: CrispCacheShape) -> Tuple[int, int]:
     return int(a.value), int(b.value)
 
 
-def _i32(t: torch.Tensor, name: str, dims: int, device):
-    if not (t.dtype == torch.int32 and t.dim() == dims and t.device == device and t.is_contiguous()):
-        raise ValueError(f"{name} must be a contiguous {dims}-d int32 tensor on {device}, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+def _call(gpu: int, what: str, fn, *args) -> None:
+    """fn(*args, the GPU's current stream) with that GPU as the current device.  These calls are made once
+    a layer and token, so the checks before them are kept short."""
+    if torch.cuda.current_device() == gpu:
+        status = fn(*args, torch._C._cuda_getCurrentRawStream(gpu))
+    else:
+        with torch.cuda.device(gpu):
+            status = fn(*args, torch._C._cuda_getCurrentRawStream(gpu))
+    if status != CRISP_OK:
+        _check(status, what)
 
 
-def _batch(cache: Cache, table, seq_len, row_ptr, n_rows: int) -> CrispCacheBatch:
-    dev = cache.pages.device
-    _i32(table, "table", 2, dev)
-    _i32(seq_len, "seq_len", 1, dev)
-    _i32(row_ptr, "row_ptr", 1, dev)
-    n = table.shape[0]
-    if seq_len.shape[0] != n or row_ptr.shape[0] != n + 1:
-        raise ValueError(f"table {tuple(table.shape)}, seq_len {tuple(seq_len.shape)} and row_ptr "
-                         f"{tuple(row_ptr.shape)} must be [n, pages], [n] and [n + 1]")
-    return CrispCacheBatch(n, table.shape[1], n_rows)
+def _i32(t: torch.Tensor, name: str, dims: int, gpu: int) -> torch.Size:
+    shape = t.shape
+    if t.dtype is not torch.int32 or len(shape) != dims or t.get_device() != gpu or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dims}-d int32 tensor on cuda:{gpu}, "
+                         f"got {t.dtype} {tuple(shape)} on {t.device}")
+    return shape
 
 
-def _rows(t: torch.Tensor, name: str, heads: Optional[int], device) -> Tuple[int, int]:
-    """A packed tensor [heads, n_rows, 128] of any head and row stride -> those strides.  A stride that no
-    second head or row uses does not matter and is passed as 0 (128 would be as good)."""
-    if not (t.dtype == torch.bfloat16 and t.dim() == 3 and t.device == device and t.shape[2] == 128
-            and t.stride(2) == 1 and (heads is None or t.shape[0] == heads)):
-        raise ValueError(f"{name} must be a bf16 tensor [{heads or 'heads'}, n_rows, 128] on {device} whose rows are "
-                         f"contiguous, got {t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
-    return (t.stride(0) if t.shape[0] > 1 else 0), (t.stride(1) if t.shape[1] > 1 else 0)
+def _i32_of(t: torch.Tensor, name: str, shape, gpu: int) -> None:
+    if _i32(t, name, len(shape), gpu) != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _batch(gpu: int, table, seq_len, row_ptr, n_rows: int) -> CrispCacheBatch:
+    n, wide = _i32(table, "table", 2, gpu)
+    _i32_of(seq_len, "seq_len", (n,), gpu)
+    _i32_of(row_ptr, "row_ptr", (n + 1,), gpu)
+    return CrispCacheBatch(n, wide, n_rows)
+
+
+def _rows(t: torch.Tensor, name: str, heads: Optional[int], gpu: int) -> Tuple[int, int, int, int]:
+    """A packed tensor [heads, n_rows, 128] of any head and row stride -> heads, n_rows and those strides, 0
+    where there is no second head or row."""
+    shape, stride = t.shape, t.stride()
+    if (t.dtype is not torch.bfloat16 or len(shape) != 3 or t.get_device() != gpu or shape[2] != 128 or stride[2] != 1
+            or (heads is not None and shape[0] != heads)):
+        raise ValueError(f"{name} must be a bf16 tensor [{'heads' if heads is None else heads}, n_rows, 128] on cuda:{gpu} "
+                         f"whose rows are contiguous, got {t.dtype} {tuple(shape)} strides {stride} on {t.device}")
+    return shape[0], shape[1], stride[0] if shape[0] > 1 else 0, stride[1] if shape[1] > 1 else 0
 
 
 def crisp_cache_append(cache: Cache, table: torch.Tensor, seq_len: torch.Tensor, row_ptr: torch.Tensor,
                        k: torch.Tensor, v: torch.Tensor) -> None:
     """K and V rows [H_kv, n_rows, 128] (any head and row strides that are multiples of 8) quantised into the
     pages behind each sequence's seq_len tokens."""
-    dev = cache.pages.device
-    kh, kr = _rows(k, "k", cache.n_kv_heads, dev)
-    vh, vr = _rows(v, "v", cache.n_kv_heads, dev)
-    if v.shape != k.shape:
+    gpu = cache._gpu
+    heads, n, kh, kr = _rows(k, "k", cache.n_kv_heads, gpu)
+    _, m, vh, vr = _rows(v, "v", heads, gpu)
+    if m != n:
         raise ValueError(f"v {tuple(v.shape)} must have k's shape {tuple(k.shape)}")
-    b = _batch(cache, table, seq_len, row_ptr, k.shape[1])
-    with torch.cuda.device(dev):
-        _check(lib.crisp_cache_append(ctypes.byref(cache.shape), ctypes.byref(b), cache.pages.data_ptr(),
-                                      cache.scales.data_ptr(), table.data_ptr(), seq_len.data_ptr(), row_ptr.data_ptr(),
-                                      k.data_ptr(), kh, kr, v.data_ptr(), vh, vr, _stream(dev)), "crisp_cache_append")
+    b = _batch(gpu, table, seq_len, row_ptr, n)
+    _call(gpu, "crisp_cache_append", lib.crisp_cache_append, cache._ref, b, cache.pages.data_ptr(),
+          cache.scales.data_ptr(), table.data_ptr(), seq_len.data_ptr(), row_ptr.data_ptr(), k.data_ptr(), kh, kr,
+          v.data_ptr(), vh, vr)
 
 
 def crisp_cache_attn_workspace_size(cache: Cache, n_q_heads: int, n_seqs: int, max_pages: int, n_rows: int) -> int:
@@ -438,38 +453,33 @@ def crisp_cache_attn(cache: Cache, table: torch.Tensor, seq_len: torch.Tensor, r
                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of rows q [H_q, n_rows, 128] over the cached tokens (the rows' own appended before)
     -> o bf16 [H_q, n_rows, 128]; rows that row_ptr does not cover are left as they were in out."""
-    dev = cache.pages.device
-    qh, qr = _rows(q, "q", None, dev)
-    if out is None:
-        o = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
-    else:
-        o = out
-        if o.shape != q.shape:
-            raise ValueError(f"out {tuple(o.shape)} must have q's shape {tuple(q.shape)}")
-    oh, orow = _rows(o, "out", None, dev)
-    b = _batch(cache, table, seq_len, row_ptr, q.shape[1])
+    gpu = cache._gpu
+    heads, n, qh, qr = _rows(q, "q", None, gpu)
+    o = torch.empty((heads, n, 128), dtype=torch.bfloat16, device=q.device) if out is None else out
+    _, m, oh, orow = _rows(o, "out", heads, gpu)
+    if m != n:
+        raise ValueError(f"out {tuple(o.shape)} must have q's shape {tuple(q.shape)}")
+    b = _batch(gpu, table, seq_len, row_ptr, n)
     if ws is None:
-        ws = cache_workspace(cache, q.shape[0], b.n_seqs, b.n_rows, b.max_pages)
-    else:
-        _ws(ws, dev)
-    with torch.cuda.device(dev):
-        _check(lib.crisp_cache_attn(ctypes.byref(cache.shape), ctypes.byref(b), q.shape[0], softmax_scale,
-                                    cache.pages.data_ptr(), cache.scales.data_ptr(), table.data_ptr(),
-                                    seq_len.data_ptr(), row_ptr.data_ptr(), q.data_ptr(), qh, qr, o.data_ptr(), oh, orow,
-                                    ws.data_ptr(), ws.numel(), _stream(dev)), "crisp_cache_attn")
+        ws = cache_workspace(cache, heads, b.n_seqs, n, b.max_pages)
+    elif ws.dtype is not torch.uint8 or ws.get_device() != gpu or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous uint8 tensor on cuda:{gpu}, got {ws.dtype} on {ws.device}")
+    _call(gpu, "crisp_cache_attn", lib.crisp_cache_attn, cache._ref, b, heads, softmax_scale, cache.pages.data_ptr(),
+          cache.scales.data_ptr(), table.data_ptr(), seq_len.data_ptr(), row_ptr.data_ptr(), q.data_ptr(), qh, qr,
+          o.data_ptr(), oh, orow, ws.data_ptr(), ws.numel())
     return o
 
 
 def crisp_cache_copy(cache: Cache, pairs: torch.Tensor, count: Optional[torch.Tensor] = None) -> None:
     """Page copies: pairs int32 [n, 2] of (from, to), of which the first count[0] count (all without it)."""
-    dev = cache.pages.device
-    _tensor(pairs, "pairs", torch.int32, (None, 2), dev)
+    gpu = cache._gpu
+    n, two = _i32(pairs, "pairs", 2, gpu)
+    if two != 2:
+        raise ValueError(f"pairs must have shape [n, 2], got {tuple(pairs.shape)}")
     if count is not None:
-        _tensor(count, "count", torch.int32, (1,), dev)
-    with torch.cuda.device(dev):
-        _check(lib.crisp_cache_copy(ctypes.byref(cache.shape), cache.pages.data_ptr(), cache.scales.data_ptr(),
-                                    pairs.data_ptr(), pairs.shape[0], None if count is None else count.data_ptr(),
-                                    _stream(dev)), "crisp_cache_copy")
+        _i32_of(count, "count", (1,), gpu)
+    _call(gpu, "crisp_cache_copy", lib.crisp_cache_copy, cache._ref, cache.pages.data_ptr(), cache.scales.data_ptr(),
+          pairs.data_ptr(), n, None if count is None else count.data_ptr())
 
 
 def crisp_pool_words(n_pages: int) -> int:
@@ -484,8 +494,7 @@ def crisp_pool_init(n_pages: int, device="cuda") -> torch.Tensor:
     if torch.device(device).type != "cuda":
         raise ValueError(f"a pool lives on a GPU, got device {device}")
     pool = torch.empty(crisp_pool_words(n_pages), dtype=torch.int32, device=device)
-    with torch.cuda.device(pool.device):
-        _check(lib.crisp_pool_init(n_pages, pool.data_ptr(), _stream(pool.device)), "crisp_pool_init")
+    _call(pool.get_device(), "crisp_pool_init", lib.crisp_pool_init, n_pages, pool.data_ptr())
     return pool
 
 
@@ -498,59 +507,55 @@ def pool_pages(pool: torch.Tensor) -> int:
     return n
 
 
-def _pool(pool: torch.Tensor, table: torch.Tensor, seq_len: Optional[torch.Tensor]) -> int:
-    dev = pool.device
-    _tensor(pool, "pool", torch.int32, (None,), dev)
-    _i32(table, "table", 2, dev)
+def _pool(pool: torch.Tensor, table: torch.Tensor, seq_len: Optional[torch.Tensor]) -> Tuple[int, int, int, int]:
+    """GPU, pages, sequences, slots of a sequence."""
+    gpu = pool.get_device()
+    if gpu < 0:
+        raise ValueError(f"pool must be a CUDA tensor, got one on {pool.device}")
+    _i32(pool, "pool", 1, gpu)
+    n_seqs, wide = _i32(table, "table", 2, gpu)
     if seq_len is not None:
-        _tensor(seq_len, "seq_len", torch.int32, (table.shape[0],), dev)
-    return pool_pages(pool)
+        _i32_of(seq_len, "seq_len", (n_seqs,), gpu)
+    return gpu, pool_pages(pool), n_seqs, wide
 
 
 def crisp_pool_reserve(pool: torch.Tensor, block: int, table: torch.Tensor, seq_len: torch.Tensor,
                        counts: torch.Tensor) -> torch.Tensor:
     """Pages for counts[s] more tokens of each sequence -> granted int32 [n_seqs] (counts[s] or 0)."""
-    n = _pool(pool, table, seq_len)
-    _tensor(counts, "counts", torch.int32, (table.shape[0],), pool.device)
+    gpu, n, n_seqs, wide = _pool(pool, table, seq_len)
+    _i32_of(counts, "counts", (n_seqs,), gpu)
     granted = torch.empty_like(counts)
-    with torch.cuda.device(pool.device):
-        _check(lib.crisp_pool_reserve(n, block, table.shape[0], table.shape[1], pool.data_ptr(), table.data_ptr(),
-                                      seq_len.data_ptr(), counts.data_ptr(), granted.data_ptr(), _stream(pool.device)),
-               "crisp_pool_reserve")
+    _call(gpu, "crisp_pool_reserve", lib.crisp_pool_reserve, n, block, n_seqs, wide, pool.data_ptr(), table.data_ptr(),
+          seq_len.data_ptr(), counts.data_ptr(), granted.data_ptr())
     return granted
 
 
 def crisp_pool_fork(pool: torch.Tensor, block: int, table: torch.Tensor, seq_len: torch.Tensor, src: torch.Tensor,
                     dst: torch.Tensor) -> torch.Tensor:
     """Sequences dst[i] become copies of src[i] -> copies int32 [n, 2], the page pairs for crisp_cache_copy."""
-    n = _pool(pool, table, seq_len)
-    _tensor(src, "src", torch.int32, (None,), pool.device)
-    _tensor(dst, "dst", torch.int32, (src.shape[0],), pool.device)
-    copies = torch.empty(src.shape[0], 2, dtype=torch.int32, device=pool.device)
-    with torch.cuda.device(pool.device):
-        _check(lib.crisp_pool_fork(n, block, table.shape[0], table.shape[1], pool.data_ptr(), table.data_ptr(),
-                                   seq_len.data_ptr(), src.data_ptr(), dst.data_ptr(), src.shape[0], copies.data_ptr(),
-                                   _stream(pool.device)), "crisp_pool_fork")
+    gpu, n, n_seqs, wide = _pool(pool, table, seq_len)
+    m, = _i32(src, "src", 1, gpu)
+    _i32_of(dst, "dst", (m,), gpu)
+    copies = torch.empty((m, 2), dtype=torch.int32, device=pool.device)
+    _call(gpu, "crisp_pool_fork", lib.crisp_pool_fork, n, block, n_seqs, wide, pool.data_ptr(), table.data_ptr(),
+          seq_len.data_ptr(), src.data_ptr(), dst.data_ptr(), m, copies.data_ptr())
     return copies
 
 
 def crisp_pool_free(pool: torch.Tensor, table: torch.Tensor, seq_len: torch.Tensor, ids: torch.Tensor) -> None:
     """Sequences ids[i] end: their pages lose a use, their rows become -1, their lengths 0."""
-    n = _pool(pool, table, seq_len)
-    _tensor(ids, "ids", torch.int32, (None,), pool.device)
-    with torch.cuda.device(pool.device):
-        _check(lib.crisp_pool_free(n, table.shape[0], table.shape[1], pool.data_ptr(), table.data_ptr(),
-                                   seq_len.data_ptr(), ids.data_ptr(), ids.shape[0], _stream(pool.device)),
-               "crisp_pool_free")
+    gpu, n, n_seqs, wide = _pool(pool, table, seq_len)
+    m, = _i32(ids, "ids", 1, gpu)
+    _call(gpu, "crisp_pool_free", lib.crisp_pool_free, n, n_seqs, wide, pool.data_ptr(), table.data_ptr(),
+          seq_len.data_ptr(), ids.data_ptr(), m)
 
 
 def crisp_pool_compact(pool: torch.Tensor, table: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """The pages in use gathered at the front -> (moves int32 [max(1, n_pages // 2), 2], count int32 [1]) for
     crisp_cache_copy; pool and table follow."""
-    n = _pool(pool, table, None)
-    moves = torch.empty(max(1, n // 2), 2, dtype=torch.int32, device=pool.device)
+    gpu, n, n_seqs, wide = _pool(pool, table, None)
+    moves = torch.empty((max(1, n // 2), 2), dtype=torch.int32, device=pool.device)
     count = torch.empty(1, dtype=torch.int32, device=pool.device)
-    with torch.cuda.device(pool.device):
-        _check(lib.crisp_pool_compact(n, table.shape[0], table.shape[1], pool.data_ptr(), table.data_ptr(),
-                                      moves.data_ptr(), count.data_ptr(), _stream(pool.device)), "crisp_pool_compact")
+    _call(gpu, "crisp_pool_compact", lib.crisp_pool_compact, n, n_seqs, wide, pool.data_ptr(), table.data_ptr(),
+          moves.data_ptr(), count.data_ptr())
     return moves, count

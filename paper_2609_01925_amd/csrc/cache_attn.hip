@@ -11,9 +11,17 @@ namespace crisp {
 
 namespace {
 
-constexpr int kWaves = 4;
-constexpr int kThreads = kWaves * kWave;
-constexpr int kMinShare = 4;  // tiles a workgroup takes at least: one a wave
+constexpr int kJoinWaves = 4;
+// Tiles that are not cut apart: one a wave.  Sequences of 2000 tokens, 32 heads over 8, grains of 4 / 8 / 16, us: one
+// sequence 9.3 / 10.3 / 12.0, 4 10.8 / 10.3 / 12.0, 16 20.6 / 17.6 / 19.7, 64 40.5 / 42.5 / 36.2; one of 6000 9.9 / 10.5 / 11.7.
+constexpr int kGrain = 4;
+
+// The unit that the boundary behind a workgroup's share cuts: the first workgroup with a piece of it and
+// the number of boundaries inside it (0: the boundary cuts none), KV head, first row in
+// the order i G + g, number of rows, first row of the sequence.
+struct Cut {
+  int first, cuts, head, row, rows, row0;
+};
 
 struct AttnArgs {
   CacheDims c;
@@ -26,8 +34,10 @@ struct AttnArgs {
   uint16_t* o;
   Strides os;
   int G;
+  int grain;    // tiles
   float c2;     // scale log2(e)
-  float* part;  // [2 gridDim.x][16 C][128 + 2]
+  Cut* cut;     // [gridDim.x]; null where no unit has more than one grain
+  float* part;  // [2 gridDim.x][rows of a unit x 128, M, L]
 };
 
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float acc4;
@@ -38,7 +48,7 @@ __device__ __forceinline__ acc4 mfma16(bf16x8 a, bf16x8 b, acc4 c) {
 
 // Keeps a loaded chunk in its four registers up to here: left to itself the compiler splits what
 // the loop carries into single codes, a register each.
-__device__ __forceinline__ void keep_whole(u32x4& x) { asm volatile("" : "+v"(x)); }
+__device__ __forceinline__ void keep_whole(u32x4& x) { asm("" : "+v"(x)); }
 
 // The value of all four lanes that hold a column (lanes l, l ^ 16, l ^ 32, l ^ 48) combined.
 template <typename Op>
@@ -49,94 +59,239 @@ __device__ __forceinline__ float column(float x, Op op) {
   return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// What a sequence's units are: nrt groups of 16 C rows for each KV head, each over T tiles (one at
-// least, so that rows that see nothing are written too).
-template <int C>
+// What a sequence's units are: nrt groups of R rows for each KV head, each over T tiles (one at
+// least, so that rows that see nothing are written too).  Where the work is divided, a unit counts in
+// grains of so many tiles, the last perhaps smaller, and is cut between grains only.
+template <int R>
 struct SeqWork {
   SeqRows r;
-  int T, nrt;
-  int64_t tiles;
+  int T, nrt, grains;
   __device__ __forceinline__ SeqWork() {}
-  __device__ __forceinline__ SeqWork(const AttnArgs& a, int s) {
-    r = seq_rows(a.s, a.b, a.c.B, s);
+  __device__ __forceinline__ SeqWork(const AttnArgs& a, SeqRows rows) : r(rows) {
     const int end = min(r.len + r.n, a.b.max_pages * a.c.B);
     T = max((end + kTile - 1) / kTile, 1);
-    nrt = (int)(((int64_t)r.n * a.G + 16 * C - 1) / (16 * C));
-    tiles = (int64_t)a.c.hkv * nrt * T;
+    nrt = (r.n * a.G + R - 1) / R;
+    grains = (T + a.grain - 1) / a.grain;
+  }
+  __device__ __forceinline__ int64_t all(const AttnArgs& a) const { return (int64_t)a.c.hkv * nrt * grains; }
+};
+
+__device__ __forceinline__ int64_t div64(int64_t x, int64_t y) {  // x, y >= 0; both are small but for the longest calls
+  return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
+// The units of all sequences in a row, cut into equal shares.  Up to 64 sequences every wave looks
+// them over by itself, one a lane; more are counted by the workgroup, some a thread.
+template <int R, int NW>
+struct Places {
+  int64_t total, share;
+  int64_t end, own;  // of this lane's sequence (few), of this thread's sequences (many)
+  SeqRows mine;
+  bool few;
+  int per;
+
+  __device__ __forceinline__ void count(const AttnArgs& a, int workgroups, int64_t* lds) {
+    few = a.b.n_seqs <= kWave;
+    own = 0;
+    if (few) {
+      const int lane = lane_id();
+      mine = SeqRows{0, 0, 0};
+      if (lane < a.b.n_seqs) {
+        mine = seq_rows(a.s, a.b, a.c.B, lane);
+        own = SeqWork<R>(a, mine).all(a);
+      }
+      end = wave_scan(own);
+      total = lane_value(end, kWave - 1);
+    } else {
+      per = (a.b.n_seqs + NW * kWave - 1) / (NW * kWave);
+      for (int i = 0; i < per; ++i) {
+        const int s = (int)threadIdx.x * per + i;
+        if (s < a.b.n_seqs) own += SeqWork<R>(a, seq_rows(a.s, a.b, a.c.B, s)).all(a);
+      }
+      end = block_scan<int64_t, NW>(own, lds, &total);
+    }
+    total = lane_value(total, 0);
+    share = max(div64(total + workgroups - 1, workgroups), (int64_t)1);
+  }
+
+  static __device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, lane) |
+                     (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32);
+  }
+
+  // Sequence s's part of the work.
+  __device__ __forceinline__ SeqWork<R> work(const AttnArgs& a, int s) const {
+    if (!few) return SeqWork<R>(a, seq_rows(a.s, a.b, a.c.B, s));
+    return SeqWork<R>(a, SeqRows{__builtin_amdgcn_readlane(mine.len, s), __builtin_amdgcn_readlane(mine.row0, s),
+                                 __builtin_amdgcn_readlane(mine.n, s)});
+  }
+
+  // The sequence that holds place `pos` < total, and *base, the places before it.
+  __device__ __forceinline__ int find(const AttnArgs& a, int64_t pos, int64_t* lds, int64_t* base) const {
+    if (few) {
+      const int s = __builtin_ctzll(__ballot(pos < end));
+      *base = lane_value(end - own, s);
+      return s;
+    }
+    if (pos >= end - own && pos < end) {
+      int64_t b = end - own;
+      int s = (int)threadIdx.x * per;
+      for (int64_t t; (t = SeqWork<R>(a, seq_rows(a.s, a.b, a.c.B, s)).all(a)) + b <= pos; ++s) b += t;  // ends: pos < end
+      lds[NW] = b;
+      lds[NW + 1] = s;
+    }
+    __syncthreads();
+    *base = lane_value(lds[NW], 0);
+    return __builtin_amdgcn_readfirstlane((int)lds[NW + 1]);
   }
 };
 
-// All sequences' tiles in a row, cut into equal shares: total, share, and the sequence that holds
-// tile `pos` with the number of tiles before it.
-struct Place {
-  int64_t total, share, base;
-  int seq;
+// The cut, if any, that a share leaves behind it: it ends `done` of `grains` into the unit.
+__device__ __forceinline__ Cut cut_of(int64_t share, int64_t base, int unit, int grains, int done, int head, int row, int rows,
+                                      int row0) {
+  Cut k{0, 0, head, row, rows, row0};
+  if (done < grains) {
+    const int64_t first = base + (int64_t)unit * grains;
+    k.first = (int)div64(first, share);
+    k.cuts = (int)div64(first + grains - 1, share) - k.first;
+  }
+  return k;
+}
+
+struct TileInfo {
+  int t, page, ev;  // tile of the sequence, its page (-1: no tile is left), exponent of V
+  float kc;         // scale of K times the softmax's
 };
 
-template <int C>
-__device__ __forceinline__ void count_tiles(const AttnArgs& a, int workgroups, int64_t* lds, Place* p, int64_t* end,
-                                            int64_t* own) {
-  const int per = (a.b.n_seqs + kThreads - 1) / kThreads;
-  int64_t sum = 0;
-  for (int i = 0; i < per; ++i) {
-    const int s = (int)threadIdx.x * per + i;
-    if (s < a.b.n_seqs) sum += SeqWork<C>(a, s).tiles;
+// The mapped tiles among t0, t0 + STEP, ... < end of one sequence and KV head.  64 are looked up in one round
+// of loads, one a lane, and then read from their lanes.
+template <int STEP>
+struct TileList {
+  const int32_t* row;
+  int tb, end, pg, ev;
+  float kc;
+  uint64_t todo;
+
+  __device__ __forceinline__ TileList(const AttnArgs& a, int s, int head, int t0, int t_end)
+      : row(a.s.table + (int64_t)s * a.b.max_pages), tb(t0 - STEP * kWave), end(t_end), pg(0), ev(0), kc(0.f), todo(0) {}
+
+  __device__ __forceinline__ TileInfo next(const AttnArgs& a, int head) {
+    while (todo == 0 && tb + STEP * kWave < end) {
+      tb += STEP * kWave;
+      const int t = tb + STEP * lane_id(), slot = a.c.tiles == 2 ? t >> 1 : t;
+      pg = t < end && slot < a.b.max_pages ? row[slot] : -1;
+      const bool ok = pg >= 0 && pg < a.c.n_pages;
+      todo = __ballot(ok);
+      if (ok) {
+        const float* sc = a.scales + ((int64_t)pg * a.c.hkv + head) * 2;
+        kc = pow2f(stored_exp(sc[0])) * a.c2;
+        ev = stored_exp(sc[1]);
+      }
+    }
+    if (todo == 0) return TileInfo{0, -1, 0, 0.f};
+    const int i = __builtin_ctzll(todo);
+    todo &= todo - 1;
+    return TileInfo{tb + STEP * i, __builtin_amdgcn_readlane(pg, i), __builtin_amdgcn_readlane(ev, i),
+                    __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kc), i))};
   }
-  *own = sum;
-  *end = block_scan<int64_t, kWaves>(sum, lds, &p->total);
-  p->share = max((p->total + workgroups - 1) / workgroups, (int64_t)kMinShare);
+
+  __device__ __forceinline__ const uint8_t* at(const AttnArgs& a, const TileInfo& x, int head) const {
+    return a.pages + (((int64_t)x.page * a.c.hkv + head) * a.c.tiles + (a.c.tiles == 2 ? x.t & 1 : 0)) * (2 * kTileBytes);
+  }
+};
+
+// One tile's softmax for C groups of columns: S (raw products, register i of score tile ti is key
+// 16 g + 4 ti + i) becomes P, the next product's operands; kc takes S to the base-2 exponent, and P is made as
+// 2^ev p, what V's codes are to be multiplied by.  The probabilities are formed against the reference M
+// of their column at once, without looking for the tile's maximum; they stand while a lane's sum of them is
+// at most 2^8, so that every p is, where its bf16 rounding is that of one below 1 and the 32-bit sums have
+// room.  Otherwise, and for a column without a reference, M is raised to the maximum, O and L are
+// rescaled, and P is formed again.  L sums the rounded p's, which are what PV adds.
+template <int C>
+__device__ __forceinline__ void softmax_step(const acc4 (&S)[C][4], float kc, int ev, float (&M)[C], float (&L)[C],
+                                             acc4 (&O)[C][8], bf16x8 (&P)[C][2]) {
+  const float inv_v = pow2f(-ev);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const auto form = [&] {
+      const float sub = M[c] - (float)ev;
+      float sum = 0.f;
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        float p[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = fast_exp2(__builtin_fmaf(S[c][2 * st + e / 4][e & 3], kc, -sub));
+        const bf16x2 x = pack_bf16(p[0], p[1]), y = pack_bf16(p[2], p[3]), z = pack_bf16(p[4], p[5]), v = pack_bf16(p[6], p[7]);
+        sum = dot2_bf16_sum(v, dot2_bf16_sum(z, dot2_bf16_sum(y, dot2_bf16_sum(x, sum))));
+        P[c][st] = bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], v[0], v[1]};
+      }
+      return sum * inv_v;
+    };
+    float sum = form();
+    if (__ballot(!(sum <= 256.f))) {  // also an infinity or NaN, as from M = -inf
+      float mx = S[c][0][0];
+#pragma unroll
+      for (int ti = 0; ti < 4; ++ti)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S[c][ti][i]);
+      mx = column(mx, [](float x, float y) { return fmaxf(x, y); }) * kc;
+      const float m = fmaxf(M[c], mx);
+      if (m != M[c]) {
+        const float f = fast_exp2(M[c] - m);
+        L[c] *= f;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) O[c][dt][i] *= f;
+        M[c] = m;
+      }
+      sum = form();
+      if (M[c] == -__builtin_inff()) {  // this column has seen no key yet
+        sum = 0.f;
+        P[c][0] = P[c][1] = bf16x8{};
+      }
+    }
+    L[c] += sum;
+  }
 }
 
-template <int C>
-__device__ __forceinline__ void find_tile(const AttnArgs& a, int64_t pos, int64_t end, int64_t own, int64_t* lds, Place* p) {
-  if (pos >= end - own && pos < end) {
-    const int per = (a.b.n_seqs + kThreads - 1) / kThreads;
-    int64_t base = end - own;
-    int s = (int)threadIdx.x * per;
-    for (int64_t t; (t = SeqWork<C>(a, s).tiles) + base <= pos; ++s) base += t;  // ends: pos < end
-    lds[kWaves] = base;
-    lds[kWaves + 1] = s;
-  }
-  __syncthreads();
-  p->base = lds[kWaves];
-  p->seq = (int)lds[kWaves + 1];
-}
-
-// One workgroup's share.  Tiles of a unit go round the four waves; each wave keeps its own running
+// One workgroup's share.  Tiles of a unit go round the waves; each wave keeps its own running
 // maximum, sum and output, joined through LDS at the unit's end.  A lane's 16-byte loads are
 // matrix operands as they stand (cache_device.h): K of the next tile is loaded while the softmax
 // and PV of this one run, V while the next scores are made, nothing passes through LDS.
-template <int FMT, int C>
-__global__ __launch_bounds__(kThreads, C == 4 ? 1 : 2) void cache_attn(AttnArgs a) {
-  constexpr int kRows = 16 * C;
-  __shared__ __attribute__((aligned(16))) float xo[2][C][8][kWave][4];
-  __shared__ float xm[kWaves][kRows], xl[kWaves][kRows];
-  __shared__ int64_t lds[kWaves + 2];
+template <int FMT, int NW>
+__global__ __launch_bounds__(NW * kWave, 2) void cache_attn(AttnArgs a) {
+  constexpr int C = 1, kRows = 16 * C;
+  __shared__ __attribute__((aligned(16))) float xo[NW][C][8][kWave][4];
+  __shared__ float xm[NW][kRows], xl[NW][kRows];
+  __shared__ int64_t lds[NW + 2];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, g = lane >> 4;
   const int wgs = gridDim.x;
   // workgroup i runs on XCD i % 8: neighbouring shares go to one XCD, whose L2 then serves the row
   // groups that read the same keys
   const int wg = wgs % kNumXcd == 0 ? (int)blockIdx.x % kNumXcd * (wgs / kNumXcd) + (int)blockIdx.x / kNumXcd : (int)blockIdx.x;
-  Place pl;
-  int64_t end, own;
-  count_tiles<C>(a, wgs, lds, &pl, &end, &own);
+  Places<kRows, NW> pl;
+  pl.count(a, wgs, lds);
   int64_t pos = wg * pl.share;
   const int64_t stop = min(pos + pl.share, pl.total);
-  if (pos >= stop) return;
-  find_tile<C>(a, pos, end, own, lds, &pl);
-  int s = pl.seq;
-  int64_t base = pl.base;
-  SeqWork<C> sw(a, s);
+  if (pos >= stop) {
+    if (a.cut && tid == 0) a.cut[wg].cuts = 0;
+    return;
+  }
+  int64_t base;
+  int s = pl.find(a, pos, lds, &base);
+  SeqWork<kRows> sw = pl.work(a, s);
   while (pos < stop) {
-    while (pos >= base + sw.tiles) {
-      base += sw.tiles;
-      sw = SeqWork<C>(a, ++s);
+    while (pos >= base + sw.all(a)) {
+      base += sw.all(a);
+      sw = pl.work(a, ++s);
     }
     const int64_t off = pos - base;
-    const int unit = (int)(off / sw.T), u0 = (int)(off % sw.T);
+    const int unit = (int)div64(off, sw.grains), u0 = (int)(off - (int64_t)unit * sw.grains);
     const int rt = unit % sw.nrt, head = unit / sw.nrt;
-    const int take = (int)min((int64_t)(sw.T - u0), stop - pos);
+    const int part = (int)min((int64_t)(sw.grains - u0), stop - pos);
+    const int t0 = u0 * a.grain, t1 = min((u0 + part) * a.grain, sw.T);  // the tiles of this piece
     const int rows = sw.r.n * a.G;  // fits: n_rows G is checked on the host
     const int held = min(sw.r.len + sw.r.n, a.b.max_pages * a.c.B);
     // q: lane holds its column's elements 32 g + [0, 32)
@@ -160,59 +315,40 @@ __global__ __launch_bounds__(kThreads, C == 4 ? 1 : 2) void cache_attn(AttnArgs 
     float M[C], L[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      M[c] = -__builtin_inff();
+      M[c] = see[c] >= 0 ? -__builtin_inff() : 0.f;  // a column without a row asks for no reference
       L[c] = 0.f;
 #pragma unroll
       for (int dt = 0; dt < 8; ++dt) O[c][dt] = acc4{0.f, 0.f, 0.f, 0.f};
     }
-    const int t_end = min(u0 + take, see_last / kTile + 1);
-    const int32_t* row = a.s.table + (int64_t)s * a.b.max_pages;
-    // this wave's next tile from t on whose page is mapped, and the page; t_end if there is none
-    const auto mapped = [&](int& t) {
-      for (; t < t_end; t += kWaves) {
-        const int slot = t / a.c.tiles;
-        const int p = __builtin_amdgcn_readfirstlane(slot < a.b.max_pages ? row[slot] : -1);
-        if (p >= 0 && p < a.c.n_pages) return p;
-      }
-      return -1;
-    };
-    const auto load = [&](u32x4* x, int t, int p, int tensor) {
-      const uint8_t* src = a.pages + (((int64_t)p * a.c.hkv + head) * a.c.tiles + t % a.c.tiles) * (2 * kTileBytes) +
-                           tensor * kTileBytes + lane * kChunk;
+    TileList<NW> list(a, s, head, t0 + w, min(t1, see_last / kTile + 1));
+    const auto load = [&](u32x4* x, const TileInfo& tl, int tensor) {
+      const uint8_t* src = list.at(a, tl, head) + tensor * kTileBytes + lane * kChunk;
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const u32x4*>(src + i * (kWave * kChunk));
     };
     u32x4 K[8], V[8];
-    int t = u0 + w;
-    int page = mapped(t);
-    if (page >= 0) {
-      load(K, t, page, 0);
-      load(V, t, page, 1);
+    TileInfo now = list.next(a, head);
+    if (now.page >= 0) {
+      load(K, now, 0);
+      load(V, now, 1);
     }
-    while (page >= 0) {
-      int t_next = t + kWaves;
-      const int next = mapped(t_next);
-      const float* sc = a.scales + ((int64_t)page * a.c.hkv + head) * 2;
-      const float kc = pow2f(stored_exp(sc[0])) * a.c2;
-      const int ev = stored_exp(sc[1]);
+    while (now.page >= 0) {
+      const TileInfo next = list.next(a, head);
       acc4 S[C][4];
 #pragma unroll
-      for (int ti = 0; ti < 4; ++ti) {
+      for (int j = 0; j < 4; ++j)  // by steps of d, so that products into one accumulator are apart
 #pragma unroll
-        for (int c = 0; c < C; ++c) S[c][ti] = acc4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int ti = 0; ti < 4; ++ti) {
           if (j % 2 == 0) keep_whole(K[2 * ti + j / 2]);
           const u32x4 x = K[2 * ti + j / 2];
           const bf16x8 k = codes_to_bf16<FMT>(x[2 * (j & 1)], x[2 * (j & 1) + 1]);
 #pragma unroll
-          for (int c = 0; c < C; ++c) S[c][ti] = mfma16(k, Q[c][j], S[c][ti]);
+          for (int c = 0; c < C; ++c) S[c][ti] = mfma16(k, Q[c][j], j == 0 ? acc4{0.f, 0.f, 0.f, 0.f} : S[c][ti]);
         }
-      }
       __builtin_amdgcn_sched_barrier(0);
-      if (next >= 0) load(K, t_next, next, 0);
-      const int key0 = t * kTile + 16 * g;
-      if (t * kTile + kTile - 1 > see_first) {  // some column does not see the whole tile
+      if (next.page >= 0) load(K, next, 0);
+      const int key0 = now.t * kTile + 16 * g;
+      if (now.t * kTile + kTile - 1 > see_first) {  // some column does not see the whole tile
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -233,170 +369,332 @@ __global__ __launch_bounds__(kThreads, C == 4 ? 1 : 2) void cache_attn(AttnArgs 
       }
       __builtin_amdgcn_sched_barrier(0);
       bf16x8 P[C][2];
-      const float inv_v = pow2f(-ev);
+      softmax_step<C>(S, now.kc, now.ev, M, L, O, P);
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        float mx = S[c][0][0];
+      for (int st = 0; st < 2; ++st)
 #pragma unroll
-        for (int ti = 0; ti < 4; ++ti)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S[c][ti][i]);
-        mx = column(mx, [](float x, float y) { return fmaxf(x, y); }) * kc;
-        const float m = fmaxf(M[c], mx);
-        const float ms = m == -__builtin_inff() ? 0.f : m;  // no key yet
-        if (__ballot(m != M[c])) {
-          const float f = fast_exp2(M[c] - ms);
-          L[c] *= f;
-#pragma unroll
-          for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) O[c][dt][i] *= f;
-          M[c] = m;
-        }
-        // P is made as 2^ev p, what V's codes are to be multiplied by; its sum is taken back to p's
-        const float sub = ms - (float)ev;
-        float sum = 0.f;
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          float p[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            p[e] = fast_exp2(__builtin_fmaf(S[c][2 * st + e / 4][e & 3], kc, -sub));
-            sum += p[e];
-          }
-          const bf16x2 x = pack_bf16(p[0], p[1]), y = pack_bf16(p[2], p[3]), z = pack_bf16(p[4], p[5]), v = pack_bf16(p[6], p[7]);
-          P[c][st] = bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], v[0], v[1]};
-        }
-        L[c] = __builtin_fmaf(sum, inv_v, L[c]);
-      }
-#pragma unroll
-      for (int dt = 0; dt < 8; ++dt) {
-        keep_whole(V[dt]);
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
+        for (int dt = 0; dt < 8; ++dt) {
+          if (st == 0) keep_whole(V[dt]);
           const bf16x8 v = codes_to_bf16<FMT>(V[dt][2 * st], V[dt][2 * st + 1]);
 #pragma unroll
           for (int c = 0; c < C; ++c) O[c][dt] = mfma16(v, P[c][st], O[c][dt]);
         }
-      }
       __builtin_amdgcn_sched_barrier(0);
-      if (next >= 0) load(V, t_next, next, 1);
-      page = next;
-      t = t_next;
+      if (next.page >= 0) load(V, next, 1);
+      now = next;
     }
-    // join the waves: the common maximum, then outputs 2, 3 into 0, 1 and 1 into 0
-    float Lt[C];
+    // join the waves: each leaves its output in LDS and sums 8 / NW of the eight 16-element parts of all
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      Lt[c] = column(L[c], [](float x, float y) { return x + y; });
+      const float l = column(L[c], [](float x, float y) { return x + y; });
       if (g == 0) {
         xm[w][16 * c + col] = M[c];
-        xl[w][16 * c + col] = Lt[c];
+        xl[w][16 * c + col] = l;
+      }
+#pragma unroll
+      for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<acc4*>(xo[w][c][dt][lane]) = O[c][dt];
+    }
+    __syncthreads();
+    const bool whole = part == sw.grains;
+    float* slot = a.part + (int64_t)(2 * wg + (u0 == 0)) * (kRows * (kHeadDim + 2));
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int r = rt * kRows + 16 * c + col;
+      float m = -__builtin_inff(), l = 0.f, f[NW];
+#pragma unroll
+      for (int i = 0; i < NW; ++i) m = fmaxf(m, xm[i][16 * c + col]);
+      const float ms = m == -__builtin_inff() ? 0.f : m;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) {
+        f[i] = fast_exp2(xm[i][16 * c + col] - ms);
+        l += f[i] * xl[i][16 * c + col];
+      }
+      if (r >= rows) continue;
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const int i = r / a.G;
+      uint16_t* dst = a.o + (head * a.G + (r - i * a.G)) * a.os.head + (sw.r.row0 + i) * a.os.row + 4 * g;
+#pragma unroll
+      for (int x = 0; x < 8 / NW; ++x) {
+        const int dt = w * (8 / NW) + x;
+        acc4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int y = 0; y < NW; ++y) {
+          const acc4 z = *reinterpret_cast<const acc4*>(xo[y][c][dt][lane]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(f[y], z[e], o[e]);
+        }
+        if (whole) {
+          const bf16x2 p = pack_bf16(o[0] * inv, o[1] * inv), q = pack_bf16(o[2] * inv, o[3] * inv);
+          *reinterpret_cast<bf16x4*>(dst + 16 * dt) = bf16x4{p[0], p[1], q[0], q[1]};
+        } else {
+          *reinterpret_cast<acc4*>(slot + (16 * c + col) * kHeadDim + 16 * dt + 4 * g) = o;
+        }
+      }
+      if (!whole && w == 0 && g == 0) {
+        slot[kRows * kHeadDim + 16 * c + col] = m;
+        slot[kRows * kHeadDim + kRows + 16 * c + col] = l;
       }
     }
     __syncthreads();
+    pos += part;
+    if (pos >= stop && a.cut && tid == 0)
+      a.cut[wg] = cut_of(pl.share, base, unit, sw.grains, u0 + part, head, rt * kRows, min(rows - rt * kRows, kRows), sw.r.row0);
+  }
+}
+
+// Many rows a sequence: a unit is 128 rows, 32 a wave, and all four waves go over the same tiles, whose
+// codes come into LDS once a workgroup by direct loads, three tiles deep.  The waves' rows
+// are their own, so nothing is joined inside the workgroup.  Two workgroups share a CU: while a wave of one
+// forms probabilities, one of the other feeds the matrix unit.
+constexpr int kRowWaves = 4, kRowGroups = 2, kRowUnit = 16 * kRowGroups * kRowWaves;
+
+#if defined(__HIP_DEVICE_COMPILE__)
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+__device__ __forceinline__ u32x4 lds_chunk_at(int addr) { return *(const lds_u32x4*)(uint32_t)addr; }
+#endif
+
+template <int FMT>
+__global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int C = kRowGroups, NW = kRowWaves, kRows = kRowUnit, kStages = 3;
+  constexpr int kStage = 2 * kTileBytes;
+  __shared__ __attribute__((aligned(1024))) char ring[kStages * kStage];
+  __shared__ int64_t lds[NW + 2];
+  const int ring0 = __builtin_amdgcn_readfirstlane((int)(size_t)ring);
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 15, g = lane >> 4;
+  const int wgs = gridDim.x;
+  const int wg = (int)blockIdx.x % kNumXcd * (wgs / kNumXcd) + (int)blockIdx.x / kNumXcd;
+  Places<kRows, NW> pl;
+  pl.count(a, wgs, lds);
+  int64_t pos = wg * pl.share;
+  const int64_t stop = min(pos + pl.share, pl.total);
+  if (pos >= stop) {
+    if (a.cut && tid == 0) a.cut[wg].cuts = 0;
+    return;
+  }
+  int64_t base;
+  int s = pl.find(a, pos, lds, &base);
+  SeqWork<kRows> sw = pl.work(a, s);
+  while (pos < stop) {
+    while (pos >= base + sw.all(a)) {
+      base += sw.all(a);
+      sw = pl.work(a, ++s);
+    }
+    const int64_t off = pos - base;
+    const int unit = (int)div64(off, sw.grains), u0 = (int)(off - (int64_t)unit * sw.grains);
+    const int rt = unit % sw.nrt, head = unit / sw.nrt;
+    const int part = (int)min((int64_t)(sw.grains - u0), stop - pos);
+    const int t0 = u0 * a.grain, t1 = min((u0 + part) * a.grain, sw.T);  // the tiles of this piece
+    const int rows = sw.r.n * a.G;
+    const int held = min(sw.r.len + sw.r.n, a.b.max_pages * a.c.B);
+    const int r0 = rt * kRows + w * (16 * C);  // the wave's first row
+    const bool live = r0 < rows;
+    bf16x8 Q[C][4];
+    int see[C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      float m = -__builtin_inff();
+      const int r = r0 + 16 * c + col;
+      const int i = r / a.G;
+      see[c] = r < rows ? sw.r.len + i : -1;
+      const uint16_t* src = a.q + (head * a.G + (r - i * a.G)) * a.qs.head + (sw.r.row0 + i) * a.qs.row + 32 * g;
 #pragma unroll
-      for (int i = 0; i < kWaves; ++i) m = fmaxf(m, xm[i][16 * c + col]);
-      const float ms = m == -__builtin_inff() ? 0.f : m;
-      float l = 0.f;
-#pragma unroll
-      for (int i = 0; i < kWaves; ++i) l += xl[i][16 * c + col] * fast_exp2(xm[i][16 * c + col] - ms);
-      const float f = fast_exp2(M[c] - ms);
-#pragma unroll
-      for (int dt = 0; dt < 8; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) O[c][dt][i] *= f;
-      M[c] = m;
-      Lt[c] = l;
+      for (int j = 0; j < 4; ++j) {
+        Q[c][j] = bf16x8{};
+        if (r < rows) Q[c][j] = *reinterpret_cast<const bf16x8*>(src + 8 * j);
+      }
     }
+    const int see_first = sw.r.len + r0 / a.G;
+    const int see_last = sw.r.len + (min(rt * kRows + kRows, rows) - 1) / a.G;
+    acc4 O[C][8];
+    float M[C], L[C];
 #pragma unroll
-    for (int half = 2; half >= 1; half /= 2) {
-      if (w >= half && w < 2 * half)
+    for (int c = 0; c < C; ++c) {
+      M[c] = see[c] >= 0 ? -__builtin_inff() : 0.f;  // a column without a row asks for no reference
+      L[c] = 0.f;
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-          for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<acc4*>(xo[w - half][c][dt][lane]) = O[c][dt];
-      __syncthreads();
-      if (w < half)
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-          for (int dt = 0; dt < 8; ++dt) O[c][dt] += *reinterpret_cast<const acc4*>(xo[w][c][dt][lane]);
-      __syncthreads();
+      for (int dt = 0; dt < 8; ++dt) O[c][dt] = acc4{0.f, 0.f, 0.f, 0.f};
     }
-    if (w == 0) {
-      const bool whole = take == sw.T;
-      float* part = a.part + (int64_t)(2 * wg + (u0 == 0)) * (kRows * (kHeadDim + 2));
+    TileList<1> list(a, s, head, t0, min(t1, see_last / kTile + 1));
+    // a wave copies a quarter of the tile: its chunks 256 w ..
+    const auto fetch = [&](const TileInfo& tl, int stage) {
+      const uint8_t* src = list.at(a, tl, head);
+      const unsigned long long p = (unsigned long long)src;
+      const i32x4 rsrc = {__builtin_amdgcn_readfirstlane((int)(unsigned)p), __builtin_amdgcn_readfirstlane((int)(unsigned)(p >> 32)),
+                          kStage, 0x00020000};
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int r = rt * kRows + 16 * c + col;
-        if (r >= rows) continue;
-        if (whole) {
-          const float f = Lt[c] > 0.f ? 1.f / Lt[c] : 0.f;
-          const int i = r / a.G;
-          uint16_t* dst = a.o + (head * a.G + (r - i * a.G)) * a.os.head + (sw.r.row0 + i) * a.os.row + 4 * g;
+      for (int j = 0; j < kStage / (NW * kWave * kChunk); ++j)
+        dma16(rsrc, lane * kChunk, (w * 4 + j) * (kWave * kChunk), ring0 + stage * kStage + (w * 4 + j) * (kWave * kChunk));
+    };
+    TileInfo now = list.next(a, head), next{0, -1, 0, 0.f};
+    if (now.page >= 0) {
+      fetch(now, 0);
+      next = list.next(a, head);
+      if (next.page >= 0) fetch(next, 1);
+    }
+    int stage = 0;
+    while (now.page >= 0) {
+      if (next.page >= 0) wait_dma_but4();
+      else wait_dma();
+      __syncthreads();  // this tile is there for all waves, and all are done with the one before it
+      const TileInfo then = next.page >= 0 ? list.next(a, head) : TileInfo{0, -1, 0, 0.f};
+      if (then.page >= 0) fetch(then, stage == 0 ? 2 : stage - 1);
+      if (live && now.t * kTile <= see_last) {
+        const int kt = ring0 + stage * kStage + lane * kChunk, vt = kt + kTileBytes;
+        u32x4 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = lds_chunk_at(kt + i * (kWave * kChunk));
+        acc4 S[C][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)  // by steps of d, so that products into one accumulator are apart
+#pragma unroll
+          for (int ti = 0; ti < 4; ++ti) {
+            const u32x4 y = x[2 * ti + j / 2];
+            const bf16x8 k = codes_to_bf16<FMT>(y[2 * (j & 1)], y[2 * (j & 1) + 1]);
+#pragma unroll
+            for (int c = 0; c < C; ++c) S[c][ti] = mfma16(k, Q[c][j], j == 0 ? acc4{0.f, 0.f, 0.f, 0.f} : S[c][ti]);
+          }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = lds_chunk_at(vt + i * (kWave * kChunk));
+        const int key0 = now.t * kTile + 16 * g;
+        const bool edge = now.t * kTile + kTile - 1 > see_first;
+        if (edge) {
+#pragma unroll
+          for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int ti = 0; ti < 4; ++ti)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (key0 + 4 * ti + i > see[c]) S[c][ti][i] = -__builtin_inff();
+        }
+        bf16x8 P[C][2];
+        __builtin_amdgcn_s_setprio(1);
+        softmax_step<C>(S, now.kc, now.ev, M, L, O, P);
+        __builtin_amdgcn_s_setprio(0);
+        if (edge) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int bytes = min(max(held - key0 - 4 * e, 0), 4);
+            const uint32_t keep = bytes == 4 ? ~0u : (1u << (8 * bytes)) - 1u;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i][e] = without_nan<FMT>(x[i][e] & keep);
+          }
+        }
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
 #pragma unroll
           for (int dt = 0; dt < 8; ++dt) {
-            const bf16x2 x = pack_bf16(O[c][dt][0] * f, O[c][dt][1] * f), y = pack_bf16(O[c][dt][2] * f, O[c][dt][3] * f);
-            *reinterpret_cast<bf16x4*>(dst + 16 * dt) = bf16x4{x[0], x[1], y[0], y[1]};
-          }
-        } else {
-          float* dst = part + (16 * c + col) * kHeadDim + 4 * g;
+            const bf16x8 v = codes_to_bf16<FMT>(x[dt][2 * st], x[dt][2 * st + 1]);
 #pragma unroll
-          for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<acc4*>(dst + 16 * dt) = O[c][dt];
-          if (g == 0) {
-            part[kRows * kHeadDim + 16 * c + col] = M[c];
-            part[kRows * kHeadDim + kRows + 16 * c + col] = Lt[c];
+            for (int c = 0; c < C; ++c) O[c][dt] = mfma16(v, P[c][st], O[c][dt]);
           }
+      }
+      now = next;
+      next = then;
+      stage = stage == 2 ? 0 : stage + 1;
+    }
+    const bool whole = part == sw.grains;
+    float* slot = a.part + (int64_t)(2 * wg + (u0 == 0)) * (kRows * (kHeadDim + 2));
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const float l = column(L[c], [](float x, float y) { return x + y; });
+      const int r = r0 + 16 * c + col, x = r - rt * kRows;
+      if (r >= rows) continue;
+      if (whole) {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        const int i = r / a.G;
+        uint16_t* dst = a.o + (head * a.G + (r - i * a.G)) * a.os.head + (sw.r.row0 + i) * a.os.row + 4 * g;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+          const bf16x2 p = pack_bf16(O[c][dt][0] * inv, O[c][dt][1] * inv), q = pack_bf16(O[c][dt][2] * inv, O[c][dt][3] * inv);
+          *reinterpret_cast<bf16x4*>(dst + 16 * dt) = bf16x4{p[0], p[1], q[0], q[1]};
+        }
+      } else {
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<acc4*>(slot + x * kHeadDim + 16 * dt + 4 * g) = O[c][dt];
+        if (g == 0) {
+          slot[kRows * kHeadDim + x] = M[c];
+          slot[kRows * kHeadDim + kRows + x] = l;
         }
       }
     }
-    pos += take;
+    pos += part;
+    if (pos >= stop && a.cut && tid == 0) a.cut[wg] = cut_of(pl.share, base, unit, sw.grains, u0 + part, head, rt * kRows, min(rows - rt * kRows, kRows), sw.r.row0);
+    __syncthreads();  // all waves are done with the ring before the next unit fills it
   }
+#endif
 }
 
 // Joins the pieces of the units that share boundaries cut.  Workgroup b stands at the boundary between
 // shares b and b + 1; the boundaries inside one unit take its rows in turn.  A piece that begins
-// its unit lies in the second slot of its workgroup, any other in the first.
-template <int C>
-__global__ __launch_bounds__(kThreads) void cache_attn_join(AttnArgs a, int wgs) {
-  constexpr int kRows = 16 * C;
+// its unit lies in the second slot of its workgroup, any other in the first.  Pieces are added in
+// a fixed order.
+template <int kRows>
+__global__ __launch_bounds__(kJoinWaves* kWave) void cache_attn_join(AttnArgs a) {
   constexpr int64_t kSlot = kRows * (kHeadDim + 2);
-  __shared__ int64_t lds[kWaves + 2];
-  __shared__ float red[kWaves], acc[8][kHeadDim], sum[8];
+  constexpr int kGroups = kJoinWaves * 2;  // of 32 lanes, each lane four elements
+  __shared__ float red[kJoinWaves], acc[kGroups][kHeadDim], sum[kGroups];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  Place pl;
-  int64_t end, own;
-  count_tiles<C>(a, wgs, lds, &pl, &end, &own);
-  const int64_t pos = ((int64_t)blockIdx.x + 1) * pl.share;
-  if (pos >= pl.total) return;
-  find_tile<C>(a, pos, end, own, lds, &pl);
-  const SeqWork<C> sw(a, pl.seq);
-  const int64_t off = pos - pl.base;
-  const int64_t u0 = pl.base + off / sw.T * sw.T;  // the unit's first tile
-  if (u0 == pos) return;                            // not cut here
-  const int unit = (int)(off / sw.T), rt = unit % sw.nrt, head = unit / sw.nrt;
-  const int first = (int)(u0 / pl.share), last = (int)((u0 + sw.T - 1) / pl.share);
-  const int cuts = last - first, mine = (int)blockIdx.x - first;  // boundaries first .. last - 1 lie inside
-  const int rows = min(sw.r.n * a.G - rt * kRows, kRows);
+  const Cut k = a.cut[blockIdx.x];
+  if (k.cuts == 0) return;
+  const int first = k.first, cuts = k.cuts, mine = (int)blockIdx.x - first, rows = k.rows;
+  const int grp = tid >> 5, d = 4 * (tid & 31);
   const auto slot = [&](int p) { return a.part + (int64_t)(2 * (first + p) + (p == 0)) * kSlot; };
-  for (int r = mine; r < rows; r += cuts) {
+  const auto dst = [&](int r) {
+    const int i = (k.row + r) / a.G;
+    return a.o + (k.head * a.G + (k.row + r - i * a.G)) * a.os.head + (k.row0 + i) * a.os.row;
+  };
+  if (cuts < rows) {  // some rows a workgroup: one a group, whose lanes look up a piece each, then add all in turn
+    for (int r = mine + cuts * (grp + kGroups * (int)blockIdx.y); r < rows; r += cuts * kGroups * (int)gridDim.y) {
+      float m = -__builtin_inff();
+      for (int p = tid & 31; p <= cuts; p += 32) m = fmaxf(m, slot(p)[kRows * kHeadDim + r]);
+#pragma unroll
+      for (int o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor(m, o, 32));
+      const float ms = m == -__builtin_inff() ? 0.f : m;
+      float l = 0.f;
+      acc4 o = {0.f, 0.f, 0.f, 0.f};
+      for (int p0 = 0; p0 <= cuts; p0 += 32) {
+        const int p1 = p0 + (tid & 31);
+        float f = 0.f;
+        if (p1 <= cuts) {
+          const float* src = slot(p1) + kRows * kHeadDim + r;
+          f = fast_exp2(src[0] - ms);
+          l += f * src[kRows];
+        }
+        for (int i = 0; i < min(cuts + 1 - p0, 32); i += 4) {
+          acc4 x[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k)  // past the last: that one again, with the weight 0
+            x[k] = *reinterpret_cast<const acc4*>(slot(min(p0 + i + k, cuts)) + r * kHeadDim + d);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const float fi = __shfl(f, i + k, 32);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(fi, x[k][e], o[e]);
+          }
+        }
+      }
+#pragma unroll
+      for (int o2 = 16; o2; o2 /= 2) l += __shfl_xor(l, o2, 32);
+      const float f = l > 0.f ? 1.f / l : 0.f;
+      const bf16x2 x = pack_bf16(o[0] * f, o[1] * f), y = pack_bf16(o[2] * f, o[3] * f);
+      *reinterpret_cast<bf16x4*>(dst(r) + d) = bf16x4{x[0], x[1], y[0], y[1]};
+    }
+    return;
+  }
+  if (blockIdx.y > 0) return;
+  for (int r = mine; r < rows; r += cuts) {  // at most one: each group takes every eighth piece
     float m = -__builtin_inff();
-    for (int p = tid; p <= cuts; p += kThreads) m = fmaxf(m, slot(p)[kRows * kHeadDim + r]);
+    for (int p = tid; p <= cuts; p += kJoinWaves * kWave) m = fmaxf(m, slot(p)[kRows * kHeadDim + r]);
     m = wave_max(m);
     if (lane == 0) red[w] = m;
     __syncthreads();
     m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
     const float ms = m == -__builtin_inff() ? 0.f : m;
-    // eight groups of 32 lanes, each every eighth piece, four elements a lane
-    const int grp = tid >> 5, d = 4 * (tid & 31);
     float l = 0.f;
     acc4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int p = grp; p <= cuts; p += 8) {
+#pragma unroll 8
+    for (int p = grp; p <= cuts; p += kGroups) {
       const float* src = slot(p);
       const float f = fast_exp2(src[kRows * kHeadDim + r] - ms);
       l += f * src[kRows * kHeadDim + kRows + r];
@@ -410,50 +708,54 @@ __global__ __launch_bounds__(kThreads) void cache_attn_join(AttnArgs a, int wgs)
     if (tid < kHeadDim / 2) {
       float x = 0.f, y = 0.f, t = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < kGroups; ++i) {
         x += acc[i][2 * tid];
         y += acc[i][2 * tid + 1];
         t += sum[i];
       }
       const float f = t > 0.f ? 1.f / t : 0.f;
-      const int rr = rt * kRows + r, i = rr / a.G;
-      uint16_t* dst = a.o + (head * a.G + (rr - i * a.G)) * a.os.head + (sw.r.row0 + i) * a.os.row;
-      *reinterpret_cast<bf16x2*>(dst + 2 * tid) = pack_bf16(x * f, y * f);
+      *reinterpret_cast<bf16x2*>(dst(r) + 2 * tid) = pack_bf16(x * f, y * f);
     }
     __syncthreads();
   }
 }
 
-template <int FMT, int C>
-hipError_t launch(const AttnArgs& a, int wgs, hipStream_t stream) {
-  hipLaunchKernelGGL((cache_attn<FMT, C>), dim3(wgs), dim3(kThreads), 0, stream, a);
-  if (wgs > 1) hipLaunchKernelGGL((cache_attn_join<C>), dim3(wgs - 1), dim3(kThreads), 0, stream, a, wgs);
-  return hipGetLastError();
-}
-
 template <int FMT>
-hipError_t launch_groups(const AttnArgs& a, const CacheAttnPlan& p, hipStream_t stream) {
-  if (p.groups == 1) return launch<FMT, 1>(a, p.workgroups, stream);
-  return launch<FMT, 4>(a, p.workgroups, stream);
+hipError_t launch(const AttnArgs& a, const CacheAttnPlan& p, hipStream_t stream) {
+  const dim3 grid(p.workgroups), joins(p.workgroups - 1, p.rows == 16 ? 1 : 4), threads(kRowWaves * kWave);
+  if (p.rows == 16) hipLaunchKernelGGL((cache_attn<FMT, 4>), grid, dim3(4 * kWave), 0, stream, a);
+  else hipLaunchKernelGGL((cache_attn_rows<FMT>), grid, threads, 0, stream, a);
+  if (joins.x > 0 && a.cut) {
+    if (p.rows == 16) hipLaunchKernelGGL((cache_attn_join<16>), joins, dim3(kJoinWaves * kWave), 0, stream, a);
+    else hipLaunchKernelGGL((cache_attn_join<kRowUnit>), joins, dim3(kJoinWaves * kWave), 0, stream, a);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
 
 CacheAttnPlan cache_attn_plan(const CacheDims& c, const BatchDims& b, int hq) {
-  CacheAttnPlan p{1, 0, 0};
+  CacheAttnPlan p{16, kGrain, 0, 0, 0};
   if (b.n_seqs == 0 || b.n_rows == 0 || hq == 0) return p;
   const int64_t G = hq / c.hkv;
-  const int64_t rows = ((int64_t)b.n_rows + b.n_seqs - 1) / b.n_seqs * G;  // of an average sequence
-  p.groups = rows <= 16 ? 1 : 4;
-  // tiles that the table has room for, an upper bound of what the lengths say on the device
-  const int64_t nrt = (int64_t)b.n_rows * G / (16 * p.groups) + b.n_seqs;
-  const int64_t room = (int64_t)b.max_pages * c.tiles;
-  const double tiles = (double)nrt * c.hkv * (double)(room > 1 ? room : 1);
-  const int most = p.groups == 4 ? 256 : 512;
-  int64_t wgs = tiles >= (double)most * kMinShare ? most : ((int64_t)tiles + kMinShare - 1) / kMinShare;
+  // 16 rows a unit up to 48 rows a sequence on average, 128 above.  8 sequences of 4k to 8k tokens, e4m3, 16 /
+  // 128, us: 32 heads over 8, 33 rows 31.5 / 43.6 and 66 rows 66.5 / 49.3; 28 over 4, 49 rows 27.7 / 39.7, 115 rows
+  // 45.7 / 45.0 and 302 rows 72.0 / 69.3.
+  p.rows = (int64_t)b.n_rows * G <= 48 * (int64_t)b.n_seqs ? 16 : kRowUnit;
+  // units, and tiles of one, that the table has room for: upper bounds of what the lengths say on the device
+  const int64_t units = ((int64_t)b.n_rows * G / p.rows + b.n_seqs) * c.hkv;
+  const int64_t room = (int64_t)b.max_pages * c.tiles > 1 ? (int64_t)b.max_pages * c.tiles : 1;
+  // Short tables: units are not cut, which saves the second launch.  One row a sequence, 32 heads over 8, cut / not, us:
+  // 1 sequence of 1000 tokens (16 tiles) 9.5 / 8.8, of 2000 9.3 / 12.3; 16 of 1000 11.8 / 10.1, 64 of 1000 27.3 / 26.0.
+  const bool whole = room <= 16;
+  if (whole) p.grain = (int)room;
+  constexpr int kMost = 512;  // what the GPU holds at once: two a CU, of four waves with up to 256 registers
+  const double work = (double)units * (double)((room + p.grain - 1) / p.grain);
+  int64_t wgs = work < kMost || whole ? (int64_t)(work < 4096 ? work : 4096) : kMost;
   wgs = (wgs + kNumXcd - 1) / kNumXcd * kNumXcd;
   p.workgroups = (int)wgs;
-  p.bytes = (size_t)wgs * 2 * 16 * p.groups * (kHeadDim + 2) * sizeof(float);
+  p.cut_bytes = whole ? 0 : ((size_t)wgs * sizeof(Cut) + 255) / 256 * 256;
+  p.bytes = whole ? 256 : p.cut_bytes + (size_t)wgs * 2 * p.rows * (kHeadDim + 2) * sizeof(float);
   return p;
 }
 
@@ -461,8 +763,9 @@ hipError_t launch_cache_attn(const CacheDims& c, const BatchDims& b, const Seqs&
                              const uint16_t* q, Strides qs, const uint8_t* pages, const float* scales, uint16_t* o,
                              Strides os, void* ws, hipStream_t stream) {
   const CacheAttnPlan p = cache_attn_plan(c, b, hq);
-  const AttnArgs a{c, b, s, q, qs, pages, scales, o, os, hq / c.hkv, scale * kLog2e, (float*)ws};
-  return c.fmt == kCacheE4M3 ? launch_groups<kCacheE4M3>(a, p, stream) : launch_groups<kCacheInt8>(a, p, stream);
+  const AttnArgs a{c, b, s, q, qs, pages, scales, o, os, hq / c.hkv, p.grain, scale * kLog2e,
+                   p.cut_bytes ? (Cut*)ws : nullptr, (float*)((char*)ws + p.cut_bytes)};
+  return c.fmt == kCacheE4M3 ? launch<kCacheE4M3>(a, p, stream) : launch<kCacheInt8>(a, p, stream);
 }
 
 }  // namespace crisp

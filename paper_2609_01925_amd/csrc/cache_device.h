@@ -101,16 +101,38 @@ __device__ __forceinline__ SeqRows seq_rows(const Seqs& s, const BatchDims& b, i
   return r;
 }
 
-// Inclusive sum over the workgroup's 64-lane waves in thread order; lds: one value a wave.  Every
-// thread also gets the whole sum.  Ends with the waves' values still in lds: a barrier before the next use.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t shifted(uint32_t x) {  // lanes that the move does not reach get 0
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, true);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int shifted(int x) {
+  return (int)shifted<CTRL, ROWS>((uint32_t)x);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t shifted(int64_t x) {
+  return (int64_t)((uint64_t)shifted<CTRL, ROWS>((uint32_t)((uint64_t)x >> 32)) << 32 | shifted<CTRL, ROWS>((uint32_t)x));
+}
+
+// Inclusive sum over the wave in lane order, by register moves: within rows of 16 lanes, then
+// the last lane of a row into the next.
+template <typename T>
+__device__ __forceinline__ T wave_scan(T x) {
+  x += shifted<0x111, 0xf>(x);
+  x += shifted<0x112, 0xf>(x);
+  x += shifted<0x114, 0xf>(x);
+  x += shifted<0x118, 0xf>(x);
+  x += shifted<0x142, 0xa>(x);
+  x += shifted<0x143, 0xc>(x);
+  return x;
+}
+
+// Inclusive sum over the workgroup in thread order; lds: one value a wave.  Every thread also
+// gets the whole sum.  Ends with the waves' values still in lds: a barrier before the next use.
 template <typename T, int kWaves>
 __device__ __forceinline__ T block_scan(T x, T* lds, T* total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const T y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
-  }
+  x = wave_scan(x);
   if (lane == 63) lds[w] = x;
   __syncthreads();
   T before = 0, all = 0;
@@ -123,5 +145,10 @@ __device__ __forceinline__ T block_scan(T x, T* lds, T* total) {
   *total = all;
   return x + before;
 }
+
+#if defined(__HIP_DEVICE_COMPILE__)
+// Waits until at most the last four vector memory operations of this wave are under way (vmcnt(4)).
+__device__ __forceinline__ void wait_dma_but4() { __builtin_amdgcn_s_waitcnt(4 | (7 << 4) | (15 << 8)); }
+#endif
 
 }  // namespace crisp

@@ -42,11 +42,11 @@ hipError_t launch_cache_append(const CacheDims& c, const BatchDims& b, const Seq
 hipError_t launch_cache_copy(const CacheDims& c, const int32_t* pairs, int n_pairs, const int32_t* count,
                              uint8_t* pages, float* scales, hipStream_t stream);
 
-// What the attention's launch is cut into: row groups of 16 query rows that a wave holds at once,
-// and workgroups, each with an equal share of the 64-token tiles.
+// What the attention's launch is cut into: units of so many query rows of one sequence and KV head, and workgroups
+// with an equal share of the units' 64-token tiles each.
 struct CacheAttnPlan {
-  int groups, workgroups;
-  size_t bytes;  // workspace: two partial results a workgroup
+  int rows, grain, workgroups;  // grain: tiles that are never cut apart
+  size_t cut_bytes, bytes;      // workspace: what each boundary between shares cuts (0: nothing is cut), and all of it
 };
 CacheAttnPlan cache_attn_plan(const CacheDims& c, const BatchDims& b, int hq);
 

@@ -18,6 +18,7 @@ constexpr int kThreads = 1024;
 constexpr int kWavesPool = kThreads / kWave;
 constexpr int kBuf = 4096;  // free pages collected at a time
 constexpr int kPerThread = kPoolMaxSeqs / kThreads;
+static_assert(kPoolMaxSeqs <= kBuf, "a fork collects its pages at once");
 
 __device__ __forceinline__ uint32_t* bits_of(int32_t* pool, int n_pages) { return reinterpret_cast<uint32_t*>(pool + n_pages); }
 __device__ __forceinline__ uint32_t load_word(const uint32_t* p) {  // past L1: other threads set bits atomically
@@ -34,20 +35,10 @@ struct PoolLds {
   int buf[kBuf];
 };
 
-// Pages not in use, counted by the workgroup.
-__device__ __forceinline__ int count_free(const uint32_t* bits, int n_pages, int* wsum) {
-  const int words = (n_pages + 31) / 32;
-  int n = 0;
-  for (int i = threadIdx.x; i < words; i += kThreads) n += __popc(~load_word(bits + i) & word_mask(i, n_pages));
-  int total;
-  __syncthreads();
-  block_scan<int, kWavesPool>(n, wsum, &total);
-  return total;
-}
-
-// Pages not in use, lowest first, into buf until `want` (<= kBuf, and no more than there are)
-// are found; *word is where to begin, in words, and where to go on.
-__device__ __forceinline__ void collect_free(const uint32_t* bits, int n_pages, int want, int* word, PoolLds& l) {
+// Pages not in use, lowest first, into buf from word *word on until `want` (<= kBuf) are found; returns
+// the number found (it may pass `want`, of which no more than kBuf are in buf).  *word is then where
+// to look on: the words before it hold none but those in buf.
+__device__ __forceinline__ int collect_free(const uint32_t* bits, int n_pages, int want, int* word, PoolLds& l) {
   const int words = (n_pages + 31) / 32;
   int found = 0;
   while (found < want && *word < words) {
@@ -59,9 +50,22 @@ __device__ __forceinline__ void collect_free(const uint32_t* bits, int n_pages, 
     int at = found + block_scan<int, kWavesPool>(cnt, l.wsum, &total) - cnt;
     for (; f && at < want; f &= f - 1, ++at) l.buf[at] = 32 * i + __builtin_ctz(f);
     found += total;
-    if (found < want) *word += kThreads;
+    if (found <= want) *word += kThreads;
   }
   __syncthreads();
+  return found;
+}
+
+// Pages not in use among the words from `word` on, counted by the workgroup.
+__device__ __forceinline__ int count_free(const uint32_t* bits, int n_pages, int word, int* wsum) {
+  const int words = (n_pages + 31) / 32;
+  int n = 0;
+#pragma unroll 4
+  for (int i = word + (int)threadIdx.x; i < words; i += kThreads) n += __popc(~load_word(bits + i) & word_mask(i, n_pages));
+  int total;
+  __syncthreads();
+  block_scan<int, kWavesPool>(n, wsum, &total);
+  return total;
 }
 
 __device__ __forceinline__ void take_page(int32_t* pool, uint32_t* bits, int page) {
@@ -77,69 +81,99 @@ __global__ __launch_bounds__(256) void pool_init(int32_t* pool, int64_t words) {
 // Sequence s asks for room for counts[s] tokens behind its seq_len[s]: the slots len / B ..
 // ceil((len + count) / B) - 1 that hold no page.  Asked for in order of sequence and slot; a
 // sequence whose running sum (its own included) passes the free pages, or whose slots pass the
-// table, gets none.
+// table, gets none.  The slots of all sequences in a row are looked at kEach a thread; where one
+// round covers them all, what was read serves for the assignment too.
 __global__ __launch_bounds__(kThreads) void pool_reserve(int n_pages, int B, int n_seqs, int max_pages, int32_t* pool,
                                                          int32_t* table, const int32_t* seq_len, const int32_t* counts,
                                                          int32_t* granted) {
+  constexpr int kEach = 4, kRound = kEach * kThreads;
   __shared__ PoolLds l;
-  __shared__ int first[kPoolMaxSeqs + 1], miss[kPoolMaxSeqs];
+  // place of a sequence's first slot among all, what leads from a place to its table entry, and
+  // its missing pages (then: whether it is served)
+  __shared__ int first[kPoolMaxSeqs + 1], entry[kPoolMaxSeqs], miss[kPoolMaxSeqs];
   uint32_t* bits = bits_of(pool, n_pages);
   const int tid = threadIdx.x;
   const int per = (n_seqs + kThreads - 1) / kThreads;
-  const auto len_of = [&](int s) { return (int)min((int64_t)max(seq_len[s], 0), (int64_t)max_pages * B); };
   bool fits[kPerThread];
-  int ask[kPerThread];
-  int own = 0, range[kPerThread];
-  for (int i = 0; i < per; ++i) {
+  int ask[kPerThread], range[kPerThread], from[kPerThread], own = 0;
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i) {
     const int s = tid * per + i;
-    range[i] = 0, fits[i] = false, ask[i] = 0;
-    if (s < n_seqs) {
-      const int len = len_of(s);
+    range[i] = 0, fits[i] = false, ask[i] = 0, from[i] = 0;
+    if (i < per && s < n_seqs) {
+      const int len = (int)min((int64_t)max(seq_len[s], 0), (int64_t)max_pages * B);
       ask[i] = max(counts[s], 0);
       const int64_t last = ((int64_t)len + ask[i] + B - 1) / B;
       fits[i] = ask[i] > 0 && last <= max_pages;
-      if (fits[i]) range[i] = (int)last - len / B;
+      from[i] = len / B;
+      if (fits[i]) range[i] = (int)last - from[i];
     }
     own += range[i];
   }
   int total;
   int at = block_scan<int, kWavesPool>(own, l.wsum, &total) - own;
-  for (int i = 0; i < per; ++i) {
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i) {
     const int s = tid * per + i;
-    if (s < n_seqs) {
+    if (i < per && s < n_seqs) {
       first[s] = at;
+      entry[s] = s * max_pages + from[i] - at;  // fits: the table has less than 2^31 entries
       miss[s] = 0;
       at += range[i];
     }
   }
   if (tid == 0) first[n_seqs] = total;
-  const int n_free = count_free(bits, n_pages, l.wsum);  // its barriers also publish first and miss
-  // the pair (sequence, slot) at place p of all ranges in a row
-  const auto pair_of = [&](int p, int* s) {
-    int lo = 0, hi = n_seqs;  // first[lo] <= p < first[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (first[mid] <= p) lo = mid;
-      else hi = mid;
-    }
-    *s = lo;
-    return (int64_t)lo * max_pages + len_of(lo) / B + (p - first[lo]);
+  // the lowest free pages, and how many there are
+  int word = 0;
+  int n_free = collect_free(bits, n_pages, kBuf, &word, l);  // its barriers also publish first, entry and miss
+  if (n_free > kBuf) {  // those of the words up to the last one looked at are in n_free
+    n_free += count_free(bits, n_pages, word + kThreads, l.wsum);
+  } else if (n_free == kBuf) {
+    n_free += count_free(bits, n_pages, word, l.wsum);
+  }
+  struct Slots {
+    int s[kEach], e[kEach];
+    bool lack[kEach];
   };
-  for (int p = tid; p < total; p += kThreads) {
-    int s;
-    const int64_t e = pair_of(p, &s);
-    if (table[e] < 0) atomicAdd(&miss[s], 1);
+  const auto read = [&](int p0, Slots& x) {
+    const int p = p0 + kEach * tid;
+    int lo = 0, hi = n_seqs;  // first[lo] <= p < first[hi]
+    if (p < total)
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (first[mid] <= p) lo = mid;
+        else hi = mid;
+      }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      x.lack[k] = false;
+      if (p + k < total) {
+        while (first[lo + 1] <= p + k) ++lo;  // ends: first[n_seqs] = total
+        x.s[k] = lo;
+        x.e[k] = entry[lo] + p + k;
+        x.lack[k] = table[x.e[k]] < 0;
+      }
+    }
+  };
+  Slots x;
+  for (int p0 = 0; p0 < total; p0 += kRound) {
+    read(p0, x);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+      if (x.lack[k]) atomicAdd(&miss[x.s[k]], 1);
   }
   __syncthreads();
   own = 0;
-  for (int i = 0; i < per; ++i)
-    if (tid * per + i < n_seqs) own += miss[tid * per + i];
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i)
+    if (i < per && tid * per + i < n_seqs) own += miss[tid * per + i];
   int all;
   int sum = block_scan<int, kWavesPool>(own, l.wsum, &all) - own;
   int taken = 0;
-  for (int i = 0; i < per; ++i) {
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i) {
     const int s = tid * per + i;
-    if (s >= n_seqs) break;
+    if (i >= per || s >= n_seqs) break;
     const int m = miss[s];
     sum += m;
     const bool ok = fits[i] && (m == 0 || sum <= n_free);
@@ -150,26 +184,33 @@ __global__ __launch_bounds__(kThreads) void pool_reserve(int n_pages, int B, int
   __syncthreads();
   int want;
   block_scan<int, kWavesPool>(taken, l.wsum, &want);
-  int word = 0;
   for (int done = 0; done < want; done += kBuf) {
     const int now = min(want - done, kBuf);
-    collect_free(bits, n_pages, now, &word, l);
+    if (done > 0) {
+      word = 0;
+      collect_free(bits, n_pages, now, &word, l);
+    }
     int rank = 0;
-    for (int p0 = 0; p0 < total && rank < now; p0 += kThreads) {
-      const int p = p0 + tid;
-      int s = 0, flag = 0;
-      int64_t e = 0;
-      if (p < total) {
-        e = pair_of(p, &s);
-        flag = miss[s] && table[e] < 0;
+    for (int p0 = 0; p0 < total && rank < now; p0 += kRound) {
+      if (total > kRound) read(p0, x);  // otherwise x is still that of the only round
+      int mine = 0;
+#pragma unroll
+      for (int k = 0; k < kEach; ++k) {
+        x.lack[k] = x.lack[k] && miss[x.s[k]] && (done == 0 || table[x.e[k]] < 0);
+        mine += x.lack[k];
       }
       int here;
       __syncthreads();
-      const int k = rank + block_scan<int, kWavesPool>(flag, l.wsum, &here) - flag;
-      if (flag && k < now) {
-        table[e] = l.buf[k];
-        take_page(pool, bits, l.buf[k]);
-      }
+      int k0 = rank + block_scan<int, kWavesPool>(mine, l.wsum, &here) - mine;
+#pragma unroll
+      for (int k = 0; k < kEach; ++k)
+        if (x.lack[k]) {
+          if (k0 < now) {
+            table[x.e[k]] = l.buf[k0];
+            take_page(pool, bits, l.buf[k0]);
+          }
+          ++k0;
+        }
       rank += here;
     }
     __threadfence();  // the next round looks for free pages in what this one has set
@@ -198,7 +239,7 @@ __global__ __launch_bounds__(kThreads) void pool_fork(int n_pages, int B, int n_
       len = (int)min((int64_t)max(seq_len[s], 0), (int64_t)max_pages * B);
     lens[i] = len;
   }
-  const int n_free = count_free(bits, n_pages, l.wsum);
+  __syncthreads();
   for (int i = tid; i < n; i += kThreads)
     if (lens[i] >= 0) atomicMin(&owner[dst[i]], i);
   __syncthreads();
@@ -217,7 +258,7 @@ __global__ __launch_bounds__(kThreads) void pool_fork(int n_pages, int B, int n_
   int need;
   int rank = block_scan<int, kWavesPool>(own, l.wsum, &need) - own;
   int word = 0;
-  collect_free(bits, n_pages, min(need, n_free), &word, l);
+  const int n_free = collect_free(bits, n_pages, need, &word, l);  // need <= kPoolMaxSeqs <= kBuf
   for (int k = 0; k < per; ++k) {
     const int i = tid * per + k;
     if (i >= n) break;
@@ -287,7 +328,7 @@ __global__ __launch_bounds__(kThreads) void pool_compact(int n_pages, int32_t* p
   uint32_t* bits = bits_of(pool, n_pages);
   const int tid = threadIdx.x;
   const int words = (n_pages + 31) / 32;
-  const int used = n_pages - count_free(bits, n_pages, wsum);
+  const int used = n_pages - count_free(bits, n_pages, 0, wsum);
   int holes = 0, movers = 0;
   for (int w0 = 0; w0 < words; w0 += kThreads) {
     const int i = w0 + tid;
