@@ -371,8 +371,10 @@ crisp_status crisp_pool_init(int32_t n_pages, int32_t* pool, crisp_stream stream
 
 /* Room for counts[s] more tokens behind seq_len[s]: the slots seq_len / block .. ceil((seq_len + count) /
  * block) - 1 of row s that have no page (a negative entry) get one.  granted[s] = counts[s], or 0 where the
- * row is too short or the free pages do not cover what the sequences up to and with s ask for: such a
- * sequence gets none.  seq_len stays as it is. */
+ * row is too short, the free pages do not cover what the sequences up to and with s ask for, or one of
+ * those slots has a page that is used more than once (after seq_len was taken back into pages that a
+ * fork shares; a fork of the sequence as it then is has a page of its own there): such a sequence gets
+ * none.  seq_len stays as it is. */
 crisp_status crisp_pool_reserve(int32_t n_pages, int32_t block, int32_t n_seqs, int32_t max_pages, int32_t* pool,
                                 int32_t* table, const int32_t* seq_len, const int32_t* counts, int32_t* granted,
                                 crisp_stream stream);

@@ -3,4 +3,4 @@
 The compute path is libcrisp.so (HIP kernels behind the C ABI of
 include/crisp.h); `paper_2609_01925_amd.crisp` is its Python binding.
 """
-__all__ = ["crisp"]
+__all__ = ["crisp", "cache"]

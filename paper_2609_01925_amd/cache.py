@@ -1,0 +1,87 @@
+"""K and V of a model's layers between a prompt's prefill and the tokens that follow it: the 8-bit paged
+cache of every layer, one table and one pool of pages for all of them.
+
+    kv = KVCache(n_layers, n_pages, n_kv_heads, max_seqs, max_tokens)
+    granted = kv.reserve(counts)              # pages for the next rows, all layers
+    o = kv.prefill(layer, seq, q, k, v)       # a prompt: sparse prefill, then K and V into the cache
+    o = kv.attend(layer, row_ptr, q, k, v)    # a step: the rows' K and V in, then attention over all
+    kv.advance(counts)                        # once all layers have run
+
+Everything stays on the GPU and is only enqueued, on the current stream; nothing waits for the device.
+"""
+from __future__ import annotations
+
+from typing import Optional
+
+import torch
+
+from . import crisp as C
+
+
+class KVCache:
+    """table int32 [max_seqs, pages of max_tokens], seq_len int32 [max_seqs] (tokens that all layers hold),
+    pool (C.crisp_pool_init) and layers (a C.Cache each)."""
+
+    def __init__(self, n_layers: int, n_pages: int, n_kv_heads: int, max_seqs: int, max_tokens: int, block: int = 64,
+                 fmt: int = C.CACHE_E4M3, device="cuda"):
+        if n_layers < 1 or max_seqs < 1 or max_tokens < 1:
+            raise ValueError(f"n_layers {n_layers}, max_seqs {max_seqs} and max_tokens {max_tokens} must be positive")
+        self.layers = [C.make_cache(n_pages, n_kv_heads, block, fmt, device) for _ in range(n_layers)]
+        self.block = block
+        self.pool = C.crisp_pool_init(n_pages, device)
+        dev = self.pool.device
+        self.table = torch.full((max_seqs, -(-max_tokens // block)), -1, dtype=torch.int32, device=dev)
+        self.seq_len = torch.zeros(max_seqs, dtype=torch.int32, device=dev)
+        self._row = torch.arange(max_seqs + 1, dtype=torch.int32, device=dev)
+
+    def reserve(self, counts: torch.Tensor) -> torch.Tensor:
+        """Pages for counts[s] (int32 [max_seqs]) more tokens of each sequence -> granted: counts[s], or 0 where the
+        free pages or the table do not suffice, or the rows would go into a page that a fork shares."""
+        return C.crisp_pool_reserve(self.pool, self.block, self.table, self.seq_len, counts)
+
+    def prefill(self, layer: int, seq: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                params: Optional[C.CrispParams] = None) -> torch.Tensor:
+        """One layer of a prompt, sequence `seq` holding nothing yet and its pages reserved: sparse prefill
+        attention over q [H_q, n, 128], k and v [H_kv, n, 128] as they are, then k and v into the cache -> o."""
+        if not 0 <= seq < self.table.shape[0]:
+            raise ValueError(f"sequence {seq} outside [0, {self.table.shape[0]})")
+        o = C.crisp_prefill_attn(q, k, v, C.make_params() if params is None else params)
+        C.crisp_cache_append(self.layers[layer], self.table, self.seq_len, self.rows_of(seq, k.shape[1]), k, v)
+        return o
+
+    def rows_of(self, seq: int, n: int) -> torch.Tensor:
+        """row_ptr of a call whose n rows are all sequence seq's."""
+        return (self._row > seq).to(torch.int32) * n
+
+    def attend(self, layer: int, row_ptr: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+               softmax_scale: float = 0.0, ws: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """One layer of a step: rows row_ptr[s] .. row_ptr[s + 1] of k and v behind sequence s's tokens, then q's
+        rows over all of them -> o."""
+        cache = self.layers[layer]
+        C.crisp_cache_append(cache, self.table, self.seq_len, row_ptr, k, v)
+        return C.crisp_cache_attn(cache, self.table, self.seq_len, row_ptr, q, softmax_scale, ws, out)
+
+    def advance(self, counts: torch.Tensor) -> None:
+        """The rows of a step count as held from here on (int32 [max_seqs]; negative to take tokens back:
+        reserve() before the next rows then sees to it that none go into a page that a fork shares)."""
+        self.seq_len += counts
+
+    def fork(self, src: torch.Tensor, dst: torch.Tensor) -> torch.Tensor:
+        """Empty sequences dst[i] become copies of src[i], sharing full pages -> copies int32 [n, 2], (-2, -2) where
+        a fork was refused."""
+        copies = C.crisp_pool_fork(self.pool, self.block, self.table, self.seq_len, src, dst)
+        for cache in self.layers:
+            C.crisp_cache_copy(cache, copies)
+        return copies
+
+    def free(self, ids: torch.Tensor) -> None:
+        """Sequences ids[i] end."""
+        C.crisp_pool_free(self.pool, self.table, self.seq_len, ids)
+
+    def compact(self) -> torch.Tensor:
+        """All pages in use gathered at the front of every layer's cache -> the number of pages moved, int32 [1]."""
+        moves, count = C.crisp_pool_compact(self.pool, self.table)
+        for cache in self.layers:
+            C.crisp_cache_copy(cache, moves, count)
+        return count

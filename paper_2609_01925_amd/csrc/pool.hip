@@ -80,16 +80,18 @@ __global__ __launch_bounds__(256) void pool_init(int32_t* pool, int64_t words) {
 
 // Sequence s asks for room for counts[s] tokens behind its seq_len[s]: the slots len / B ..
 // ceil((len + count) / B) - 1 that hold no page.  Asked for in order of sequence and slot; a
-// sequence whose running sum (its own included) passes the free pages, or whose slots pass the
-// table, gets none.  The slots of all sequences in a row are looked at kEach a thread; where one
+// sequence whose running sum (its own included) passes the free pages, whose slots pass the
+// table, or one of whose slots has a page that is used more than once (tokens were taken back into
+// what a fork shares: rows written there would change the other's) gets none.  The slots of all sequences in a row are looked at kEach a thread; where one
 // round covers them all, what was read serves for the assignment too.
 __global__ __launch_bounds__(kThreads) void pool_reserve(int n_pages, int B, int n_seqs, int max_pages, int32_t* pool,
                                                          int32_t* table, const int32_t* seq_len, const int32_t* counts,
                                                          int32_t* granted) {
   constexpr int kEach = 4, kRound = kEach * kThreads;
   __shared__ PoolLds l;
+  constexpr int kShared = 1 << 30;
   // place of a sequence's first slot among all, what leads from a place to its table entry, and
-  // its missing pages (then: whether it is served)
+  // its missing pages and kShared if one is shared (then: whether it is served)
   __shared__ int first[kPoolMaxSeqs + 1], entry[kPoolMaxSeqs], miss[kPoolMaxSeqs];
   uint32_t* bits = bits_of(pool, n_pages);
   const int tid = threadIdx.x;
@@ -132,7 +134,7 @@ __global__ __launch_bounds__(kThreads) void pool_reserve(int n_pages, int B, int
     n_free += count_free(bits, n_pages, word, l.wsum);
   }
   struct Slots {
-    int s[kEach], e[kEach];
+    int s[kEach], e[kEach], page[kEach];
     bool lack[kEach];
   };
   const auto read = [&](int p0, Slots& x) {
@@ -147,11 +149,13 @@ __global__ __launch_bounds__(kThreads) void pool_reserve(int n_pages, int B, int
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
       x.lack[k] = false;
+      x.page[k] = -1;
       if (p + k < total) {
         while (first[lo + 1] <= p + k) ++lo;  // ends: first[n_seqs] = total
         x.s[k] = lo;
         x.e[k] = entry[lo] + p + k;
-        x.lack[k] = table[x.e[k]] < 0;
+        x.page[k] = table[x.e[k]];
+        x.lack[k] = x.page[k] < 0;
       }
     }
   };
@@ -159,14 +163,24 @@ __global__ __launch_bounds__(kThreads) void pool_reserve(int n_pages, int B, int
   for (int p0 = 0; p0 < total; p0 += kRound) {
     read(p0, x);
 #pragma unroll
-    for (int k = 0; k < kEach; ++k)
+    for (int k = 0; k < kEach; ++k) {
       if (x.lack[k]) atomicAdd(&miss[x.s[k]], 1);
+      else if (x.page[k] >= 0 && x.page[k] < n_pages && pool[x.page[k]] > 1) atomicOr(&miss[x.s[k]], kShared);
+    }
   }
   __syncthreads();
   own = 0;
 #pragma unroll
   for (int i = 0; i < kPerThread; ++i)
-    if (i < per && tid * per + i < n_seqs) own += miss[tid * per + i];
+    if (i < per && tid * per + i < n_seqs) {
+      const int m = miss[tid * per + i];
+      if (m & kShared) {
+        fits[i] = false;
+        miss[tid * per + i] = 0;
+      } else {
+        own += m;
+      }
+    }
   int all;
   int sum = block_scan<int, kWavesPool>(own, l.wsum, &all) - own;
   int taken = 0;

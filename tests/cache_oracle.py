@@ -177,6 +177,9 @@ class Pool:
             if c <= 0 or last > len(row):
                 granted.append(0)
                 continue
+            if any(0 <= row[j] < len(self.uses) and self.uses[row[j]] > 1 for j in range(n // self.block, last)):
+                granted.append(0)
+                continue
             lack = [j for j in range(n // self.block, last) if row[j] < 0]
             asked += len(lack)
             if lack and asked > len(free):

@@ -463,12 +463,33 @@ def test_pool_operations_in_random_order(n_pages):
             C.crisp_pool_free(pool, table, seq_len, _ints(ids))
             oracle.free(ids.tolist())
         _same_pool(pool, table, seq_len, oracle, f"step {step} op {what}")
+        if step % 7 == 3:  # tokens taken back, perhaps into pages that a fork shares
+            back = rng.integers(0, 100, n_seqs) * (rng.random(n_seqs) < 0.3)
+            seq_len -= torch.minimum(_ints(back), seq_len)
+            oracle.seq_len = [max(0, a - int(b)) for a, b in zip(oracle.seq_len, back)]
         if step % 5 == 4:
             moves, count = C.crisp_pool_compact(pool, table)
             want = oracle.compact()
             assert count.item() == len(want) and moves[: len(want)].tolist() == [list(x) for x in want]
             assert (moves[len(want):] == -1).all()
             _same_pool(pool, table, seq_len, oracle, f"step {step} compact")
+
+
+def test_shared_page_is_not_reserved_again():
+    """A sequence whose tokens are taken back into a page that its fork shares gets no rows there; a fork of it does."""
+    C = _crisp()
+    _say("shared page")
+    pool, table, seq_len, oracle = _pool_state(C, 10, 64, 4, 4)
+    counts = [128, 0, 0, 0]
+    assert C.crisp_pool_reserve(pool, 64, table, seq_len, _ints(counts)).tolist() == oracle.reserve(counts) == counts
+    seq_len[0] = oracle.seq_len[0] = 128
+    assert C.crisp_pool_fork(pool, 64, table, seq_len, _ints([0]), _ints([1])).tolist() == [[-1, -1]]
+    oracle.fork([0], [1])
+    seq_len[0] = oracle.seq_len[0] = 125
+    assert C.crisp_pool_reserve(pool, 64, table, seq_len, _ints([1, 1, 0, 0])).tolist() == oracle.reserve([1, 1, 0, 0]) == [0, 1, 0, 0]
+    assert C.crisp_pool_fork(pool, 64, table, seq_len, _ints([0]), _ints([2])).tolist() == [list(x) for x in oracle.fork([0], [2])]
+    assert C.crisp_pool_reserve(pool, 64, table, seq_len, _ints([0, 0, 3, 0])).tolist() == oracle.reserve([0, 0, 3, 0]) == [0, 0, 3, 0]
+    _same_pool(pool, table, seq_len, oracle, "shared")
 
 
 def test_pool_large_reservation_and_many_sequences():
