@@ -11,8 +11,8 @@ namespace crisp {
 
 namespace {
 
-constexpr int kJoinWaves = 4;
-// Tiles that are not cut apart: one a wave.  Sequences of 2000 tokens, 32 heads over 8, grains of 4 / 8 / 16, us: one
+constexpr int kFewWaves = 4, kJoinWaves = 4;
+// Tiles that are not cut apart: one a wave of cache_attn.  Sequences of 2000 tokens, 32 heads over 8, grains of 4 / 8 / 16, us: one
 // sequence 9.3 / 10.3 / 12.0, 4 10.8 / 10.3 / 12.0, 16 20.6 / 17.6 / 19.7, 64 40.5 / 42.5 / 36.2; one of 6000 9.9 / 10.5 / 11.7.
 constexpr int kGrain = 4;
 
@@ -259,9 +259,9 @@ __device__ __forceinline__ void softmax_step(const acc4 (&S)[C][4], float kc, in
 // maximum, sum and output, joined through LDS at the unit's end.  A lane's 16-byte loads are
 // matrix operands as they stand (cache_device.h): K of the next tile is loaded while the softmax
 // and PV of this one run, V while the next scores are made, nothing passes through LDS.
-template <int FMT, int NW>
-__global__ __launch_bounds__(NW * kWave, 2) void cache_attn(AttnArgs a) {
-  constexpr int C = 1, kRows = 16 * C;
+template <int FMT, bool ONCE>
+__global__ __launch_bounds__(kFewWaves* kWave, 2) void cache_attn(AttnArgs a) {
+  constexpr int NW = kFewWaves, C = 1, kRows = 16 * C;
   __shared__ __attribute__((aligned(16))) float xo[NW][C][8][kWave][4];
   __shared__ float xm[NW][kRows], xl[NW][kRows];
   __shared__ int64_t lds[NW + 2];
@@ -324,7 +324,10 @@ __global__ __launch_bounds__(NW * kWave, 2) void cache_attn(AttnArgs a) {
     const auto load = [&](u32x4* x, const TileInfo& tl, int tensor) {
       const uint8_t* src = list.at(a, tl, head) + tensor * kTileBytes + lane * kChunk;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = *reinterpret_cast<const u32x4*>(src + i * (kWave * kChunk));
+      for (int i = 0; i < 8; ++i) {
+        const u32x4* at = reinterpret_cast<const u32x4*>(src + i * (kWave * kChunk));
+        x[i] = ONCE ? __builtin_nontemporal_load(at) : *at;
+      }
     };
     u32x4 K[8], V[8];
     TileInfo now = list.next(a, head);
@@ -722,9 +725,10 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void cache_attn_join(AttnArgs a)
 
 template <int FMT>
 hipError_t launch(const AttnArgs& a, const CacheAttnPlan& p, hipStream_t stream) {
-  const dim3 grid(p.workgroups), joins(p.workgroups - 1, p.rows == 16 ? 1 : 4), threads(kRowWaves * kWave);
-  if (p.rows == 16) hipLaunchKernelGGL((cache_attn<FMT, 4>), grid, dim3(4 * kWave), 0, stream, a);
-  else hipLaunchKernelGGL((cache_attn_rows<FMT>), grid, threads, 0, stream, a);
+  const dim3 grid(p.workgroups), joins(p.workgroups - 1, p.rows == 16 ? 1 : 4);
+  if (p.rows == kRowUnit) hipLaunchKernelGGL((cache_attn_rows<FMT>), grid, dim3(kRowWaves * kWave), 0, stream, a);
+  else if (p.once) hipLaunchKernelGGL((cache_attn<FMT, true>), grid, dim3(kFewWaves * kWave), 0, stream, a);
+  else hipLaunchKernelGGL((cache_attn<FMT, false>), grid, dim3(kFewWaves * kWave), 0, stream, a);
   if (joins.x > 0 && a.cut) {
     if (p.rows == 16) hipLaunchKernelGGL((cache_attn_join<16>), joins, dim3(kJoinWaves * kWave), 0, stream, a);
     else hipLaunchKernelGGL((cache_attn_join<kRowUnit>), joins, dim3(kJoinWaves * kWave), 0, stream, a);
@@ -735,13 +739,16 @@ hipError_t launch(const AttnArgs& a, const CacheAttnPlan& p, hipStream_t stream)
 }  // namespace
 
 CacheAttnPlan cache_attn_plan(const CacheDims& c, const BatchDims& b, int hq) {
-  CacheAttnPlan p{16, kGrain, 0, 0, 0};
+  CacheAttnPlan p{16, kGrain, 0, false, 0, 0};
   if (b.n_seqs == 0 || b.n_rows == 0 || hq == 0) return p;
   const int64_t G = hq / c.hkv;
   // 16 rows a unit up to 48 rows a sequence on average, 128 above.  8 sequences of 4k to 8k tokens, e4m3, 16 /
   // 128, us: 32 heads over 8, 33 rows 31.5 / 43.6 and 66 rows 66.5 / 49.3; 28 over 4, 49 rows 27.7 / 39.7, 115 rows
   // 45.7 / 45.0 and 302 rows 72.0 / 69.3.
   p.rows = (int64_t)b.n_rows * G <= 48 * (int64_t)b.n_seqs ? 16 : kRowUnit;
+  // One unit a sequence and KV head on average: no tile is read again, and the loads say so.  Plain / such loads, us: 48
+  // rows over 0.3k to 8k tokens 93.6 / 83.6, one over 128k 37.5 / 33.5; but 32 sequences of 4k to 8k with 27 rows 123 / 144.
+  p.once = (int64_t)b.n_rows * G <= 16 * (int64_t)b.n_seqs;
   // units, and tiles of one, that the table has room for: upper bounds of what the lengths say on the device
   const int64_t units = ((int64_t)b.n_rows * G / p.rows + b.n_seqs) * c.hkv;
   const int64_t room = (int64_t)b.max_pages * c.tiles > 1 ? (int64_t)b.max_pages * c.tiles : 1;

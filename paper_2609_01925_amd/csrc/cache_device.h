@@ -50,6 +50,38 @@ __device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d)
   }
 }
 
+// Four finite bf16 (two a dword), |x| <= MAX 2^e, to four codes of scale 2^e, rounded to nearest even.
+// e4m3: the conversion divides by the scale.  int8: x 2^-e + 128 is exact in 32 bits wherever its
+// rounding is in question (x has eight significant bits), and the conversion to a byte rounds to even.
+template <int FMT>
+__device__ __forceinline__ uint32_t finite_codes(uint32_t x, uint32_t y, int e) {
+  if constexpr (FMT == kCacheE4M3) {
+    typedef __attribute__((__vector_size__(2 * sizeof(short)))) short i16x2;
+    i16x2 r = {0, 0};
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, x), pow2f(e), false);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, y), pow2f(e), true);
+    return __builtin_bit_cast(uint32_t, r);
+  } else {
+    const float inv = pow2f(-e);
+    const auto f = [&](uint32_t bits) { return __builtin_fmaf(__uint_as_float(bits), inv, 128.f); };
+    uint32_t r = __builtin_amdgcn_cvt_pk_u8_f32(f(x << 16), 0, 0);
+    r = __builtin_amdgcn_cvt_pk_u8_f32(f(x & 0xffff0000u), 1, r);
+    r = __builtin_amdgcn_cvt_pk_u8_f32(f(y << 16), 2, r);
+    r = __builtin_amdgcn_cvt_pk_u8_f32(f(y & 0xffff0000u), 3, r);
+    return r ^ 0x80808080u;
+  }
+}
+
+// Bytes of four dwords transposed: out[j] = byte j of r0, r1, r2, r3.
+__device__ __forceinline__ void transpose4(uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3, uint32_t (&out)[4]) {
+  const uint32_t t0 = __builtin_amdgcn_perm(r1, r0, 0x05010400u), t1 = __builtin_amdgcn_perm(r1, r0, 0x07030602u);
+  const uint32_t u0 = __builtin_amdgcn_perm(r3, r2, 0x05010400u), u1 = __builtin_amdgcn_perm(r3, r2, 0x07030602u);
+  out[0] = __builtin_amdgcn_perm(u0, t0, 0x05040100u);
+  out[1] = __builtin_amdgcn_perm(u0, t0, 0x07060302u);
+  out[2] = __builtin_amdgcn_perm(u1, t1, 0x05040100u);
+  out[3] = __builtin_amdgcn_perm(u1, t1, 0x07060302u);
+}
+
 typedef __attribute__((__vector_size__(2 * sizeof(float)))) float f32x2;
 
 // Four codes to floats.

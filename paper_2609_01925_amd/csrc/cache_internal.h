@@ -46,6 +46,7 @@ hipError_t launch_cache_copy(const CacheDims& c, const int32_t* pairs, int n_pai
 // with an equal share of the units' 64-token tiles each.
 struct CacheAttnPlan {
   int rows, grain, workgroups;  // grain: tiles that are never cut apart
+  bool once;                    // most tiles are read by one workgroup only
   size_t cut_bytes, bytes;      // workspace: what each boundary between shares cuts (0: nothing is cut), and all of it
 };
 CacheAttnPlan cache_attn_plan(const CacheDims& c, const BatchDims& b, int hq);

@@ -56,6 +56,28 @@ __device__ __forceinline__ int collect_free(const uint32_t* bits, int n_pages, i
   return found;
 }
 
+// Marks the n lowest free pages as in use, n of them being free: a word a thread, so that no two
+// threads write one.
+__device__ __forceinline__ void take_lowest(uint32_t* bits, int n_pages, int n, PoolLds& l) {
+  const int words = (n_pages + 31) / 32;
+  int found = 0;
+  for (int w0 = 0; w0 < words && found < n; w0 += kThreads) {
+    const int i = w0 + (int)threadIdx.x;
+    const uint32_t was = i < words ? load_word(bits + i) : ~0u;
+    uint32_t f = ~was & word_mask(i, n_pages);
+    const int cnt = __popc(f);
+    int total;
+    __syncthreads();
+    const int at = found + block_scan<int, kWavesPool>(cnt, l.wsum, &total) - cnt;
+    uint32_t left = f;  // what stays free: all but the lowest n - at
+    if (at + cnt <= n) left = 0;
+    else
+      for (int k = at; k < n; ++k) left &= left - 1;
+    if (f != left) bits[i] = was | (f & ~left);
+    found += total;
+  }
+}
+
 // Pages not in use among the words from `word` on, counted by the workgroup.
 __device__ __forceinline__ int count_free(const uint32_t* bits, int n_pages, int word, int* wsum) {
   const int words = (n_pages + 31) / 32;
@@ -162,10 +184,15 @@ __global__ __launch_bounds__(kThreads) void pool_reserve(int n_pages, int B, int
   Slots x;
   for (int p0 = 0; p0 < total; p0 += kRound) {
     read(p0, x);
+    int n = 0;  // missing pages of one sequence among the thread's slots
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
-      if (x.lack[k]) atomicAdd(&miss[x.s[k]], 1);
-      else if (x.page[k] >= 0 && x.page[k] < n_pages && pool[x.page[k]] > 1) atomicOr(&miss[x.s[k]], kShared);
+      n += x.lack[k];
+      if (n && (k == kEach - 1 || !x.lack[k + 1] || x.s[k + 1] != x.s[k])) {
+        atomicAdd(&miss[x.s[k]], n);
+        n = 0;
+      }
+      if (x.page[k] >= 0 && x.page[k] < n_pages && pool[x.page[k]] > 1) atomicOr(&miss[x.s[k]], kShared);
     }
   }
   __syncthreads();
@@ -221,12 +248,13 @@ __global__ __launch_bounds__(kThreads) void pool_reserve(int n_pages, int B, int
         if (x.lack[k]) {
           if (k0 < now) {
             table[x.e[k]] = l.buf[k0];
-            take_page(pool, bits, l.buf[k0]);
+            pool[l.buf[k0]] = 1;
           }
           ++k0;
         }
       rank += here;
     }
+    take_lowest(bits, n_pages, now, l);
     __threadfence();  // the next round looks for free pages in what this one has set
     __syncthreads();
   }
