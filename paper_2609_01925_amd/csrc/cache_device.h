@@ -113,9 +113,11 @@ __device__ __forceinline__ bf16x8 codes_to_bf16(uint32_t lo, uint32_t hi) {
     const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
   } else {
+    // the upper halves of the floats, whose lower halves are 0
     const f32x4 a = from_codes<FMT>(lo), b = from_codes<FMT>(hi);
-    const bf16x2 x = pack_bf16(a[0], a[1]), y = pack_bf16(a[2], a[3]), z = pack_bf16(b[0], b[1]), w = pack_bf16(b[2], b[3]);
-    return bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+    const auto pair = [](float x, float y) { return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u); };
+    const u32x4 r = {pair(a[0], a[1]), pair(a[2], a[3]), pair(b[0], b[1]), pair(b[2], b[3])};
+    return __builtin_bit_cast(bf16x8, r);
   }
 }
 
