@@ -259,9 +259,9 @@ __device__ __forceinline__ void softmax_step(const acc4 (&S)[C][4], float kc, in
 // maximum, sum and output, joined through LDS at the unit's end.  A lane's 16-byte loads are
 // matrix operands as they stand (cache_device.h): K of the next tile is loaded while the softmax
 // and PV of this one run, V while the next scores are made, nothing passes through LDS.
-template <int FMT, bool ONCE>
+template <int FMT, int C, bool ONCE>
 __global__ __launch_bounds__(kFewWaves* kWave, 2) void cache_attn(AttnArgs a) {
-  constexpr int NW = kFewWaves, C = 1, kRows = 16 * C;
+  constexpr int NW = kFewWaves, kRows = 16 * C;
   __shared__ __attribute__((aligned(16))) float xo[NW][C][8][kWave][4];
   __shared__ float xm[NW][kRows], xl[NW][kRows];
   __shared__ int64_t lds[NW + 2];
@@ -725,12 +725,14 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void cache_attn_join(AttnArgs a)
 
 template <int FMT>
 hipError_t launch(const AttnArgs& a, const CacheAttnPlan& p, hipStream_t stream) {
-  const dim3 grid(p.workgroups), joins(p.workgroups - 1, p.rows == 16 ? 1 : 4);
+  const dim3 grid(p.workgroups), joins(p.workgroups - 1, p.rows <= 32 ? 1 : 4);
   if (p.rows == kRowUnit) hipLaunchKernelGGL((cache_attn_rows<FMT>), grid, dim3(kRowWaves * kWave), 0, stream, a);
-  else if (p.once) hipLaunchKernelGGL((cache_attn<FMT, true>), grid, dim3(kFewWaves * kWave), 0, stream, a);
-  else hipLaunchKernelGGL((cache_attn<FMT, false>), grid, dim3(kFewWaves * kWave), 0, stream, a);
+  else if (p.rows == 16) hipLaunchKernelGGL((cache_attn<FMT, 1, true>), grid, dim3(kFewWaves * kWave), 0, stream, a);
+  else if (p.once) hipLaunchKernelGGL((cache_attn<FMT, 2, true>), grid, dim3(kFewWaves * kWave), 0, stream, a);
+  else hipLaunchKernelGGL((cache_attn<FMT, 2, false>), grid, dim3(kFewWaves * kWave), 0, stream, a);
   if (joins.x > 0 && a.cut) {
     if (p.rows == 16) hipLaunchKernelGGL((cache_attn_join<16>), joins, dim3(kJoinWaves * kWave), 0, stream, a);
+    else if (p.rows == 32) hipLaunchKernelGGL((cache_attn_join<32>), joins, dim3(kJoinWaves * kWave), 0, stream, a);
     else hipLaunchKernelGGL((cache_attn_join<kRowUnit>), joins, dim3(kJoinWaves * kWave), 0, stream, a);
   }
   return hipGetLastError();
@@ -742,13 +744,17 @@ CacheAttnPlan cache_attn_plan(const CacheDims& c, const BatchDims& b, int hq) {
   CacheAttnPlan p{16, kGrain, 0, false, 0, 0};
   if (b.n_seqs == 0 || b.n_rows == 0 || hq == 0) return p;
   const int64_t G = hq / c.hkv;
-  // 16 rows a unit up to 48 rows a sequence on average, 128 above.  8 sequences of 4k to 8k tokens, e4m3, 16 /
-  // 128, us: 32 heads over 8, 33 rows 31.5 / 43.6 and 66 rows 66.5 / 49.3; 28 over 4, 49 rows 27.7 / 39.7, 115 rows
-  // 45.7 / 45.0 and 302 rows 72.0 / 69.3.
-  p.rows = (int64_t)b.n_rows * G <= 48 * (int64_t)b.n_seqs ? 16 : kRowUnit;
-  // One unit a sequence and KV head on average: no tile is read again, and the loads say so.  Plain / such loads, us: 48
-  // rows over 0.3k to 8k tokens 93.6 / 83.6, one over 128k 37.5 / 33.5; but 32 sequences of 4k to 8k with 27 rows 123 / 144.
-  p.once = (int64_t)b.n_rows * G <= 16 * (int64_t)b.n_seqs;
+  // Rows of a unit, by the rows of an average sequence and KV head.  Sequences of 4k to 8k tokens, us, 16 / 32 / 128 rows a unit:
+  //   32 of 10 rows 77.5 / 77.3 / 113, of 18 103 / 81.6 / 115, of 27 122 / 105 / 135; 8 of 66 66.9 / 53.2 / 49.1, of 172 127 / 96.0 /
+  //   77.5 (e4m3); 8 of 66 68.6 / 53.6 / 57.0, of 106 84.9 / 67.7 / 81.3, of 172 130 / 97.2 / 95.4 (int8, whose codes cost more in
+  //   each of 128 rows' four waves); 64 of 4 rows, 2k tokens, 57.5 / 58.5 / 89.4, of 16 each 22.6 / 24.3 / 26.8.
+  const int64_t rows = (int64_t)b.n_rows * G, seqs = b.n_seqs;
+  const bool even16 = b.n_rows % seqs == 0 && rows <= 16 * seqs;
+  p.rows = rows <= 8 * seqs || even16 ? 16 : rows <= (c.fmt == kCacheE4M3 ? 64 : 128) * seqs ? 32 : kRowUnit;
+  // About one unit a sequence and KV head: tiles are not read again, and the loads say so.  Plain / such loads, us: 48 rows
+  // over 0.3k to 8k tokens 93.6 / 83.6, one over 128k 37.5 / 33.5; in units of 32 rows, 32 sequences of 18 rows 96.6 / 83.6, of
+  // 27 109 / 106, of 38 44.3 / 46.8, of 54 73.3 / 84.2.
+  p.once = rows <= 32 * seqs;
   // units, and tiles of one, that the table has room for: upper bounds of what the lengths say on the device
   const int64_t units = ((int64_t)b.n_rows * G / p.rows + b.n_seqs) * c.hkv;
   const int64_t room = (int64_t)b.max_pages * c.tiles > 1 ? (int64_t)b.max_pages * c.tiles : 1;
