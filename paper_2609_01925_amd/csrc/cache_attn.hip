@@ -80,11 +80,13 @@ __device__ __forceinline__ int64_t div64(int64_t x, int64_t y) {  // x, y >= 0; 
   return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
 }
 
-// The units of all sequences in a row, cut into equal shares.  Up to 64 sequences every wave looks
+// The grains of all units in a row, in shares that differ by one at most: workgroup i of n takes the places
+// from i total / n on (rounded down), where n is the grid or, if there are fewer, the grains.  Up to 64 sequences every wave looks
 // them over by itself, one a lane; more are counted by the workgroup, some a thread.
 template <int R, int NW>
 struct Places {
-  int64_t total, share;
+  int64_t total;
+  int shares;
   int64_t end, own;  // of this lane's sequence (few), of this thread's sequences (many)
   SeqRows mine;
   bool few;
@@ -111,8 +113,12 @@ struct Places {
       end = block_scan<int64_t, NW>(own, lds, &total);
     }
     total = lane_value(total, 0);
-    share = max(div64(total + workgroups - 1, workgroups), (int64_t)1);
+    shares = (int)min((int64_t)workgroups, total);
   }
+
+  __device__ __forceinline__ int64_t start(int wg) const { return div64(wg * total, shares); }
+  // The workgroup whose share holds a place.
+  __device__ __forceinline__ int owner(int64_t pos) const { return (int)div64((pos + 1) * shares - 1, total); }
 
   static __device__ __forceinline__ int64_t lane_value(int64_t x, int lane) {
     return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, lane) |
@@ -147,13 +153,14 @@ struct Places {
 };
 
 // The cut, if any, that a share leaves behind it: it ends `done` of `grains` into the unit.
-__device__ __forceinline__ Cut cut_of(int64_t share, int64_t base, int unit, int grains, int done, int head, int row, int rows,
+template <typename P>
+__device__ __forceinline__ Cut cut_of(const P& pl, int64_t base, int unit, int grains, int done, int head, int row, int rows,
                                       int row0) {
   Cut k{0, 0, head, row, rows, row0};
   if (done < grains) {
     const int64_t first = base + (int64_t)unit * grains;
-    k.first = (int)div64(first, share);
-    k.cuts = (int)div64(first + grains - 1, share) - k.first;
+    k.first = pl.owner(first);
+    k.cuts = pl.owner(first + grains - 1) - k.first;
   }
   return k;
 }
@@ -273,12 +280,12 @@ __global__ __launch_bounds__(kFewWaves* kWave, 2) void cache_attn(AttnArgs a) {
   const int wg = wgs % kNumXcd == 0 ? (int)blockIdx.x % kNumXcd * (wgs / kNumXcd) + (int)blockIdx.x / kNumXcd : (int)blockIdx.x;
   Places<kRows, NW> pl;
   pl.count(a, wgs, lds);
-  int64_t pos = wg * pl.share;
-  const int64_t stop = min(pos + pl.share, pl.total);
-  if (pos >= stop) {
+  if (wg >= pl.shares) {
     if (a.cut && tid == 0) a.cut[wg].cuts = 0;
     return;
   }
+  int64_t pos = pl.start(wg);
+  const int64_t stop = pl.start(wg + 1);
   int64_t base;
   int s = pl.find(a, pos, lds, &base);
   SeqWork<kRows> sw = pl.work(a, s);
@@ -441,7 +448,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, 2) void cache_attn(AttnArgs a) {
     __syncthreads();
     pos += part;
     if (pos >= stop && a.cut && tid == 0)
-      a.cut[wg] = cut_of(pl.share, base, unit, sw.grains, u0 + part, head, rt * kRows, min(rows - rt * kRows, kRows), sw.r.row0);
+      a.cut[wg] = cut_of(pl, base, unit, sw.grains, u0 + part, head, rt * kRows, min(rows - rt * kRows, kRows), sw.r.row0);
   }
 }
 
@@ -470,12 +477,12 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
   const int wg = (int)blockIdx.x % kNumXcd * (wgs / kNumXcd) + (int)blockIdx.x / kNumXcd;
   Places<kRows, NW> pl;
   pl.count(a, wgs, lds);
-  int64_t pos = wg * pl.share;
-  const int64_t stop = min(pos + pl.share, pl.total);
-  if (pos >= stop) {
+  if (wg >= pl.shares) {
     if (a.cut && tid == 0) a.cut[wg].cuts = 0;
     return;
   }
+  int64_t pos = pl.start(wg);
+  const int64_t stop = pl.start(wg + 1);
   int64_t base;
   int s = pl.find(a, pos, lds, &base);
   SeqWork<kRows> sw = pl.work(a, s);
@@ -622,105 +629,108 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
       }
     }
     pos += part;
-    if (pos >= stop && a.cut && tid == 0) a.cut[wg] = cut_of(pl.share, base, unit, sw.grains, u0 + part, head, rt * kRows, min(rows - rt * kRows, kRows), sw.r.row0);
+    if (pos >= stop && a.cut && tid == 0) a.cut[wg] = cut_of(pl, base, unit, sw.grains, u0 + part, head, rt * kRows, min(rows - rt * kRows, kRows), sw.r.row0);
     __syncthreads();  // all waves are done with the ring before the next unit fills it
   }
 #endif
 }
 
+// Pieces p = from, from + step, ... <= last of one row, added up by 32 lanes of four elements each: the common
+// reference m, the sum l and the output o under it.  N pieces are loaded at once; past the last it is that
+// one again, with the weight 0.
+template <int N, typename Slot>
+__device__ __forceinline__ void add_pieces(const Slot& slot, int rows, int r, int d, int from, int step, int last, float& m,
+                                           float& l, acc4& o) {
+  m = -__builtin_inff();
+  l = 0.f;
+  o = acc4{0.f, 0.f, 0.f, 0.f};
+  for (int p0 = from; p0 <= last; p0 += N * step) {
+    float pm[N], pl[N];
+    acc4 x[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float* src = slot(min(p0 + k * step, last));
+      pm[k] = src[rows * kHeadDim + r];
+      pl[k] = src[rows * kHeadDim + rows + r];
+      x[k] = *reinterpret_cast<const acc4*>(src + r * kHeadDim + d);
+    }
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      if (p0 + k * step > last) pm[k] = -__builtin_inff();
+      top = fmaxf(top, pm[k]);
+    }
+    const float ts = top == -__builtin_inff() ? 0.f : top, f = fast_exp2(m - ts);
+    l *= f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float w = fast_exp2(pm[k] - ts);
+      l = __builtin_fmaf(w, pl[k], l);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(w, x[k][e], o[e]);
+    }
+    m = top;
+  }
+}
+
 // Joins the pieces of the units that share boundaries cut.  Workgroup b stands at the boundary between
 // shares b and b + 1; the boundaries inside one unit take its rows in turn.  A piece that begins
 // its unit lies in the second slot of its workgroup, any other in the first.  Pieces are added in
-// a fixed order.
+// a fixed order.  All latency: the record, the pieces, the result.
 template <int kRows>
 __global__ __launch_bounds__(kJoinWaves* kWave) void cache_attn_join(AttnArgs a) {
   constexpr int64_t kSlot = kRows * (kHeadDim + 2);
   constexpr int kGroups = kJoinWaves * 2;  // of 32 lanes, each lane four elements
-  __shared__ float red[kJoinWaves], acc[kGroups][kHeadDim], sum[kGroups];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  __shared__ float ms[kGroups], ls[kGroups], acc[kGroups][kHeadDim];
+  const int tid = threadIdx.x;
   const Cut k = a.cut[blockIdx.x];
   if (k.cuts == 0) return;
   const int first = k.first, cuts = k.cuts, mine = (int)blockIdx.x - first, rows = k.rows;
   const int grp = tid >> 5, d = 4 * (tid & 31);
   const auto slot = [&](int p) { return a.part + (int64_t)(2 * (first + p) + (p == 0)) * kSlot; };
-  const auto dst = [&](int r) {
+  const auto write = [&](int r, float l, acc4 o) {
+    const float f = l > 0.f ? 1.f / l : 0.f;
     const int i = (k.row + r) / a.G;
-    return a.o + (k.head * a.G + (k.row + r - i * a.G)) * a.os.head + (k.row0 + i) * a.os.row;
+    uint16_t* dst = a.o + (k.head * a.G + (k.row + r - i * a.G)) * a.os.head + (k.row0 + i) * a.os.row + d;
+    const bf16x2 x = pack_bf16(o[0] * f, o[1] * f), y = pack_bf16(o[2] * f, o[3] * f);
+    *reinterpret_cast<bf16x4*>(dst) = bf16x4{x[0], x[1], y[0], y[1]};
   };
-  if (cuts < rows) {  // some rows a workgroup: one a group, whose lanes look up a piece each, then add all in turn
+  float m, l;
+  acc4 o;
+  if (cuts < rows) {  // some rows a workgroup: one a group
     for (int r = mine + cuts * (grp + kGroups * (int)blockIdx.y); r < rows; r += cuts * kGroups * (int)gridDim.y) {
-      float m = -__builtin_inff();
-      for (int p = tid & 31; p <= cuts; p += 32) m = fmaxf(m, slot(p)[kRows * kHeadDim + r]);
-#pragma unroll
-      for (int o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor(m, o, 32));
-      const float ms = m == -__builtin_inff() ? 0.f : m;
-      float l = 0.f;
-      acc4 o = {0.f, 0.f, 0.f, 0.f};
-      for (int p0 = 0; p0 <= cuts; p0 += 32) {
-        const int p1 = p0 + (tid & 31);
-        float f = 0.f;
-        if (p1 <= cuts) {
-          const float* src = slot(p1) + kRows * kHeadDim + r;
-          f = fast_exp2(src[0] - ms);
-          l += f * src[kRows];
-        }
-        for (int i = 0; i < min(cuts + 1 - p0, 32); i += 4) {
-          acc4 x[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k)  // past the last: that one again, with the weight 0
-            x[k] = *reinterpret_cast<const acc4*>(slot(min(p0 + i + k, cuts)) + r * kHeadDim + d);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float fi = __shfl(f, i + k, 32);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(fi, x[k][e], o[e]);
-          }
-        }
-      }
-#pragma unroll
-      for (int o2 = 16; o2; o2 /= 2) l += __shfl_xor(l, o2, 32);
-      const float f = l > 0.f ? 1.f / l : 0.f;
-      const bf16x2 x = pack_bf16(o[0] * f, o[1] * f), y = pack_bf16(o[2] * f, o[3] * f);
-      *reinterpret_cast<bf16x4*>(dst(r) + d) = bf16x4{x[0], x[1], y[0], y[1]};
+      add_pieces<4>(slot, kRows, r, d, 0, 1, cuts, m, l, o);
+      write(r, l, o);
     }
     return;
   }
-  if (blockIdx.y > 0) return;
-  for (int r = mine; r < rows; r += cuts) {  // at most one: each group takes every eighth piece
-    float m = -__builtin_inff();
-    for (int p = tid; p <= cuts; p += kJoinWaves * kWave) m = fmaxf(m, slot(p)[kRows * kHeadDim + r]);
-    m = wave_max(m);
-    if (lane == 0) red[w] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    const float ms = m == -__builtin_inff() ? 0.f : m;
-    float l = 0.f;
-    acc4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int p = grp; p <= cuts; p += kGroups) {
-      const float* src = slot(p);
-      const float f = fast_exp2(src[kRows * kHeadDim + r] - ms);
-      l += f * src[kRows * kHeadDim + kRows + r];
-      const acc4 x = *reinterpret_cast<const acc4*>(src + r * kHeadDim + d);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(f, x[i], o[i]);
-    }
-    *reinterpret_cast<acc4*>(&acc[grp][d]) = o;
-    if ((tid & 31) == 0) sum[grp] = l;
-    __syncthreads();
-    if (tid < kHeadDim / 2) {
-      float x = 0.f, y = 0.f, t = 0.f;
-#pragma unroll
-      for (int i = 0; i < kGroups; ++i) {
-        x += acc[i][2 * tid];
-        y += acc[i][2 * tid + 1];
-        t += sum[i];
-      }
-      const float f = t > 0.f ? 1.f / t : 0.f;
-      *reinterpret_cast<bf16x2*>(dst(r) + 2 * tid) = pack_bf16(x * f, y * f);
-    }
-    __syncthreads();
+  if (mine >= rows || blockIdx.y > 0) return;
+  // at most one: each group takes every eighth piece, and the first joins the groups
+  add_pieces<8>(slot, kRows, mine, d, grp, kGroups, cuts, m, l, o);
+  if ((tid & 31) == 0) {
+    ms[grp] = m;
+    ls[grp] = l;
   }
+  *reinterpret_cast<acc4*>(&acc[grp][d]) = o;
+  __syncthreads();
+  if (grp > 0) return;
+  float top = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) top = fmaxf(top, ms[i]);
+  if (top == -__builtin_inff()) top = 0.f;
+  l = 0.f;
+  o = acc4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kGroups; ++i) {
+    const float w = fast_exp2(ms[i] - top);
+    l = __builtin_fmaf(w, ls[i], l);
+    const acc4 x = *reinterpret_cast<const acc4*>(&acc[i][d]);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(w, x[e], o[e]);
+  }
+  write(mine, l, o);
 }
 
 template <int FMT>
