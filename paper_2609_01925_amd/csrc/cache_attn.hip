@@ -207,6 +207,13 @@ struct TileList {
   }
 };
 
+// Eight probabilities to bf16, and the sum of what they are rounded to.
+__device__ __forceinline__ float form_eight(const float (&p)[8], bf16x8& P) {
+  const bf16x2 x = pack_bf16(p[0], p[1]), y = pack_bf16(p[2], p[3]), z = pack_bf16(p[4], p[5]), v = pack_bf16(p[6], p[7]);
+  P = bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], v[0], v[1]};
+  return dot2_bf16_sum(v, dot2_bf16_sum(z, dot2_bf16_sum(y, dot2_bf16_sum(x, 0.f))));
+}
+
 // One tile's softmax for C groups of columns: S (raw products, register i of score tile ti is key
 // 16 g + 4 ti + i) becomes P, the next product's operands; kc takes S to the base-2 exponent, and P is made as
 // 2^ev p, what V's codes are to be multiplied by.  The probabilities are formed against the reference M
@@ -228,9 +235,7 @@ __device__ __forceinline__ void softmax_step(const acc4 (&S)[C][4], float kc, in
         float p[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[e] = fast_exp2(__builtin_fmaf(S[c][2 * st + e / 4][e & 3], kc, -sub));
-        const bf16x2 x = pack_bf16(p[0], p[1]), y = pack_bf16(p[2], p[3]), z = pack_bf16(p[4], p[5]), v = pack_bf16(p[6], p[7]);
-        sum = dot2_bf16_sum(v, dot2_bf16_sum(z, dot2_bf16_sum(y, dot2_bf16_sum(x, sum))));
-        P[c][st] = bf16x8{x[0], x[1], y[0], y[1], z[0], z[1], v[0], v[1]};
+        sum += form_eight(p, P[c][st]);
       }
       return sum * inv_v;
     };
@@ -456,7 +461,17 @@ __global__ __launch_bounds__(kFewWaves* kWave, 2) void cache_attn(AttnArgs a) {
 // codes come into LDS once a workgroup by direct loads, three tiles deep.  The waves' rows
 // are their own, so nothing is joined inside the workgroup.  Two workgroups share a CU: while a wave of one
 // forms probabilities, one of the other feeds the matrix unit.
-constexpr int kRowWaves = 4, kRowGroups = 2, kRowUnit = 16 * kRowGroups * kRowWaves;
+//
+// The products are v_mfma_f32_32x32x16_bf16 (layouts in crisp_device.h): beside these the other wave's vector
+// instructions run 1.45 times as long as alone, beside the 16 x 16 ones 1.9 times.  The tile's chunks serve them as
+// well, each lane reading from LDS the ones it needs (a quarter of a wave reads 256 bytes in a row).
+// With h = l / 32:
+//   K: score tile T (32 keys), step (g, m): lane l takes chunk (t = 2 T + l % 32 / 16, half = h, g, r = l % 16), bytes
+//      8 m ..: key of row l % 32, elements 32 g + 16 h + 8 m + [0, 8).  The result's register i of a lane is key
+//      16 (2 q + h) + 4 (2 T + i / 8) + i % 4 with q = i / 4 % 2: 16 keys in a row for each q.
+//   V: output rows 32 D .., step (q, s): chunk (dt = 2 D + l % 32 / 16, g = 2 q + h, r = l % 16), bytes 8 s ..: those
+//      keys' 8 s + [0, 8), so that P again stays in its lane.
+constexpr int kRowWaves = 4, kRowUnit = 32 * kRowWaves;
 
 #if defined(__HIP_DEVICE_COMPILE__)
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
@@ -466,13 +481,13 @@ __device__ __forceinline__ u32x4 lds_chunk_at(int addr) { return *(const lds_u32
 template <int FMT>
 __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int C = kRowGroups, NW = kRowWaves, kRows = kRowUnit, kStages = 3;
+  constexpr int NW = kRowWaves, kRows = kRowUnit, kStages = 3;
   constexpr int kStage = 2 * kTileBytes;
   __shared__ __attribute__((aligned(1024))) char ring[kStages * kStage];
   __shared__ int64_t lds[NW + 2];
   const int ring0 = __builtin_amdgcn_readfirstlane((int)(size_t)ring);
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int col = lane & 15, g = lane >> 4;
+  const int col = lane & 31, h = lane >> 5;
   const int wgs = gridDim.x;
   const int wg = (int)blockIdx.x % kNumXcd * (wgs / kNumXcd) + (int)blockIdx.x / kNumXcd;
   Places<kRows, NW> pl;
@@ -486,6 +501,8 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
   int64_t base;
   int s = pl.find(a, pos, lds, &base);
   SeqWork<kRows> sw = pl.work(a, s);
+  const int k_at = ring0 + (col >> 4) * 2048 + h * 1024 + (col & 15) * kChunk;              // + T 4096 + g 256
+  const int v_at = ring0 + kTileBytes + (col >> 4) * 1024 + h * 256 + (col & 15) * kChunk;  // + D 2048 + q 512
   while (pos < stop) {
     while (pos >= base + sw.all(a)) {
       base += sw.all(a);
@@ -498,33 +515,25 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
     const int t0 = u0 * a.grain, t1 = min((u0 + part) * a.grain, sw.T);  // the tiles of this piece
     const int rows = sw.r.n * a.G;
     const int held = min(sw.r.len + sw.r.n, a.b.max_pages * a.c.B);
-    const int r0 = rt * kRows + w * (16 * C);  // the wave's first row
+    const int r0 = rt * kRows + w * 32;  // the wave's first row
     const bool live = r0 < rows;
-    bf16x8 Q[C][4];
-    int see[C];
+    const int r = r0 + col, row_i = r / a.G;
+    const int see = r < rows ? sw.r.len + row_i : -1;  // the last position that this lane's column sees
+    const int64_t q_at = (head * a.G + (r - row_i * a.G)) * a.qs.head + (sw.r.row0 + row_i) * a.qs.row;
+    bf16x8 Q[4][2];  // step (g, m)
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int r = r0 + 16 * c + col;
-      const int i = r / a.G;
-      see[c] = r < rows ? sw.r.len + i : -1;
-      const uint16_t* src = a.q + (head * a.G + (r - i * a.G)) * a.qs.head + (sw.r.row0 + i) * a.qs.row + 32 * g;
+    for (int g = 0; g < 4; ++g)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        Q[c][j] = bf16x8{};
-        if (r < rows) Q[c][j] = *reinterpret_cast<const bf16x8*>(src + 8 * j);
+      for (int m = 0; m < 2; ++m) {
+        Q[g][m] = bf16x8{};
+        if (r < rows) Q[g][m] = *reinterpret_cast<const bf16x8*>(a.q + q_at + 32 * g + 16 * h + 8 * m);
       }
-    }
     const int see_first = sw.r.len + r0 / a.G;
     const int see_last = sw.r.len + (min(rt * kRows + kRows, rows) - 1) / a.G;
-    acc4 O[C][8];
-    float M[C], L[C];
+    f32x16 O[4];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      M[c] = see[c] >= 0 ? -__builtin_inff() : 0.f;  // a column without a row asks for no reference
-      L[c] = 0.f;
-#pragma unroll
-      for (int dt = 0; dt < 8; ++dt) O[c][dt] = acc4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int D = 0; D < 4; ++D) O[D] = zero16();
+    float M = see >= 0 ? -__builtin_inff() : 0.f, L = 0.f;  // a column without a row asks for no reference
     TileList<1> list(a, s, head, t0, min(t1, see_last / kTile + 1));
     // a wave copies a quarter of the tile: its chunks 256 w ..
     const auto fetch = [&](const TileInfo& tl, int stage) {
@@ -549,87 +558,119 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
       __syncthreads();  // this tile is there for all waves, and all are done with the one before it
       const TileInfo then = next.page >= 0 ? list.next(a, head) : TileInfo{0, -1, 0, 0.f};
       if (then.page >= 0) fetch(then, stage == 0 ? 2 : stage - 1);
-      if (live && now.t * kTile <= see_last) {
-        const int kt = ring0 + stage * kStage + lane * kChunk, vt = kt + kTileBytes;
+      if (live) {
         u32x4 x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = lds_chunk_at(kt + i * (kWave * kChunk));
-        acc4 S[C][4];
+        for (int i = 0; i < 8; ++i) x[i] = lds_chunk_at(k_at + stage * kStage + (i & 1) * 4096 + (i >> 1) * 256);
+        f32x16 S[2] = {zero16(), zero16()};
 #pragma unroll
-        for (int j = 0; j < 4; ++j)  // by steps of d, so that products into one accumulator are apart
+        for (int g = 0; g < 4; ++g)
 #pragma unroll
-          for (int ti = 0; ti < 4; ++ti) {
-            const u32x4 y = x[2 * ti + j / 2];
-            const bf16x8 k = codes_to_bf16<FMT>(y[2 * (j & 1)], y[2 * (j & 1) + 1]);
+          for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int c = 0; c < C; ++c) S[c][ti] = mfma16(k, Q[c][j], j == 0 ? acc4{0.f, 0.f, 0.f, 0.f} : S[c][ti]);
-          }
+            for (int T = 0; T < 2; ++T) S[T] = mfma32(codes_to_bf16<FMT>(x[2 * g + T][2 * m], x[2 * g + T][2 * m + 1]), Q[g][m], S[T]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = lds_chunk_at(vt + i * (kWave * kChunk));
-        const int key0 = now.t * kTile + 16 * g;
-        const bool edge = now.t * kTile + kTile - 1 > see_first;
-        if (edge) {
+        for (int i = 0; i < 8; ++i) x[i] = lds_chunk_at(v_at + stage * kStage + (i >> 1) * 2048 + (i & 1) * 512);
+        if (now.t * kTile + kTile - 1 > see_first) {  // some column does not see the whole tile
 #pragma unroll
-          for (int c = 0; c < C; ++c)
+          for (int T = 0; T < 2; ++T)
 #pragma unroll
-            for (int ti = 0; ti < 4; ++ti)
+            for (int i = 0; i < 16; ++i)
+              if (now.t * kTile + 16 * (2 * (i / 4 % 2) + h) + 4 * (2 * T + i / 8) + i % 4 > see) S[T][i] = -__builtin_inff();
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (key0 + 4 * ti + i > see[c]) S[c][ti][i] = -__builtin_inff();
+          for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int bytes = min(max(held - now.t * kTile - 16 * (2 * q + h) - 4 * e, 0), 4);
+              const uint32_t keep = bytes == 4 ? ~0u : (1u << (8 * bytes)) - 1u;
+#pragma unroll
+              for (int D = 0; D < 4; ++D) x[2 * D + q][e] = without_nan<FMT>(x[2 * D + q][e] & keep);
+            }
         }
-        bf16x8 P[C][2];
+        bf16x8 P[2][2];  // (q, s)
+        const float inv_v = pow2f(-now.ev);
+        const auto form = [&] {
+          const float sub = M - (float)now.ev;
+          float sum = 0.f;
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+              float p[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) p[j] = fast_exp2(__builtin_fmaf(S[st][4 * (j / 4 * 2 + q) + j % 4], now.kc, -sub));
+              sum += form_eight(p, P[q][st]);
+            }
+          return sum * inv_v;
+        };
         __builtin_amdgcn_s_setprio(1);
-        softmax_step<C>(S, now.kc, now.ev, M, L, O, P);
-        __builtin_amdgcn_s_setprio(0);
-        if (edge) {
+        float sum = form();
+        if (__ballot(!(sum <= 256.f))) {  // as in softmax_step
+          float mx = S[0][0];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int bytes = min(max(held - key0 - 4 * e, 0), 4);
-            const uint32_t keep = bytes == 4 ? ~0u : (1u << (8 * bytes)) - 1u;
+          for (int T = 0; T < 2; ++T)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i][e] = without_nan<FMT>(x[i][e] & keep);
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, S[T][i]);
+          const float top = fmaxf(M, half_max(mx) * now.kc);
+          if (top != M) {
+            const float f = fast_exp2(M - top);
+            L *= f;
+#pragma unroll
+            for (int D = 0; D < 4; ++D)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) O[D][i] *= f;
+            M = top;
+          }
+          sum = form();
+          if (M == -__builtin_inff()) {
+            sum = 0.f;
+            P[0][0] = P[0][1] = P[1][0] = P[1][1] = bf16x8{};
           }
         }
+        L += sum;
+        __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-        for (int st = 0; st < 2; ++st)
+        for (int q = 0; q < 2; ++q)
 #pragma unroll
-          for (int dt = 0; dt < 8; ++dt) {
-            const bf16x8 v = codes_to_bf16<FMT>(x[dt][2 * st], x[dt][2 * st + 1]);
+          for (int st = 0; st < 2; ++st)
 #pragma unroll
-            for (int c = 0; c < C; ++c) O[c][dt] = mfma16(v, P[c][st], O[c][dt]);
-          }
+            for (int D = 0; D < 4; ++D)
+              O[D] = mfma32(codes_to_bf16<FMT>(x[2 * D + q][2 * st], x[2 * D + q][2 * st + 1]), P[q][st], O[D]);
       }
       now = next;
       next = then;
       stage = stage == 2 ? 0 : stage + 1;
     }
     const bool whole = part == sw.grains;
-    float* slot = a.part + (int64_t)(2 * wg + (u0 == 0)) * (kRows * (kHeadDim + 2));
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const float l = column(L[c], [](float x, float y) { return x + y; });
-      const int r = r0 + 16 * c + col, x = r - rt * kRows;
-      if (r >= rows) continue;
+    const float l = half_sum(L);
+    if (r < rows) {  // register i of O[D] is element 32 D + 8 (i / 4) + 4 h + i % 4
       if (whole) {
         const float inv = l > 0.f ? 1.f / l : 0.f;
-        const int i = r / a.G;
-        uint16_t* dst = a.o + (head * a.G + (r - i * a.G)) * a.os.head + (sw.r.row0 + i) * a.os.row + 4 * g;
+        uint16_t* dst = a.o + (head * a.G + (r - row_i * a.G)) * a.os.head + (sw.r.row0 + row_i) * a.os.row + 4 * h;
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) {
-          const bf16x2 p = pack_bf16(O[c][dt][0] * inv, O[c][dt][1] * inv), q = pack_bf16(O[c][dt][2] * inv, O[c][dt][3] * inv);
-          *reinterpret_cast<bf16x4*>(dst + 16 * dt) = bf16x4{p[0], p[1], q[0], q[1]};
-        }
+        for (int D = 0; D < 4; ++D)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4) {
+            const bf16x2 p = pack_bf16(O[D][i] * inv, O[D][i + 1] * inv), q = pack_bf16(O[D][i + 2] * inv, O[D][i + 3] * inv);
+            *reinterpret_cast<bf16x4*>(dst + 32 * D + 2 * i) = bf16x4{p[0], p[1], q[0], q[1]};
+          }
       } else {
+        float* slot = a.part + (int64_t)(2 * wg + (u0 == 0)) * (kRows * (kHeadDim + 2));
+        const int x = r - rt * kRows;
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<acc4*>(slot + x * kHeadDim + 16 * dt + 4 * g) = O[c][dt];
-        if (g == 0) {
-          slot[kRows * kHeadDim + x] = M[c];
+        for (int D = 0; D < 4; ++D)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<acc4*>(slot + x * kHeadDim + 32 * D + 2 * i + 4 * h) = acc4{O[D][i], O[D][i + 1], O[D][i + 2], O[D][i + 3]};
+        if (h == 0) {
+          slot[kRows * kHeadDim + x] = M;
           slot[kRows * kHeadDim + kRows + x] = l;
         }
       }
     }
     pos += part;
-    if (pos >= stop && a.cut && tid == 0) a.cut[wg] = cut_of(pl, base, unit, sw.grains, u0 + part, head, rt * kRows, min(rows - rt * kRows, kRows), sw.r.row0);
+    if (pos >= stop && a.cut && tid == 0)
+      a.cut[wg] = cut_of(pl, base, unit, sw.grains, u0 + part, head, rt * kRows, min(rows - rt * kRows, kRows), sw.r.row0);
     __syncthreads();  // all waves are done with the ring before the next unit fills it
   }
 #endif
