@@ -17,6 +17,10 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWavesPool = kThreads / kWave;
 constexpr int kBuf = 4096;  // free pages collected at a time
+// Up to so many row entries a fork fills the new rows in its own launch.  A free and a fork of 16, in a second launch / here,
+// us, called from a host program and replayed from a graph: 64 slots 18.1 / 15.2 and 11.1 / 9.9; 256 (the limit) 18.0 / 15.1 and
+// 11.6 / 13.3; 512 18.1 / 17.0 and 12.8 / 16.7; 1024 18.0 / 27.1 and 15.0 / 26.6.
+constexpr int64_t kShareHere = 4096;
 constexpr int kPerThread = kPoolMaxSeqs / kThreads;
 static_assert(kPoolMaxSeqs <= kBuf, "a fork collects its pages at once");
 
@@ -260,13 +264,26 @@ __global__ __launch_bounds__(kThreads) void pool_reserve(int n_pages, int B, int
   }
 }
 
+// Slot j of a fork that holds len tokens: a full page is listed in the new row and counted once more, the
+// slots behind the last page are empty (the partial page's slot is set already).
+__device__ __forceinline__ void share_slot(int n_pages, int B, int32_t* pool, const int32_t* from, int32_t* to, int len, int j) {
+  if (j < len / B) {
+    const int p = from[j];
+    to[j] = p;
+    if (p >= 0 && p < n_pages) atomicAdd(pool + p, 1);
+  } else if (j >= (len + B - 1) / B) {
+    to[j] = -1;
+  }
+}
+
 // Fork i makes the empty sequence dst[i] hold what src[i] holds.  Of two forks into one sequence
 // the first counts.  A partial last page is not shared but copied to the lowest free page:
 // copies[i] = (page, its copy), (-1, -1) where there is nothing to copy, (-2, -2) where the fork
-// is refused.  Lengths are those before the call.
+// is refused.  Lengths are those before the call.  share: the rows are filled here too.
 __global__ __launch_bounds__(kThreads) void pool_fork(int n_pages, int B, int n_seqs, int max_pages, int32_t* pool,
                                                       int32_t* table, int32_t* seq_len, const int32_t* src,
-                                                      const int32_t* dst, int n, int32_t* copies) {
+                                                      const int32_t* dst, int n, int32_t* copies,
+                                                      bool share) {
   __shared__ PoolLds l;
   __shared__ int lens[kPoolMaxSeqs], owner[kPoolMaxSeqs];
   uint32_t* bits = bits_of(pool, n_pages);
@@ -319,30 +336,27 @@ __global__ __launch_bounds__(kThreads) void pool_fork(int n_pages, int B, int n_
         seq_len[dst[i]] = lens[i];
       }
     }
+    if (from == -2) lens[i] = -1;
     copies[2 * i] = from;
     copies[2 * i + 1] = to;
   }
+  if (!share) return;
+  __syncthreads();
+  for (int e = tid; e < n * max_pages; e += kThreads) {
+    const int i = e / max_pages, j = e % max_pages;
+    if (lens[i] >= 0)
+      share_slot(n_pages, B, pool, table + (int64_t)src[i] * max_pages, table + (int64_t)dst[i] * max_pages, lens[i], j);
+  }
 }
 
-// The full pages of a granted fork: listed in dst's row and counted once more; the slots behind are empty.
+// The rows of the granted forks, a workgroup each.
 __global__ __launch_bounds__(256) void pool_share(int n_pages, int B, int max_pages, int32_t* pool, int32_t* table,
                                                   const int32_t* seq_len, const int32_t* src, const int32_t* dst,
                                                   const int32_t* copies) {
   const int i = blockIdx.x;
   if (copies[2 * i] == -2) return;
-  const int len = seq_len[dst[i]];
-  const int full = len / B, held = (len + B - 1) / B;
-  const int32_t* from = table + (int64_t)src[i] * max_pages;
-  int32_t* to = table + (int64_t)dst[i] * max_pages;
-  for (int j = threadIdx.x; j < max_pages; j += 256) {
-    if (j < full) {
-      const int p = from[j];
-      to[j] = p;
-      if (p >= 0 && p < n_pages) atomicAdd(pool + p, 1);
-    } else if (j >= held) {
-      to[j] = -1;
-    }
-  }
+  for (int j = threadIdx.x; j < max_pages; j += 256)
+    share_slot(n_pages, B, pool, table + (int64_t)src[i] * max_pages, table + (int64_t)dst[i] * max_pages, seq_len[dst[i]], j);
 }
 
 // Every page in the row of a freed sequence loses one use.  The exchange gives each page to one
@@ -439,10 +453,11 @@ hipError_t launch_pool_reserve(int n_pages, int block, int n_seqs, int max_pages
 hipError_t launch_pool_fork(int n_pages, int block, int n_seqs, int max_pages, int32_t* pool, int32_t* table,
                             int32_t* seq_len, const int32_t* src, const int32_t* dst, int n, int32_t* copies,
                             hipStream_t stream) {
+  const bool share = (int64_t)n * max_pages <= kShareHere;
   hipLaunchKernelGGL(pool_fork, dim3(1), dim3(kThreads), 0, stream, n_pages, block, n_seqs, max_pages, pool, table,
-                     seq_len, src, dst, n, copies);
+                     seq_len, src, dst, n, copies, share);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || share) return e;
   hipLaunchKernelGGL(pool_share, dim3((unsigned)n), dim3(256), 0, stream, n_pages, block, max_pages, pool, table,
                      (const int32_t*)seq_len, src, dst, (const int32_t*)copies);
   return hipGetLastError();
