@@ -243,6 +243,92 @@ __global__ __launch_bounds__(256 * TILES) void cache_append(AppendArgs a) {
   }
 }
 
+// A wave takes a row and KV head: if the row is the first that the call writes to its page, all of them there (one, in a
+// decoding step).  A lane holds two elements; codes go out as they are, two bytes of K and a byte each of two of V's
+// chunks, since what lies beside them is only touched where a scale grows.  No LDS and no barrier: the
+// general kernel's chain without its waits, and a quarter of a workgroup a head.
+template <int FMT>
+__global__ __launch_bounds__(4 * kWave) void cache_append_few(AppendArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = (int)(wave / a.c.hkv), head = (int)(wave % a.c.hkv), B = a.c.B;
+  if (row >= a.b.n_rows) return;
+  // the row's sequence: among up to 64 the one that has it, among more the last that begins at or before it,
+  // looked for 64 at a time
+  int seq = 0;
+  if (a.b.n_seqs <= kWave) {
+    bool has = false;
+    if (lane < a.b.n_seqs) {
+      const SeqRows x = seq_rows(a.s, a.b, B, lane);
+      has = row >= x.row0 && row < x.row0 + x.n;
+    }
+    const unsigned long long found = __ballot(has);
+    if (found == 0) return;
+    seq = __builtin_ctzll(found);
+  } else {
+    for (int n = a.b.n_seqs; n > 1;) {
+      const int step = (n + kWave - 1) / kWave, probe = lane * step;
+      const unsigned long long ok = __ballot(probe < n && a.s.row_ptr[seq + min(probe, n - 1)] <= row);
+      const int k = max(__popcll(ok) - 1, 0);
+      seq += k * step;
+      n = min(step, n - k * step);
+    }
+  }
+  const SeqRows r = seq_rows(a.s, a.b, B, seq);
+  const int i = row - r.row0, pos = r.len + i, t0 = pos % B;
+  if (i < 0 || i >= r.n || (i > 0 && t0 != 0)) return;
+  const int n = min(r.n - i, B - t0), slot = pos / B;
+  const int page = slot < a.b.max_pages ? a.s.table[(int64_t)seq * a.b.max_pages + slot] : -1;
+  const uint16_t* src[2] = {a.k + head * a.ks.head + row * a.ks.row + 2 * lane, a.v + head * a.vs.head + row * a.vs.row + 2 * lane};
+  const int64_t rs[2] = {a.ks.row, a.vs.row};
+  uint32_t x[2] = {*reinterpret_cast<const uint32_t*>(src[0]), *reinterpret_cast<const uint32_t*>(src[1])};
+  if (page < 0 || page >= a.c.n_pages) return;
+  float* scale = a.scales + ((int64_t)page * a.c.hkv + head) * 2;
+  uint8_t* dst = a.pages + ((int64_t)page * a.c.hkv + head) * (2 * (int64_t)B * kHeadDim);
+  const auto finite = [](uint32_t bits) { return bits < 0x7f80u ? bits : 0u; };
+  float inv[2];
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    uint32_t m = max(finite(x[y] & 0x7fffu), finite((x[y] >> 16) & 0x7fffu));
+    for (int j = 1; j < n; ++j) {
+      const uint32_t z = *reinterpret_cast<const uint32_t*>(src[y] + j * rs[y]);
+      m = max(m, max(finite(z & 0x7fffu), finite((z >> 16) & 0x7fffu)));
+    }
+    m = wave_reduce(m, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+    int e = scale_exp<FMT>((int)m);
+    if (t0 > 0) {
+      const int old = stored_exp(scale[y]);
+      if (e > old) {  // the page's other codes under the new scale
+        const float down = pow2f(max(old - e, -126));
+        for (int c = lane; c < a.c.tiles * (kTileBytes / kChunk); c += kWave) {
+          u32x4* at = reinterpret_cast<u32x4*>(dst + (c / (kTileBytes / kChunk) * 2 + y) * kTileBytes) + c % (kTileBytes / kChunk);
+          *at = rescale<FMT>(*at, down);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the new codes are stored behind these
+      }
+      e = max(e, old);
+    }
+    if (lane == 0) scale[y] = pow2f(e);
+    inv[y] = pow2f(-e);
+  }
+  const int e0 = 2 * lane;
+  for (int j = 0; j < n; ++j) {
+    if (j > 0)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) x[y] = *reinterpret_cast<const uint32_t*>(src[y] + j * rs[y]);
+    uint32_t c[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+      c[y] = to_codes<FMT>(__uint_as_float(x[y] << 16) * inv[y], __uint_as_float(x[y] & 0xffff0000u) * inv[y], 0.f, 0.f);
+    const int t = (t0 + j) % kTile;
+    uint8_t* tile = dst + (t0 + j) / kTile * (2 * kTileBytes);
+    *reinterpret_cast<uint16_t*>(tile + ((t / 4 % 4 * 2 + e0 / 16 % 2) * 64 + e0 / 32 * 16 + t / 16 * 4 + t % 4) * 16 + e0 % 16) = (uint16_t)c[0];
+    uint8_t* v = tile + kTileBytes + (e0 / 16 * 64 + t / 16 * 16 + e0 % 16) * 16 + t % 16;
+    v[0] = (uint8_t)c[1];
+    v[16] = (uint8_t)(c[1] >> 8);
+  }
+}
+
 // pairs[i] = (from, to): 16 KB pieces (one tile of K and V of one head) over a persistent grid; a
 // pair with a page out of range or with from == to moves nothing.  Bound by HBM.
 __global__ __launch_bounds__(kThreads) void cache_copy(CacheDims c, const int32_t* pairs, int n_pairs,
@@ -271,11 +357,21 @@ __global__ __launch_bounds__(kThreads) void cache_copy(CacheDims c, const int32_
 
 hipError_t launch_cache_append(const CacheDims& c, const BatchDims& b, const Seqs& s, const uint16_t* k, Strides ks,
                                const uint16_t* v, Strides vs, uint8_t* pages, float* scales, hipStream_t stream) {
+  const AppendArgs a{c, b, s, k, v, ks, vs, pages, scales};
+  // Few rows a sequence: a wave for each row and head.  8 heads, e4m3, the page kernel / this one, us: 64 sequences of one row
+  // 5.7 / 3.9, of 2.8 on average 6.8 / 6.4, of 4.0 7.0 / 7.8; past 64 sequences, which the page kernel has to count, 1000
+  // of one 37.3 / 10.3, of 4.5 57.1 / 30.2; 4000 of one 201 / 27.3.
+  if (b.n_rows <= (b.n_seqs <= kWave ? 3 : 8) * (int64_t)b.n_seqs) {
+    const int64_t waves = (int64_t)b.n_rows * c.hkv;
+    const dim3 few((unsigned)((waves + 3) / 4));
+    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((cache_append_few<kCacheE4M3>), few, dim3(4 * kWave), 0, stream, a);
+    else hipLaunchKernelGGL((cache_append_few<kCacheInt8>), few, dim3(4 * kWave), 0, stream, a);
+    return hipGetLastError();
+  }
   // a sequence's n rows touch at most (n - 1) / B + 2 pages, and at most n
   const int64_t with_rows = b.n_seqs < b.n_rows ? b.n_seqs : b.n_rows;
   int64_t items = b.n_rows / c.B + 2 * with_rows;
   if (items > b.n_rows) items = b.n_rows;
-  const AppendArgs a{c, b, s, k, v, ks, vs, pages, scales};
   const dim3 grid((unsigned)items, (unsigned)c.hkv);
   if (c.fmt == kCacheE4M3) {
     if (c.tiles == 1) hipLaunchKernelGGL((cache_append<kCacheE4M3, 1>), grid, dim3(256), 0, stream, a);

@@ -295,7 +295,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, 2) void cache_attn(AttnArgs a) {
   int s = pl.find(a, pos, lds, &base);
   SeqWork<kRows> sw = pl.work(a, s);
   while (pos < stop) {
-    while (pos >= base + sw.all(a)) {
+    while (pos >= base + sw.all(a) && s + 1 < a.b.n_seqs) {
       base += sw.all(a);
       sw = pl.work(a, ++s);
     }
@@ -504,7 +504,7 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
   const int k_at = ring0 + (col >> 4) * 2048 + h * 1024 + (col & 15) * kChunk;              // + T 4096 + g 256
   const int v_at = ring0 + kTileBytes + (col >> 4) * 1024 + h * 256 + (col & 15) * kChunk;  // + D 2048 + q 512
   while (pos < stop) {
-    while (pos >= base + sw.all(a)) {
+    while (pos >= base + sw.all(a) && s + 1 < a.b.n_seqs) {
       base += sw.all(a);
       sw = pl.work(a, ++s);
     }

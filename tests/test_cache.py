@@ -89,19 +89,21 @@ def _check_attn(C, c, oracle, table, lens, counts, q, scale=0.0):
 # ------------------------------------------------------------------ appending
 
 
+@pytest.mark.parametrize("rows_a_call", [512, 4])
 @pytest.mark.parametrize("fmt", FORMATS)
-def test_every_bf16_value(fmt):
+def test_every_bf16_value(fmt, rows_a_call):
     """All 65536 bit patterns, 128 neighbours in magnitude a row, so that a page's values lie within
     a few octaves: rounding, subnormal codes, zeros, infinities and NaN."""
     C = _crisp()
-    _say(f"append every bf16 value fmt={fmt}")
+    _say(f"append every bf16 value fmt={fmt} rows a call={rows_a_call}")
     bits = np.arange(1 << 15).reshape(-1, 64)
     bits = np.concatenate([bits, bits | 0x8000], 1).astype(np.uint16)  # [512, 128]
     x = torch.from_numpy(bits.view(np.int16)).view(torch.bfloat16)[None]
     table = np.arange(8, dtype=np.int32)[None]
     for rows in (x, x[:, torch.randperm(512, generator=torch.Generator().manual_seed(1))]):
         c, oracle = _new(C, 8, 1, 64, fmt)
-        _append(C, c, oracle, table, [0], [512], rows, -rows)
+        for i in range(0, 512, rows_a_call):
+            _append(C, c, oracle, table, [i], [rows_a_call], rows[:, i:i + rows_a_call], -rows[:, i:i + rows_a_call])
         _check_written(c, oracle)
 
 
@@ -139,8 +141,9 @@ def test_append_token_by_token_with_growing_values(fmt):
             _check_written(c, oracle)
 
 
+@pytest.mark.parametrize("rows_a_call", [768, 3])
 @pytest.mark.parametrize("fmt", FORMATS)
-def test_append_extreme_values(fmt):
+def test_append_extreme_values(fmt, rows_a_call):
     """Zeros, the smallest and largest bf16, values under the smallest scale, infinities and NaN (which move no scale)."""
     C = _crisp()
     _say(f"append extremes fmt={fmt}")
@@ -162,7 +165,9 @@ def test_append_extreme_values(fmt):
     rows[0, 704:] = torch.randn(64, 128) * 2.0 ** 100
     rows = rows.to(torch.bfloat16)
     c, oracle = _new(C, 12, 1, 64, fmt)
-    _append(C, c, oracle, np.arange(12, dtype=np.int32)[::-1][None].copy(), [0], [768], rows, rows)
+    table = np.arange(12, dtype=np.int32)[::-1][None].copy()
+    for i in range(0, 768, rows_a_call):
+        _append(C, c, oracle, table, [i], [rows_a_call], rows[:, i:i + rows_a_call], rows[:, i:i + rows_a_call])
     _check_written(c, oracle)
 
 
@@ -356,6 +361,31 @@ def test_malformed_offsets_stay_inside():
     ref = np.array([0, 2, 2, 2, 10])  # sequence 1 falls: none; sequence 3: rows 1 .. 10, written after or before 0's
     want, tol = oracle.attention(table, np.array([63, 0, 63, 127]), ref, to_f64(q), 1 / math.sqrt(128))
     assert (np.abs(to_f64(out[:, :1]) - want[:, :1]) <= tol[:, :1]).all()
+
+
+def test_offsets_past_32_bits():
+    """A cache of 6 GB: pages past 2^31 and 2^32 bytes, appended to, attended to (by one row and by many) and copied."""
+    C = _crisp()
+    _say("offsets past 32 bits")
+    n_pages = 200_000
+    c = C.make_cache(n_pages, 2, 64, O.E4M3, DEV)
+    assert c.pages.numel() > 6 << 30
+    rows = 330
+    at = np.array([n_pages - 1, 140_000, 65_536, 131_072, 7, n_pages - 2])
+    oracle = O.Cache(6, 2, 64, O.E4M3)
+    local, table = np.arange(6, dtype=np.int32)[None], at.astype(np.int32)[None]
+    k, v, q = _rand(2, rows, 1), _rand(2, rows, 2), _rand(4, rows, 3)
+    ptr = _ptr([rows])
+    C.crisp_cache_append(c, _ints(table), _ints([0]), _ints(ptr), k.to(DEV), v.to(DEV))
+    oracle.append(local, [0], ptr, to_f64(k), to_f64(v))
+    for n in (rows, 1):
+        o = C.crisp_cache_attn(c, _ints(table), _ints([rows - n]), _ints([0, n]), q[:, :n].to(DEV))
+        want, tol = oracle.attention(local, [rows - n], [0, n], to_f64(q[:, :n]), 1 / math.sqrt(128))
+        assert (np.abs(to_f64(o) - want) <= tol).all()
+    moved = np.array([3, 150_000, 199_000, 5, 70_000, 196_000])
+    C.crisp_cache_copy(c, _ints(np.stack([at, moved], 1)))
+    for a, b in zip(at, moved):
+        assert torch.equal(c.pages[a], c.pages[b]) and torch.equal(c.scales[a], c.scales[b])
 
 
 # ------------------------------------------------------------------ the two together
