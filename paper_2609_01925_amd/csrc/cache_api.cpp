@@ -85,12 +85,17 @@ crisp_status check_seqs(const BatchDims& b, const int32_t* table, const int32_t*
   return check_ptr(row_ptr, 4, "row_ptr");
 }
 
-// An input may repeat a head or a row (stride 0); the rows of an output must be apart.
+// An input may repeat a head or a row (stride 0); an output's heads lie behind one another or between its rows.
 crisp_status check_strides(int64_t head, int64_t row, bool output, int heads, int rows, const char* name) {
   if (head < 0 || row < 0 || head % 8 || row % 8)
     return fail(CRISP_EINVAL, "%s: strides (%lld, %lld) must be multiples of 8 elements and >= 0", name,
                 (long long)head, (long long)row);
-  if (output && ((heads > 1 && head < kHeadDim) || (rows > 1 && row < kHeadDim)))
+  const auto apart = [](int64_t stride, int64_t n, int64_t inner) {  // stride >= inner's n pieces and the last one's 128
+    return n < 1 || (stride >= kHeadDim && (stride - kHeadDim) / n >= inner);
+  };
+  if (output && !(heads > 1 ? rows > 1 ? (row >= kHeadDim && apart(head, rows - 1, row)) || (head >= kHeadDim && apart(row, heads - 1, head))
+                                       : head >= kHeadDim
+                            : rows <= 1 || row >= kHeadDim))
     return fail(CRISP_EINVAL, "%s: strides (%lld, %lld) overlap its rows", name, (long long)head, (long long)row);
   return CRISP_OK;
 }

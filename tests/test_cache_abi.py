@@ -73,6 +73,14 @@ def test_bad_strides_heads_and_scales():
         assert _attn(scale=bad) == C.CRISP_EINVAL
 
 
+@pytest.mark.parametrize("head,row,apart", [(384, 128, True), (128, 512, True), (128, 128, False), (376, 128, False),
+                                            (128, 504, False), (200, 136, False), (400, 136, True), (136, 536, True)])
+def test_output_rows_must_be_apart(head, row, apart):
+    """Four heads of three rows: one stride covers the extent that the other makes."""
+    assert _attn(oh=head, orow=row, wsb=16) == C.CRISP_EINVAL
+    assert (b"too small" if apart else b"overlap") in C.lib.crisp_last_error()
+
+
 def test_nothing_to_do_needs_no_buffers():
     none = dict(p=None, s=None, t=None, n=None, r=None)
     for b in ((0, 4, 3), (2, 4, 0)):
