@@ -32,7 +32,7 @@ class KVCache:
         dev = self.pool.device
         self.table = torch.full((max_seqs, -(-max_tokens // block)), -1, dtype=torch.int32, device=dev)
         self.seq_len = torch.zeros(max_seqs, dtype=torch.int32, device=dev)
-        self._row = torch.arange(max_seqs + 1, dtype=torch.int32, device=dev)
+        self._all = torch.arange(2, dtype=torch.int32, device=dev)  # times n: row_ptr of n rows of one sequence
 
     def reserve(self, counts: torch.Tensor) -> torch.Tensor:
         """Pages for counts[s] (int32 [max_seqs]) more tokens of each sequence -> granted: counts[s], or 0 where the
@@ -46,12 +46,9 @@ class KVCache:
         if not 0 <= seq < self.table.shape[0]:
             raise ValueError(f"sequence {seq} outside [0, {self.table.shape[0]})")
         o = C.crisp_prefill_attn(q, k, v, C.make_params() if params is None else params)
-        C.crisp_cache_append(self.layers[layer], self.table, self.seq_len, self.rows_of(seq, k.shape[1]), k, v)
+        C.crisp_cache_append(self.layers[layer], self.table[seq:seq + 1], self.seq_len[seq:seq + 1],
+                             self._all * k.shape[1], k, v)
         return o
-
-    def rows_of(self, seq: int, n: int) -> torch.Tensor:
-        """row_ptr of a call whose n rows are all sequence seq's."""
-        return (self._row > seq).to(torch.int32) * n
 
     def attend(self, layer: int, row_ptr: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                softmax_scale: float = 0.0, ws: Optional[torch.Tensor] = None,

@@ -57,60 +57,25 @@ __device__ __forceinline__ u32x4 rescale(u32x4 x, float f) {
   return x;
 }
 
-// One workgroup, 256 threads a tile, writes the call's rows into one page of one KV head: it reads them once,
-// takes the scale from their largest magnitude (and from the scale of the tokens that the page holds
-// already, which never shrinks), lays the codes out in LDS in the tile's order and stores whole
+template <int TILES>
+struct PageLds {
+  __attribute__((aligned(16))) char stage[2 * TILES * kTileLds];
+  uint32_t amax[2][2][4 * TILES];
+};
+
+// One workgroup, 256 threads a tile, writes the rows r of sequence seq that go into its page `slot`, one KV head: it reads
+// them once, takes the scale from their largest magnitude (and from the scale of the tokens that the page
+// holds already, which never shrinks), lays the codes out in LDS in the tile's order and stores whole
 // chunks.  A chunk of V holds 16 tokens of one element, so one that is only partly new is read,
 // merged and written back by its thread; a page whose scale grew has its other codes rounded
 // again.  Bound by HBM on long appends (512 bytes read and 256 written a token and head), by
-// the chain lengths -> rows -> scale -> codes on single tokens; the look-up of the page runs beside the rows'.
+// the chain lengths -> rows -> scale -> codes on short ones; the look-up of the page runs beside the rows'.
 template <int FMT, int TILES>
-__global__ __launch_bounds__(256 * TILES) void cache_append(AppendArgs a) {
+__device__ __forceinline__ void append_page(const AppendArgs& a, const SeqRows& r, int seq, int slot, int head, PageLds<TILES>& l) {
   constexpr int B = TILES * kTile, kThreads = 256 * TILES, kW = kThreads / kWave;
-  __shared__ __attribute__((aligned(16))) char stage[2 * TILES * kTileLds];
-  __shared__ int wsum[kW], at[2];
-  __shared__ uint32_t amax[2][2][kW];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  // which page of which sequence: the blockIdx.x-th one that the call writes to.  Up to 64 sequences
-  // every wave looks them over, one a lane; more are counted by the workgroup.
-  SeqRows r;
-  int seq, slot;
-  const int item = blockIdx.x;
-  if (a.b.n_seqs <= kWave) {
-    SeqRows mine = {0, 0, 0};
-    if (lane < a.b.n_seqs) mine = seq_rows(a.s, a.b, B, lane);
-    const int cnt = pages_touched(mine, B), end = wave_scan(cnt);
-    const unsigned long long past = __ballot(item < end);
-    if (past == 0) return;
-    seq = __builtin_ctzll(past);
-    r = SeqRows{__builtin_amdgcn_readlane(mine.len, seq), __builtin_amdgcn_readlane(mine.row0, seq), __builtin_amdgcn_readlane(mine.n, seq)};
-    slot = r.len / B + item - __builtin_amdgcn_readlane(end - cnt, seq);
-  } else {
-    if (tid == 0) at[0] = -1;
-    int before = 0;
-    for (int s0 = 0; s0 < a.b.n_seqs; s0 += kThreads) {
-      const int s = s0 + tid;
-      int cnt = 0;
-      if (s < a.b.n_seqs) cnt = pages_touched(seq_rows(a.s, a.b, B, s), B);
-      int total;
-      __syncthreads();
-      const int end = before + block_scan<int, kW>(cnt, wsum, &total);
-      if (item >= end - cnt && item < end) {
-        at[0] = s;
-        at[1] = item - (end - cnt);
-      }
-      before += total;
-      if (item < before) break;  // the same on every thread
-    }
-    __syncthreads();
-    seq = __builtin_amdgcn_readfirstlane(at[0]);
-    if (seq < 0) return;
-    r = seq_rows(a.s, a.b, B, seq);
-    slot = r.len / B + at[1];
-  }
   const int first = slot * B;                                              // position of the page's first token
   const int t0 = max(r.len - first, 0), t1 = min(r.len + r.n - first, B);  // the call's tokens in the page
-  const int head = blockIdx.y;
   const int row0 = r.row0 + first - r.len;  // the call's row of token 0 (before its first, if t0 > 0)
   const uint16_t* src[2] = {a.k + head * a.ks.head, a.v + head * a.vs.head};
   const int64_t rs[2] = {a.ks.row, a.vs.row};
@@ -137,7 +102,7 @@ __global__ __launch_bounds__(256 * TILES) void cache_append(AppendArgs a) {
       for (int i = 0; i < 4; ++i) m = of(raw[x][i], m);
       m = max(m & 0xffffu, m >> 16);
       m = wave_reduce(m, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
-      if (lane == 0) amax[turn][x][w] = m;
+      if (lane == 0) l.amax[turn][x][w] = m;
     }
     __syncthreads();
   };
@@ -145,9 +110,9 @@ __global__ __launch_bounds__(256 * TILES) void cache_append(AppendArgs a) {
   const auto tops = [&](int turn) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      uint32_t m = amax[turn][x][0];
+      uint32_t m = l.amax[turn][x][0];
 #pragma unroll
-      for (int i = 1; i < kW; ++i) m = max(m, amax[turn][x][i]);
+      for (int i = 1; i < kW; ++i) m = max(m, l.amax[turn][x][i]);
       top[x] = (int)m;
     }
   };
@@ -190,8 +155,8 @@ __global__ __launch_bounds__(256 * TILES) void cache_append(AppendArgs a) {
       }
     }
   {
-    char* kt = stage + tl * kTileLds;
-    char* vt = stage + (TILES + tl) * kTileLds;
+    char* kt = l.stage + tl * kTileLds;
+    char* vt = l.stage + (TILES + tl) * kTileLds;
     const int q = (tid >> 4) & 3, w4 = w & 3;
     // K: token 16 w4 + 4 q + i is row r = 4 w4 + i of score tile q; elements d0.. are half of a chunk
     const int kc = ((q * 2 + ((d0 >> 4) & 1)) * 4 + (d0 >> 5)) * 16 + 4 * w4;
@@ -220,12 +185,12 @@ __global__ __launch_bounds__(256 * TILES) void cache_append(AppendArgs a) {
     const int rr = ch & 15, g = (ch >> 4) & 3;
     const int tk = td * kTile + 16 * (rr >> 2) + 4 * (ch >> 7) + (rr & 3);
     if (tk >= t0 && tk < t1)
-      *kd = *reinterpret_cast<const u32x4*>(stage + td * kTileLds + lds_chunk(ch));
+      *kd = *reinterpret_cast<const u32x4*>(l.stage + td * kTileLds + lds_chunk(ch));
     else if (down[0] != 1.f)
       *kd = rescale<FMT>(*kd, down[0]);
     const int tv = td * kTile + 16 * g;
     const int lo = max(t0 - tv, 0), hi = min(t1 - tv, 16);  // new tokens of this chunk
-    u32x4 y = *reinterpret_cast<const u32x4*>(stage + (TILES + td) * kTileLds + lds_chunk(ch));
+    u32x4 y = *reinterpret_cast<const u32x4*>(l.stage + (TILES + td) * kTileLds + lds_chunk(ch));
     if (lo == 0 && hi == 16) {
       *vd = y;
     } else if (hi > lo || down[1] != 1.f) {
@@ -243,45 +208,69 @@ __global__ __launch_bounds__(256 * TILES) void cache_append(AppendArgs a) {
   }
 }
 
-// A wave takes a row and KV head: if the row is the first that the call writes to its page, all of them there (one, in a
-// decoding step).  A lane holds two elements; codes go out as they are, two bytes of K and a byte each of two of V's
-// chunks, since what lies beside them is only touched where a scale grows.  No LDS and no barrier: the
-// general kernel's chain without its waits, and a quarter of a workgroup a head.
-template <int FMT>
-__global__ __launch_bounds__(4 * kWave) void cache_append_few(AppendArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = (int)(wave / a.c.hkv), head = (int)(wave % a.c.hkv), B = a.c.B;
-  if (row >= a.b.n_rows) return;
-  // the row's sequence: among up to 64 the one that has it, among more the last that begins at or before it,
-  // looked for 64 at a time
-  int seq = 0;
+// The page of blockIdx.x: the so-many-th one that the call writes to.  Up to 64 sequences every wave looks them
+// over, one a lane; more are counted by the workgroup.
+template <int FMT, int TILES>
+__global__ __launch_bounds__(256 * TILES) void cache_append(AppendArgs a) {
+  constexpr int B = TILES * kTile, kThreads = 256 * TILES, kW = kThreads / kWave;
+  __shared__ PageLds<TILES> l;
+  __shared__ int wsum[kW], at[2];
+  const int tid = threadIdx.x, lane = tid & 63;
+  SeqRows r;
+  int seq, slot;
+  const int item = blockIdx.x;
   if (a.b.n_seqs <= kWave) {
-    bool has = false;
-    if (lane < a.b.n_seqs) {
-      const SeqRows x = seq_rows(a.s, a.b, B, lane);
-      has = row >= x.row0 && row < x.row0 + x.n;
-    }
-    const unsigned long long found = __ballot(has);
-    if (found == 0) return;
-    seq = __builtin_ctzll(found);
+    SeqRows mine = {0, 0, 0};
+    if (lane < a.b.n_seqs) mine = seq_rows(a.s, a.b, B, lane);
+    const int cnt = pages_touched(mine, B), end = wave_scan(cnt);
+    const unsigned long long past = __ballot(item < end);
+    if (past == 0) return;
+    seq = __builtin_ctzll(past);
+    r = SeqRows{__builtin_amdgcn_readlane(mine.len, seq), __builtin_amdgcn_readlane(mine.row0, seq), __builtin_amdgcn_readlane(mine.n, seq)};
+    slot = r.len / B + item - __builtin_amdgcn_readlane(end - cnt, seq);
   } else {
-    for (int n = a.b.n_seqs; n > 1;) {
-      const int step = (n + kWave - 1) / kWave, probe = lane * step;
-      const unsigned long long ok = __ballot(probe < n && a.s.row_ptr[seq + min(probe, n - 1)] <= row);
-      const int k = max(__popcll(ok) - 1, 0);
-      seq += k * step;
-      n = min(step, n - k * step);
+    if (tid == 0) at[0] = -1;
+    int before = 0;
+    for (int s0 = 0; s0 < a.b.n_seqs; s0 += kThreads) {
+      const int s = s0 + tid;
+      int cnt = 0;
+      if (s < a.b.n_seqs) cnt = pages_touched(seq_rows(a.s, a.b, B, s), B);
+      int total;
+      __syncthreads();
+      const int end = before + block_scan<int, kW>(cnt, wsum, &total);
+      if (item >= end - cnt && item < end) {
+        at[0] = s;
+        at[1] = item - (end - cnt);
+      }
+      before += total;
+      if (item < before) break;  // the same on every thread
     }
+    __syncthreads();
+    seq = __builtin_amdgcn_readfirstlane(at[0]);
+    if (seq < 0) return;
+    r = seq_rows(a.s, a.b, B, seq);
+    slot = r.len / B + at[1];
   }
-  const SeqRows r = seq_rows(a.s, a.b, B, seq);
-  const int i = row - r.row0, pos = r.len + i, t0 = pos % B;
-  if (i < 0 || i >= r.n || (i > 0 && t0 != 0)) return;
-  const int n = min(r.n - i, B - t0), slot = pos / B;
-  const int page = slot < a.b.max_pages ? a.s.table[(int64_t)seq * a.b.max_pages + slot] : -1;
+  append_page<FMT, TILES>(a, r, seq, slot, blockIdx.y, l);
+}
+
+// The n <= kFewRows rows from row `row` on that the call writes to a page, its token t0 first, by one wave.  A lane holds two
+// elements; codes go out as they are, two bytes of K and a byte each of two of V's chunks, since what lies beside
+// them is only touched where a scale grows.  No LDS and no barrier: the page's chain without its waits.
+constexpr int kFewRows = 3;
+template <int FMT>
+__device__ __forceinline__ void append_rows(const AppendArgs& a, int row, int n, int t0, int page, int head) {
+  const int lane = threadIdx.x & 63, B = a.c.B;
   const uint16_t* src[2] = {a.k + head * a.ks.head + row * a.ks.row + 2 * lane, a.v + head * a.vs.head + row * a.vs.row + 2 * lane};
   const int64_t rs[2] = {a.ks.row, a.vs.row};
-  uint32_t x[2] = {*reinterpret_cast<const uint32_t*>(src[0]), *reinterpret_cast<const uint32_t*>(src[1])};
+  uint32_t x[2][kFewRows];
+#pragma unroll
+  for (int j = 0; j < kFewRows; ++j)
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      x[y][j] = 0;
+      if (j < n) x[y][j] = *reinterpret_cast<const uint32_t*>(src[y] + j * rs[y]);
+    }
   if (page < 0 || page >= a.c.n_pages) return;
   float* scale = a.scales + ((int64_t)page * a.c.hkv + head) * 2;
   uint8_t* dst = a.pages + ((int64_t)page * a.c.hkv + head) * (2 * (int64_t)B * kHeadDim);
@@ -289,11 +278,9 @@ __global__ __launch_bounds__(4 * kWave) void cache_append_few(AppendArgs a) {
   float inv[2];
 #pragma unroll
   for (int y = 0; y < 2; ++y) {
-    uint32_t m = max(finite(x[y] & 0x7fffu), finite((x[y] >> 16) & 0x7fffu));
-    for (int j = 1; j < n; ++j) {
-      const uint32_t z = *reinterpret_cast<const uint32_t*>(src[y] + j * rs[y]);
-      m = max(m, max(finite(z & 0x7fffu), finite((z >> 16) & 0x7fffu)));
-    }
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < kFewRows; ++j) m = max(m, max(finite(x[y][j] & 0x7fffu), finite((x[y][j] >> 16) & 0x7fffu)));
     m = wave_reduce(m, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
     int e = scale_exp<FMT>((int)m);
     if (t0 > 0) {
@@ -312,20 +299,65 @@ __global__ __launch_bounds__(4 * kWave) void cache_append_few(AppendArgs a) {
     inv[y] = pow2f(-e);
   }
   const int e0 = 2 * lane;
-  for (int j = 0; j < n; ++j) {
-    if (j > 0)
 #pragma unroll
-      for (int y = 0; y < 2; ++y) x[y] = *reinterpret_cast<const uint32_t*>(src[y] + j * rs[y]);
+  for (int j = 0; j < kFewRows; ++j) {
+    if (j >= n) break;
     uint32_t c[2];
 #pragma unroll
     for (int y = 0; y < 2; ++y)
-      c[y] = to_codes<FMT>(__uint_as_float(x[y] << 16) * inv[y], __uint_as_float(x[y] & 0xffff0000u) * inv[y], 0.f, 0.f);
+      c[y] = to_codes<FMT>(__uint_as_float(x[y][j] << 16) * inv[y], __uint_as_float(x[y][j] & 0xffff0000u) * inv[y], 0.f, 0.f);
     const int t = (t0 + j) % kTile;
     uint8_t* tile = dst + (t0 + j) / kTile * (2 * kTileBytes);
     *reinterpret_cast<uint16_t*>(tile + ((t / 4 % 4 * 2 + e0 / 16 % 2) * 64 + e0 / 32 * 16 + t / 16 * 4 + t % 4) * 16 + e0 % 16) = (uint16_t)c[0];
     uint8_t* v = tile + kTileBytes + (e0 / 16 * 64 + t / 16 * 16 + e0 % 16) * 16 + t % 16;
     v[0] = (uint8_t)c[1];
     v[16] = (uint8_t)(c[1] >> 8);
+  }
+}
+
+// A wave looks at one row: if it is the first that the call writes to its page and few follow there, the wave writes them;
+// pages with more are then written by the workgroup, one after the other.
+template <int FMT, int TILES>
+__global__ __launch_bounds__(256 * TILES) void cache_append_few(AppendArgs a) {
+  constexpr int B = TILES * kTile, kW = 4 * TILES;
+  __shared__ PageLds<TILES> l;
+  __shared__ int seqs[kW], slots[kW];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = (int)blockIdx.x * kW + w, head = blockIdx.y;
+  // the row's sequence: among up to 64 the one that has it, among more the last that begins at or before it,
+  // looked for 64 at a time
+  int seq = 0;
+  SeqRows r{0, 0, 0};
+  if (a.b.n_seqs <= kWave) {
+    SeqRows x{0, 0, 0};
+    if (lane < a.b.n_seqs) x = seq_rows(a.s, a.b, B, lane);
+    const unsigned long long found = __ballot(row >= x.row0 && row < x.row0 + x.n);
+    if (found != 0) {
+      seq = __builtin_ctzll(found);
+      r = SeqRows{__builtin_amdgcn_readlane(x.len, seq), __builtin_amdgcn_readlane(x.row0, seq), __builtin_amdgcn_readlane(x.n, seq)};
+    }
+  } else {
+    for (int n = a.b.n_seqs; n > 1;) {
+      const int step = (n + kWave - 1) / kWave, probe = lane * step;
+      const unsigned long long ok = __ballot(probe < n && a.s.row_ptr[seq + min(probe, n - 1)] <= row);
+      const int k = max(__popcll(ok) - 1, 0);
+      seq += k * step;
+      n = min(step, n - k * step);
+    }
+    r = seq_rows(a.s, a.b, B, seq);
+  }
+  const int i = row - r.row0, pos = r.len + i, t0 = pos % B, slot = pos / B;
+  const int n = i >= 0 && i < r.n && (i == 0 || t0 == 0) ? min(r.n - i, B - t0) : 0;  // rows of a page that begins here
+  if (lane == 0) {
+    seqs[w] = n > kFewRows ? seq : -1;
+    slots[w] = slot;
+  }
+  __syncthreads();
+  if (n > 0 && n <= kFewRows)
+    append_rows<FMT>(a, row, n, t0, slot < a.b.max_pages ? a.s.table[(int64_t)seq * a.b.max_pages + slot] : -1, head);
+  for (int x = 0; x < kW; ++x) {
+    const int s = __builtin_amdgcn_readfirstlane(seqs[x]);
+    if (s >= 0) append_page<FMT, TILES>(a, seq_rows(a.s, a.b, B, s), s, __builtin_amdgcn_readfirstlane(slots[x]), head, l);
   }
 }
 
@@ -361,11 +393,19 @@ hipError_t launch_cache_append(const CacheDims& c, const BatchDims& b, const Seq
   // Few rows a sequence: a wave for each row and head.  8 heads, e4m3, the page kernel / this one, us: 64 sequences of one row
   // 5.7 / 3.9, of 2.8 on average 6.8 / 6.4, of 4.0 7.0 / 7.8; past 64 sequences, which the page kernel has to count, 1000
   // of one 37.3 / 10.3, of 4.5 57.1 / 30.2; 4000 of one 201 / 27.3.
-  if (b.n_rows <= (b.n_seqs <= kWave ? 3 : 8) * (int64_t)b.n_seqs) {
-    const int64_t waves = (int64_t)b.n_rows * c.hkv;
-    const dim3 few((unsigned)((waves + 3) / 4));
-    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((cache_append_few<kCacheE4M3>), few, dim3(4 * kWave), 0, stream, a);
-    else hipLaunchKernelGGL((cache_append_few<kCacheInt8>), few, dim3(4 * kWave), 0, stream, a);
+  // Few rows a sequence on average: no list of pages is needed, a wave looks at each row.  8 heads, e4m3, the page kernel / this
+  // one, us: 256 sequences of one row 10.6 / 7.6, of 4 13.4 / 13.4, of 8 13.3 / 20.9, 255 of one and one of 512 13.6 / 11.0, one of
+  // 2000 7.9 / 14.3; past that the page kernel has to count for long: 1000 of one 38.5 / 11.2, of 4.5 56.1 / 39.7, of 10 62.5 / 62.7;
+  // 4000 of one 221 / 29.1, of 5 390 / 145.
+  if (b.n_rows <= (b.n_seqs <= 512 ? 3 : 8) * (int64_t)b.n_seqs) {
+    const dim3 few((unsigned)((b.n_rows + 4 * c.tiles - 1) / (4 * c.tiles)), (unsigned)c.hkv);
+    if (c.fmt == kCacheE4M3) {
+      if (c.tiles == 1) hipLaunchKernelGGL((cache_append_few<kCacheE4M3, 1>), few, dim3(256), 0, stream, a);
+      else hipLaunchKernelGGL((cache_append_few<kCacheE4M3, 2>), few, dim3(512), 0, stream, a);
+    } else {
+      if (c.tiles == 1) hipLaunchKernelGGL((cache_append_few<kCacheInt8, 1>), few, dim3(256), 0, stream, a);
+      else hipLaunchKernelGGL((cache_append_few<kCacheInt8, 2>), few, dim3(512), 0, stream, a);
+    }
     return hipGetLastError();
   }
   // a sequence's n rows touch at most (n - 1) / B + 2 pages, and at most n

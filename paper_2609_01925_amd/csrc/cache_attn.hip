@@ -191,7 +191,7 @@ struct TileList {
       todo = __ballot(ok);
       if (ok) {
         const float* sc = a.scales + ((int64_t)pg * a.c.hkv + head) * 2;
-        kc = pow2f(stored_exp(sc[0])) * a.c2;
+        kc = fmaxf(pow2f(stored_exp(sc[0])) * a.c2, 1.17549435e-38f);  // not 0, which a masked -inf must not meet
         ev = stored_exp(sc[1]);
       }
     }

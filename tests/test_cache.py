@@ -127,6 +127,25 @@ def test_append_ragged_in_steps(fmt, block):
         _check_written(c, oracle)
 
 
+@pytest.mark.parametrize("n_seqs,long", [(20, 41), (64, 129), (70, 141), (520, 700)])
+@pytest.mark.parametrize("fmt,block", [(O.E4M3, 128), (O.INT8, 64)])
+def test_append_short_and_long_together(fmt, block, n_seqs, long):
+    """A batch of single rows with one chunk among them, some without a row, some in a page's last place, a few of
+    two to five rows: the pages written by a wave and by a workgroup in one call, up to 64 sequences and past them."""
+    C = _crisp()
+    _say(f"append short and long fmt={fmt} block={block} sequences={n_seqs} long={long}")
+    rng = np.random.default_rng(n_seqs + fmt)
+    counts = rng.choice([0, 1, 1, 1, 1, 2, 5], n_seqs)
+    counts[n_seqs // 3], counts[n_seqs // 3 + 1] = long, 4
+    first = rng.integers(1, block + 1, n_seqs)
+    first[::7] = block - 1
+    table, n_pages = _table(first + counts, block, rng)
+    c, oracle = _new(C, n_pages, 2, block, fmt)
+    _append(C, c, oracle, table, 0 * first, first, _rand(2, first.sum(), 1), _rand(2, first.sum(), 2))
+    _append(C, c, oracle, table, first, counts, _rand(2, counts.sum(), 3, 1.6), _rand(2, counts.sum(), 4, 0.5))
+    _check_written(c, oracle)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_append_token_by_token_with_growing_values(fmt):
     """A page filled one token at a time, each larger than all before; then past it."""
@@ -303,6 +322,17 @@ def test_peaked_scores_and_scales_far_apart():
     q[:, 5] = 0
     _check_attn(C, c, oracle, table, lens, counts, q, scale=0.5)
     _check_attn(C, c, oracle, table, lens, counts, q)
+
+
+@pytest.mark.parametrize("rows", [1, 70])
+def test_scales_that_vanish(rows):
+    """A softmax_scale whose products are 0 in 32 bits: every token that a row sees has the same weight, the others none."""
+    C = _crisp()
+    _say(f"vanishing scale rows={rows}")
+    table, n_pages = _table([30 + rows], 64, np.random.default_rng(3))
+    c, oracle = _new(C, n_pages, 1, 64, O.E4M3)
+    _append(C, c, oracle, table, [0], [30 + rows], _rand(1, 30 + rows, 1, 1e-18), _rand(1, 30 + rows, 2))
+    _check_attn(C, c, oracle, table, [30], [rows], _rand(2, rows, 3), scale=1e-42)
 
 
 def test_holes_and_rows_that_see_nothing():
