@@ -274,6 +274,21 @@ def test_rows_of_different_counts(fmt, counts):
     _check_attn(C, c, oracle, table, lens, counts, _rand(6, sum(counts), 5))
 
 
+@pytest.mark.parametrize("hq,hkv", [(4, 2), (7, 1), (3, 3)])
+def test_long_chunks_with_and_without_history(hq, hkv):
+    """Chunks whose last rows see several times what the first ones do, beside one with a long history: odd and even
+    numbers of row groups, cut between workgroups and whole."""
+    C = _crisp()
+    _say(f"long chunks heads={hq}/{hkv}")
+    rng = np.random.default_rng(hq)
+    lens, counts = np.array([0, 5, 900, 64, 0]), np.array([1100, 0, 140, 333, 260])
+    table, n_pages = _table(lens + counts, 128, rng)
+    c, oracle = _new(C, n_pages, hkv, 128, O.E4M3)
+    _append(C, c, oracle, table, 0 * lens, lens, _rand(hkv, lens.sum(), 1), _rand(hkv, lens.sum(), 2))
+    _append(C, c, oracle, table, lens, counts, _rand(hkv, counts.sum(), 3), _rand(hkv, counts.sum(), 4))
+    _check_attn(C, c, oracle, table, lens, counts, _rand(hq, counts.sum(), 5))
+
+
 @pytest.mark.parametrize("fmt,rows,hq", [(O.E4M3, 1, 4), (O.INT8, 1, 1), (O.E4M3, 33, 4)])
 def test_long_sequence_is_split(fmt, rows, hq):
     """One sequence of 20000 tokens cut over many workgroups, one KV head, beside a short one."""
