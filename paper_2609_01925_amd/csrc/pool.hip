@@ -22,6 +22,7 @@ constexpr int kBuf = 4096;  // free pages collected at a time
 // 11.6 / 13.3; 512 18.1 / 17.0 and 12.8 / 16.7; 1024 18.0 / 27.1 and 15.0 / 26.6.
 constexpr int64_t kShareHere = 4096;
 constexpr int kPerThread = kPoolMaxSeqs / kThreads;
+constexpr int kMostFree = 1 << 16;  // workgroups of a free; each takes every so-many-th sequence
 static_assert(kPoolMaxSeqs <= kBuf, "a fork collects its pages at once");
 
 __device__ __forceinline__ uint32_t* bits_of(int32_t* pool, int n_pages) { return reinterpret_cast<uint32_t*>(pool + n_pages); }
@@ -362,19 +363,21 @@ __global__ __launch_bounds__(256) void pool_share(int n_pages, int B, int max_pa
 // Every page in the row of a freed sequence loses one use.  The exchange gives each page to one
 // thread, also where a sequence is listed twice.
 __global__ __launch_bounds__(256) void pool_free(int n_pages, int n_seqs, int max_pages, int32_t* pool, int32_t* table,
-                                                 int32_t* seq_len, const int32_t* ids) {
-  const int s = ids[blockIdx.x];
-  if (s < 0 || s >= n_seqs) return;
+                                                 int32_t* seq_len, const int32_t* ids, int n) {
   uint32_t* bits = bits_of(pool, n_pages);
-  int32_t* row = table + (int64_t)s * max_pages;
-  for (int j = threadIdx.x; j < max_pages; j += 256) {
-    const int p = atomicExch(row + j, -1);
-    if (p < 0 || p >= n_pages) continue;
-    const int before = atomicSub(pool + p, 1);
-    if (before == 1) atomicAnd(bits + (p >> 5), ~(1u << (p & 31)));
-    if (before <= 0) atomicAdd(pool + p, 1);  // not in use: nothing to take away
+  for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+    const int s = ids[i];
+    if (s < 0 || s >= n_seqs) continue;
+    int32_t* row = table + (int64_t)s * max_pages;
+    for (int j = threadIdx.x; j < max_pages; j += 256) {
+      const int p = atomicExch(row + j, -1);
+      if (p < 0 || p >= n_pages) continue;
+      const int before = atomicSub(pool + p, 1);
+      if (before == 1) atomicAnd(bits + (p >> 5), ~(1u << (p & 31)));
+      if (before <= 0) atomicAdd(pool + p, 1);  // not in use: nothing to take away
+    }
+    if (threadIdx.x == 0) seq_len[s] = 0;
   }
-  if (threadIdx.x == 0) seq_len[s] = 0;
 }
 
 // With U pages in use, the k-th free page below U takes the k-th page in use from U on.  Sources and
@@ -465,8 +468,8 @@ hipError_t launch_pool_fork(int n_pages, int block, int n_seqs, int max_pages, i
 
 hipError_t launch_pool_free(int n_pages, int n_seqs, int max_pages, int32_t* pool, int32_t* table, int32_t* seq_len,
                             const int32_t* ids, int n, hipStream_t stream) {
-  hipLaunchKernelGGL(pool_free, dim3((unsigned)n), dim3(256), 0, stream, n_pages, n_seqs, max_pages, pool, table,
-                     seq_len, ids);
+  hipLaunchKernelGGL(pool_free, dim3((unsigned)(n < kMostFree ? n : kMostFree)), dim3(256), 0, stream, n_pages, n_seqs,
+                     max_pages, pool, table, seq_len, ids, n);
   return hipGetLastError();
 }
 

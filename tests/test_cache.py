@@ -319,6 +319,26 @@ def test_many_sequences():
     _check_attn(C, c, oracle, table, lens, counts, _rand(2, counts.sum(), 5))
 
 
+@pytest.mark.parametrize("n_seqs", [5000, 70000])
+def test_very_many_sequences(n_seqs):
+    """Sequences of one token each, every ninth without a row: the result of a row that sees one token is its v, here
+    whole numbers that the codes hold exactly."""
+    C = _crisp()
+    _say(f"very many sequences n={n_seqs}")
+    c = C.make_cache(n_seqs, 1, 64, O.E4M3, DEV)
+    counts = np.ones(n_seqs, dtype=np.int64)
+    counts[::9] = 0
+    n = int(counts.sum())
+    g = torch.Generator().manual_seed(n_seqs)
+    k = torch.randn(1, n, 128, generator=g).to(torch.bfloat16).to(DEV)
+    v = torch.randint(-16, 17, (1, n, 128), generator=g).to(torch.bfloat16).to(DEV)
+    table = torch.randperm(n_seqs, generator=g).to(torch.int32)[:, None].to(DEV)
+    lens, ptr = torch.zeros(n_seqs, dtype=torch.int32, device=DEV), _ints(_ptr(counts))
+    C.crisp_cache_append(c, table, lens, ptr, k, v)
+    o = C.crisp_cache_attn(c, table, lens, ptr, k.expand(2, n, 128))
+    assert torch.equal(o, v.expand(2, n, 128))
+
+
 def test_peaked_scores_and_scales_far_apart():
     """Scores from far below to far above, pages whose scales are 2^40 apart, a given softmax scale."""
     C = _crisp()

@@ -108,6 +108,85 @@ def test_prompts_steps_forks_and_compaction(fmt, block):
     assert (kv.pool == 0).all() and (kv.table == -1).all() and (kv.seq_len == 0).all()
 
 
+def test_serving_loop_in_graphs():
+    """A step (reserve, append and attention of two layers, advance) and a turnover (free, fork with its page copies,
+    compaction) captured once each and replayed in turn with other counts and ids, beside the same calls made
+    eagerly on a second cache: equal outputs, pages, tables and pools after every replay."""
+    from paper_2609_01925_amd import crisp as C
+    from paper_2609_01925_amd.cache import KVCache
+    print("[gpu-case] serving loop in graphs", flush=True)
+    n, hq, hkv = 5, 4, 2
+    make = lambda: KVCache(2, 40, hkv, max_seqs=n, max_tokens=512, block=64, device=DEV)
+    rng = np.random.default_rng(1)
+    counts, ptr, rows = torch.zeros(n, dtype=torch.int32, device=DEV), torch.zeros(n + 1, dtype=torch.int32, device=DEV), 90
+    ids, src, dst = (torch.full((2,), -1, dtype=torch.int32, device=DEV) for _ in range(3))
+    q, k, v = (torch.zeros(2, h, rows, 128, dtype=torch.bfloat16, device=DEV) for h in (hq, hkv, hkv))
+    out = [torch.zeros(2, hq, rows, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+
+    def step(kv, o):
+        kv.reserve(counts)
+        for layer in range(2):
+            kv.attend(layer, ptr, q[layer], k[layer], v[layer], out=o[layer])
+        kv.advance(counts)
+
+    def turnover(kv):
+        kv.free(ids)
+        kv.fork(src, dst)
+        kv.compact()
+
+    eager, other = make(), make()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):  # nothing reserved, nothing forked: only what a first call loads
+        step(other, out[1])
+        turnover(other)
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    with torch.cuda.graph(graphs[0]):
+        step(other, out[1])
+    with torch.cuda.graph(graphs[1]):
+        turnover(other)
+    held = np.zeros(n, dtype=np.int64)
+    for i in range(8):
+        c = rng.integers(0, 18, n)
+        counts.copy_(_ints(c))
+        ptr.copy_(_ints(np.concatenate([[0], np.cumsum(c)])))
+        for x in (q, k, v):
+            x.copy_(torch.stack([_rand(x.shape[1], rows, 10 * i + j) for j in range(2)]))
+        torch.cuda.synchronize()
+        step(eager, out[0])
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        held += c
+        assert torch.equal(out[0], out[1]), i
+        gone = int(rng.integers(n))
+        parent = int(rng.choice([s for s in range(n) if s != gone]))
+        ids.copy_(_ints([gone, -1]))
+        src.copy_(_ints([parent, n]))
+        dst.copy_(_ints([gone, gone]))
+        torch.cuda.synchronize()
+        turnover(eager)
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        held[gone] = held[parent]
+        assert eager.seq_len.tolist() == held.tolist()
+        for x, y in ((eager.seq_len, other.seq_len), (eager.table, other.table), (eager.pool, other.pool)):
+            assert torch.equal(x, y), i
+        used = int((eager.pool[:40] > 0).sum())
+        assert 0 < used < 40
+        for a, b in zip(eager.layers, other.layers):
+            _same_tokens(eager, a, b, used)
+
+
+def _same_tokens(kv, a, b, used):
+    """Codes of the tokens held and scales of the pages in use, equal in two caches of one table."""
+    assert torch.equal(a.scales[:used], b.scales[:used])
+    table, x, y = kv.table.cpu().numpy(), O.decode(a.pages.cpu().numpy(), a.fmt), O.decode(b.pages.cpu().numpy(), b.fmt)
+    for s, n in enumerate(kv.seq_len.tolist()):
+        for j in range(-(-n // kv.block)):
+            t = min(n - j * kv.block, kv.block)
+            np.testing.assert_array_equal(x[table[s, j], :, :, :t], y[table[s, j], :, :, :t])
+
+
 def test_sequence_index_is_checked():
     from paper_2609_01925_amd.cache import KVCache
     kv = KVCache(1, 4, 1, max_seqs=2, max_tokens=128, device=DEV)
