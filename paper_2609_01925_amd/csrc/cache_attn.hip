@@ -311,7 +311,7 @@ __device__ __forceinline__ void softmax_step(const acc4 (&S)[C][4], float kc, in
 #pragma unroll
         for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S[c][ti][i]);
       mx = column(mx, [](float x, float y) { return fmaxf(x, y); }) * kc;
-      const float m = fmaxf(M[c], mx);
+      const float m = M[c] > mx ? M[c] : mx;  // NaN where every product is
       if (m != M[c]) {
         const float f = fast_exp2(M[c] - m);
         L[c] *= f;
@@ -678,7 +678,8 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
           for (int T = 0; T < 2; ++T)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, S[T][i]);
-          const float top = fmaxf(M, half_max(mx) * now.kc);
+          mx = half_max(mx) * now.kc;
+          const float top = M > mx ? M : mx;
           if (top != M) {
             const float f = fast_exp2(M - top);
             L *= f;

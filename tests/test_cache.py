@@ -389,6 +389,33 @@ def test_holes_and_rows_that_see_nothing():
     _check_attn(C, c, oracle, short, lens, counts, _rand(4, sum(counts), 6))
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("rows", [1, 9, 60])
+def test_queries_that_are_not_finite(rows, fmt):
+    """A NaN or an infinity in a query makes its row NaN, by the formula, and no other; a row that sees nothing stays 0."""
+    C = _crisp()
+    _say(f"queries that are not finite rows={rows} fmt={fmt}")
+    rng = np.random.default_rng(rows)
+    lens, counts = np.array([400, 0, 100]), np.array([rows] * 3)
+    table, n_pages = _table(lens + counts, 64, rng)
+    table[1] = -1  # sees nothing
+    c, oracle = _new(C, n_pages, 2, 64, fmt)
+    _append(C, c, oracle, table, 0 * lens, lens, _rand(2, lens.sum(), 1), _rand(2, lens.sum(), 2))
+    _append(C, c, oracle, table, lens, counts, _rand(2, counts.sum(), 3), _rand(2, counts.sum(), 4))
+    q = _rand(10, counts.sum(), 5)
+    bad = np.zeros((10, counts.sum()), dtype=bool)
+    for h, r, value in ((0, 0, math.nan), (3, 0, math.inf), (9, rows - 1, -math.inf), (4, 2 * rows, math.nan), (4, rows, math.nan)):
+        q[h, r, 7 * h % 128] = value
+        bad[h, r] = r // rows != 1
+    o = to_f64(C.crisp_cache_attn(c, _ints(table), _ints(lens), _ints(_ptr(counts)), q.to(DEV)))
+    q[torch.from_numpy(bad)] = 0
+    q[4, rows] = 0
+    want, tol = oracle.attention(table, lens, _ptr(counts), to_f64(q), 1 / math.sqrt(128))
+    assert np.isnan(o[bad]).all()
+    assert (np.abs(o - want)[~bad] <= tol[~bad]).all()
+    assert (o[:, rows:2 * rows] == 0).all()
+
+
 def test_padded_rows_are_left():
     """Rows behind the last sequence's keep what the output held; NaN in them and in dropped rows reaches nothing."""
     C = _crisp()
