@@ -532,6 +532,10 @@ __global__ __launch_bounds__(kFewWaves* kWave, 2) void cache_attn(AttnArgs a) {
 //   K: score tile T (32 keys), step (g, m): lane l takes chunk (t = 2 T + l % 32 / 16, half = h, g, r = l % 16), bytes
 //      8 m ..: key of row l % 32, elements 32 g + 16 h + 8 m + [0, 8).  The result's register i of a lane is key
 //      16 (2 q + h) + 4 (2 T + i / 8) + i % 4 with q = i / 4 % 2: 16 keys in a row for each q.
+//      e4m3 codes need no conversion: v_mfma_f32_32x32x64_f8f6f4 takes them as they are, 64 elements and so the chunks of two g
+//      at a time, and q comes as a sum of two e4m3 (split_row), which costs as many matrix cycles as bf16.  32 heads
+//      over 8, codes to bf16 / as they are, us: 8192 rows over no history 536 / 471 (1168 TFLOP/s), 16384 2070 / 1793, 1024
+//      over 15000 tokens 277 / 247, 2048 over 2048 119.5 / 107.7.
 //   V: output rows 32 D .., step (q, s): chunk (dt = 2 D + l % 32 / 16, g = 2 q + h, r = l % 16), bytes 8 s ..: those
 //      keys' 8 s + [0, 8), so that P again stays in its lane.
 constexpr int kRowWaves = 4, kRowUnit = 32 * kRowWaves;
@@ -541,11 +545,58 @@ typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 __device__ __forceinline__ u32x4 lds_chunk_at(int addr) { return *(const lds_u32x4*)(uint32_t)addr; }
 #endif
 
+typedef __attribute__((__vector_size__(8 * sizeof(int)))) int i32x8;
+
+// 32 x 32 products over 64 elements, e4m3 codes as they are; the second factor times 2^-5 if `second`.
+template <bool second>
+__device__ __forceinline__ f32x16 mfma32_codes(i32x8 a, i32x8 b, f32x16 c) {
+  return second ? __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 127, 0, 122)
+                : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+}
+
+// A row of q as two rows of e4m3, q = 2^e (a + 2^-5 b): its half of the 128 elements, Q[g] 16 of them, of a lane.  The
+// largest |q| lies in [2^7, 2^8) 2^e.  a is q rounded to four bits and b the rest, which has no more than four: nothing of a
+// bf16's eight is lost down to 2^-14 of the row's largest, below it no more than 2^-23 of that.  A row that
+// is not finite becomes NaN.  Returns 2^e.
+__device__ __forceinline__ float split_row(const bf16x8 (&Q)[4][2], i32x8 (&A)[2], i32x8 (&B)[2]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int g = 0; g < 4; ++g)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const u32x4 q = __builtin_bit_cast(u32x4, Q[g][x]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = max(m, max(q[i] & 0x7fffu, (q[i] >> 16) & 0x7fffu));
+    }
+  const auto r = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+  m = max(r[0], r[1]);
+  const int e = max((int)(m >> 7) - 127 - 7, -120);  // -120: q's own subnormals
+  const float inv = pow2f(-e);
+#pragma unroll
+  for (int g = 0; g < 4; ++g)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const u32x4 q = __builtin_bit_cast(u32x4, Q[g][i / 2]);
+      const uint32_t x = q[2 * (i & 1)], y = q[2 * (i & 1) + 1];
+      const f32x4 v = {__uint_as_float(x << 16) * inv, __uint_as_float(x & 0xffff0000u) * inv, __uint_as_float(y << 16) * inv,
+                       __uint_as_float(y & 0xffff0000u) * inv};
+      int a = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
+      a = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], a, true);
+      const f32x4 w = from_codes<kCacheE4M3>((uint32_t)a);
+      int b = __builtin_amdgcn_cvt_pk_fp8_f32(32.f * (v[0] - w[0]), 32.f * (v[1] - w[1]), 0, false);
+      b = __builtin_amdgcn_cvt_pk_fp8_f32(32.f * (v[2] - w[2]), 32.f * (v[3] - w[3]), b, true);
+      A[g / 2][4 * (g & 1) + i] = m < 0x7f80u ? a : 0x7f7f7f7f;
+      B[g / 2][4 * (g & 1) + i] = m < 0x7f80u ? b : 0;
+    }
+  return pow2f(e);
+}
+
 template <int FMT>
 __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int NW = kRowWaves, kRows = kRowUnit, kStages = 3;
   constexpr int kStage = 2 * kTileBytes;
+  constexpr bool kCodes = FMT == kCacheE4M3;
   __shared__ __attribute__((aligned(1024))) char ring[kStages * kStage];
   __shared__ int64_t lds[NW + 2];
   const int ring0 = __builtin_amdgcn_readfirstlane((int)(size_t)ring);
@@ -595,6 +646,9 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
         Q[g][m] = bf16x8{};
         if (r < rows) Q[g][m] = *reinterpret_cast<const bf16x8*>(a.q + q_at + 32 * g + 16 * h + 8 * m);
       }
+    i32x8 QA[2], QB[2];
+    float q_scale = 1.f;
+    if constexpr (kCodes) q_scale = split_row(Q, QA, QB);
     const int see_first = sw.r.len + r0 / a.G;
     const int see_last = sw.see_last(a, rt);
     f32x16 O[4];
@@ -630,12 +684,25 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = lds_chunk_at(k_at + stage * kStage + (i & 1) * 4096 + (i >> 1) * 256);
         f32x16 S[2] = {zero16(), zero16()};
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
+        if constexpr (kCodes) {
 #pragma unroll
           for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int T = 0; T < 2; ++T) S[T] = mfma32(codes_to_bf16<FMT>(x[2 * g + T][2 * m], x[2 * g + T][2 * m + 1]), Q[g][m], S[T]);
+            for (int T = 0; T < 2; ++T) {
+              const u32x4 u = x[4 * m + T], v = x[4 * m + 2 + T];
+              const i32x8 k = {(int)u[0], (int)u[1], (int)u[2], (int)u[3], (int)v[0], (int)v[1], (int)v[2], (int)v[3]};
+              S[T] = mfma32_codes<false>(k, QA[m], S[T]);
+              S[T] = mfma32_codes<true>(k, QB[m], S[T]);
+            }
+        } else {
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+              for (int T = 0; T < 2; ++T) S[T] = mfma32(codes_to_bf16<FMT>(x[2 * g + T][2 * m], x[2 * g + T][2 * m + 1]), Q[g][m], S[T]);
+        }
+        const float kc = kCodes ? fmaxf(now.kc * q_scale, 1.17549435e-38f) : now.kc;
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = lds_chunk_at(v_at + stage * kStage + (i >> 1) * 2048 + (i & 1) * 512);
         if (now.t * kTile + kTile - 1 > see_first) {  // some column does not see the whole tile
@@ -665,7 +732,7 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
             for (int st = 0; st < 2; ++st) {
               float p[8];
 #pragma unroll
-              for (int j = 0; j < 8; ++j) p[j] = fast_exp2(__builtin_fmaf(S[st][4 * (j / 4 * 2 + q) + j % 4], now.kc, -sub));
+              for (int j = 0; j < 8; ++j) p[j] = fast_exp2(__builtin_fmaf(S[st][4 * (j / 4 * 2 + q) + j % 4], kc, -sub));
               sum += form_eight(p, P[q][st]);
             }
           return sum * inv_v;
@@ -678,7 +745,7 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
           for (int T = 0; T < 2; ++T)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, S[T][i]);
-          mx = half_max(mx) * now.kc;
+          mx = half_max(mx) * kc;
           const float top = M > mx ? M : mx;
           if (top != M) {
             const float f = fast_exp2(M - top);
