@@ -532,6 +532,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, 2) void cache_attn(AttnArgs a) {
 //   K: score tile T (32 keys), step (g, m): lane l takes chunk (t = 2 T + l % 32 / 16, half = h, g, r = l % 16), bytes
 //      8 m ..: key of row l % 32, elements 32 g + 16 h + 8 m + [0, 8).  The result's register i of a lane is key
 //      16 (2 q + h) + 4 (2 T + i / 8) + i % 4 with q = i / 4 % 2: 16 keys in a row for each q.
+//      int8 codes become fp16, cheaper than bf16 (codes_to_half): 8192 rows over no history 681 / 657, 1024 over 15000 tokens
+//      341 / 331, 2048 over 2048 150 / 143.6 (us, as below).
 //      e4m3 codes need no conversion: v_mfma_f32_32x32x64_f8f6f4 takes them as they are, 64 elements and so the chunks of two g
 //      at a time, and q comes as a sum of two e4m3 (split_row), which costs as many matrix cycles as bf16.  32 heads
 //      over 8, codes to bf16 / as they are, us: 8192 rows over no history 536 / 471 (1168 TFLOP/s), 16384 2070 / 1793, 1024
@@ -554,11 +556,8 @@ __device__ __forceinline__ f32x16 mfma32_codes(i32x8 a, i32x8 b, f32x16 c) {
                 : __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
 }
 
-// A row of q as two rows of e4m3, q = 2^e (a + 2^-5 b): its half of the 128 elements, Q[g] 16 of them, of a lane.  The
-// largest |q| lies in [2^7, 2^8) 2^e.  a is q rounded to four bits and b the rest, which has no more than four: nothing of a
-// bf16's eight is lost down to 2^-14 of the row's largest, below it no more than 2^-23 of that.  A row that
-// is not finite becomes NaN.  Returns 2^e.
-__device__ __forceinline__ float split_row(const bf16x8 (&Q)[4][2], i32x8 (&A)[2], i32x8 (&B)[2]) {
+// The bits of a row's largest |q|, of which a lane holds half: 16 elements in Q[g].
+__device__ __forceinline__ uint32_t row_top(const bf16x8 (&Q)[4][2]) {
   uint32_t m = 0;
 #pragma unroll
   for (int g = 0; g < 4; ++g)
@@ -569,17 +568,31 @@ __device__ __forceinline__ float split_row(const bf16x8 (&Q)[4][2], i32x8 (&A)[2
       for (int i = 0; i < 4; ++i) m = max(m, max(q[i] & 0x7fffu, (q[i] >> 16) & 0x7fffu));
     }
   const auto r = __builtin_amdgcn_permlane32_swap(m, m, false, false);
-  m = max(r[0], r[1]);
-  const int e = max((int)(m >> 7) - 127 - 7, -120);  // -120: q's own subnormals
-  const float inv = pow2f(-e);
+  return max(r[0], r[1]);
+}
+
+// The exponent e that takes the largest |q| to [2^top, 2^(top + 1)) 2^e; the least is that of q's own subnormals.
+__device__ __forceinline__ int row_exp(uint32_t m, int top) { return max((int)(m >> 7) - 127 - top, -120); }
+
+// Elements 4 i .. 4 i + 3 of Q[g], times inv.
+__device__ __forceinline__ f32x4 four_of(const bf16x8 (&Q)[4][2], int g, int i, float inv) {
+  const u32x4 q = __builtin_bit_cast(u32x4, Q[g][i / 2]);
+  const uint32_t x = q[2 * (i & 1)], y = q[2 * (i & 1) + 1];
+  return f32x4{__uint_as_float(x << 16) * inv, __uint_as_float(x & 0xffff0000u) * inv, __uint_as_float(y << 16) * inv,
+               __uint_as_float(y & 0xffff0000u) * inv};
+}
+
+// A row of q as two rows of e4m3, q = 2^e (a + 2^-5 b), its largest element in [2^7, 2^8) 2^e.  a is q rounded to four
+// bits and b the rest, which has no more than four: nothing of a bf16's eight is lost down to 2^-14 of the
+// row's largest, below it no more than 2^-22 of that.  A row that is not finite becomes NaN.  Returns 2^e.
+__device__ __forceinline__ float split_row(const bf16x8 (&Q)[4][2], i32x8 (&A)[2], i32x8 (&B)[2]) {
+  const uint32_t m = row_top(Q);
+  const int e = row_exp(m, 7);
 #pragma unroll
   for (int g = 0; g < 4; ++g)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const u32x4 q = __builtin_bit_cast(u32x4, Q[g][i / 2]);
-      const uint32_t x = q[2 * (i & 1)], y = q[2 * (i & 1) + 1];
-      const f32x4 v = {__uint_as_float(x << 16) * inv, __uint_as_float(x & 0xffff0000u) * inv, __uint_as_float(y << 16) * inv,
-                       __uint_as_float(y & 0xffff0000u) * inv};
+      const f32x4 v = four_of(Q, g, i, pow2f(-e));
       int a = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], 0, false);
       a = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], a, true);
       const f32x4 w = from_codes<kCacheE4M3>((uint32_t)a);
@@ -589,6 +602,37 @@ __device__ __forceinline__ float split_row(const bf16x8 (&Q)[4][2], i32x8 (&A)[2
       B[g / 2][4 * (g & 1) + i] = m < 0x7f80u ? b : 0;
     }
   return pow2f(e);
+}
+
+typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
+typedef __attribute__((__vector_size__(2 * sizeof(_Float16)))) _Float16 f16x2;
+
+// A row of q in fp16, its largest element in [2^14, 2^15) 2^e: nothing is lost down to 2^-31 of that.  A row that is not
+// finite becomes NaN.  Returns 2^e.
+__device__ __forceinline__ float half_row(const bf16x8 (&Q)[4][2], f16x8 (&H)[4][2]) {
+  const uint32_t m = row_top(Q);
+  const int e = row_exp(m, 14);
+#pragma unroll
+  for (int g = 0; g < 4; ++g)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 v = four_of(Q, g, i, pow2f(-e));
+#pragma unroll
+      for (int x = 0; x < 4; ++x) H[g][i / 2][4 * (i & 1) + x] = m < 0x7f80u ? (_Float16)v[x] : (_Float16)__builtin_nanf("");
+    }
+  return pow2f(e);
+}
+
+// Eight int8 codes to fp16: 1024 + (c + 128), which is a byte set beside the exponent, and 1152 taken off, exactly.
+__device__ __forceinline__ f16x8 codes_to_half(uint32_t lo, uint32_t hi) {
+  const auto two = [](uint32_t x, uint32_t sel) {
+    const f16x2 off = {(_Float16)-1152.f, (_Float16)-1152.f};
+    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, x, sel)) + off);
+  };
+  lo ^= 0x80808080u;
+  hi ^= 0x80808080u;
+  const u32x4 r = {two(lo, 0x04010400u), two(lo, 0x04030402u), two(hi, 0x04010400u), two(hi, 0x04030402u)};
+  return __builtin_bit_cast(f16x8, r);
 }
 
 template <int FMT>
@@ -647,8 +691,10 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
         if (r < rows) Q[g][m] = *reinterpret_cast<const bf16x8*>(a.q + q_at + 32 * g + 16 * h + 8 * m);
       }
     i32x8 QA[2], QB[2];
-    float q_scale = 1.f;
+    f16x8 QH[4][2];
+    float q_scale;
     if constexpr (kCodes) q_scale = split_row(Q, QA, QB);
+    else q_scale = half_row(Q, QH);
     const int see_first = sw.r.len + r0 / a.G;
     const int see_last = sw.see_last(a, rt);
     f32x16 O[4];
@@ -700,9 +746,10 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-              for (int T = 0; T < 2; ++T) S[T] = mfma32(codes_to_bf16<FMT>(x[2 * g + T][2 * m], x[2 * g + T][2 * m + 1]), Q[g][m], S[T]);
+              for (int T = 0; T < 2; ++T)
+                S[T] = __builtin_amdgcn_mfma_f32_32x32x16_f16(codes_to_half(x[2 * g + T][2 * m], x[2 * g + T][2 * m + 1]), QH[g][m], S[T], 0, 0, 0);
         }
-        const float kc = kCodes ? fmaxf(now.kc * q_scale, 1.17549435e-38f) : now.kc;
+        const float kc = fmaxf(now.kc * q_scale, 1.17549435e-38f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = lds_chunk_at(v_at + stage * kStage + (i >> 1) * 2048 + (i & 1) * 512);
         if (now.t * kTile + kTile - 1 > see_first) {  // some column does not see the whole tile
