@@ -416,6 +416,28 @@ def test_queries_that_are_not_finite(rows, fmt):
     assert (o[:, rows:2 * rows] == 0).all()
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("rows", [1, 20, 90])
+def test_queries_with_outliers(rows, fmt):
+    """A few elements of every query are 1000 times the others and meet keys that are 0 there, so that the scores come from
+    the small ones; one head is of subnormal size; then large queries against keys that are small."""
+    C = _crisp()
+    _say(f"queries with outliers rows={rows} fmt={fmt}")
+    table, n_pages = _table([500 + rows], 64, np.random.default_rng(rows))
+    c, oracle = _new(C, n_pages, 1, 64, fmt)
+    k = _rand(1, 500 + rows, 1)
+    k[:, :, [3, 64, 127]] = 0
+    _append(C, c, oracle, table, [0], [500 + rows], k, _rand(1, 500 + rows, 2))
+    q = _rand(4, rows, 3)
+    q[:, :, [3, 64, 127]] *= 1000
+    q[1] *= 1e-38
+    q[2, :, 5] = 0
+    _check_attn(C, c, oracle, table, [500], [rows], q)
+    c, oracle = _new(C, n_pages, 1, 64, fmt)
+    _append(C, c, oracle, table, [0], [500 + rows], _rand(1, 500 + rows, 4, 2.0 ** -60), _rand(1, 500 + rows, 5))
+    _check_attn(C, c, oracle, table, [500], [rows], _rand(4, rows, 6, 2.0 ** 62))
+
+
 def test_padded_rows_are_left():
     """Rows behind the last sequence's keep what the output held; NaN in them and in dropped rows reaches nothing."""
     C = _crisp()
