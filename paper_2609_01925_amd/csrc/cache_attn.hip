@@ -180,6 +180,14 @@ struct Places {
     }
     total = lane_value(total, 0);
     shares = (int)min((int64_t)workgroups, total);
+    // One sequence of several row groups: if that leaves most of the workgroups busy, each unit is cut into the same number of
+    // shares, so that the groups go over the keys in step and share them in L2.  28 heads over 4, 32k tokens, as they fall / in
+    // step, us: 224 rows 43.5 / 31.5, 448 67.7 / 43.6, 672 89.5 / 57.5; 8k: 448 28.9 / 25.3.
+    if (R <= 32 && a.b.n_seqs == 1 && total > 0) {
+      const SeqWork<R> w = work(a, 0);
+      const int units = (int)min((int64_t)a.c.hkv * w.nrt, (int64_t)workgroups + 1), k = workgroups / units;
+      if (w.nrt > 1 && k > 0 && k <= w.grains && 8 * units * k >= 7 * workgroups) shares = units * k;
+    }
   }
 
   __device__ __forceinline__ int64_t start(int wg) const { return div64(wg * total, shares); }
@@ -977,27 +985,33 @@ CacheAttnPlan cache_attn_plan(const CacheDims& c, const BatchDims& b, int hq) {
   CacheAttnPlan p{16, kGrain, 0, false, 0, 0};
   if (b.n_seqs == 0 || b.n_rows == 0 || hq == 0) return p;
   const int64_t G = hq / c.hkv;
-  // Rows of a unit, by the rows of an average sequence and KV head.  Sequences of 4k to 8k tokens, us, 16 / 32 / 128 rows a unit:
-  //   32 of 10 rows 77.5 / 77.3 / 113, of 18 103 / 81.6 / 115, of 27 122 / 105 / 135; 8 of 66 66.9 / 53.2 / 49.1, of 172 127 / 96.0 /
-  //   77.5 (e4m3); 8 of 66 68.6 / 53.6 / 57.0, of 106 84.9 / 67.7 / 81.3, of 172 130 / 97.2 / 95.4 (int8, whose codes cost more in
-  //   each of 128 rows' four waves); 64 of 4 rows, 2k tokens, 57.5 / 58.5 / 89.4, of 16 each 22.6 / 24.3 / 26.8.
+  // Rows of a unit: 16, 32 or 128.  By the rows of an average sequence and KV head; sequences of 4k to 8k tokens, 16 / 32 / 128 rows a
+  // unit, us: 32 of 10 rows 77.5 / 77.3 / 113, of 18 103 / 81.6 / 115, of 27 122 / 105 / 135; 64 of 4 rows, 2k tokens, 57.5 / 58.5 / 89.4, of
+  // 16 each 22.6 / 24.3 / 26.8.
   const int64_t rows = (int64_t)b.n_rows * G, seqs = b.n_seqs;
   const bool even16 = b.n_rows % seqs == 0 && rows <= 16 * seqs;
-  p.rows = rows <= 8 * seqs || even16 ? 16 : rows <= (c.fmt == kCacheE4M3 ? 64 : 128) * seqs ? 32 : kRowUnit;
-  // About one unit a sequence and KV head: tiles are not read again, and the loads say so.  Plain / such loads, us: 48 rows
-  // over 0.3k to 8k tokens 93.6 / 83.6, one over 128k 37.5 / 33.5; in units of 32 rows, 32 sequences of 18 rows 96.6 / 83.6, of
-  // 27 109 / 106, of 38 44.3 / 46.8, of 54 73.3 / 84.2.
-  p.once = rows <= 32 * seqs;
+  p.rows = rows <= 8 * seqs || even16 ? 16 : 32;
   // units, and tiles of one, that the table has room for: upper bounds of what the lengths say on the device
-  const int64_t units = ((int64_t)b.n_rows * G / p.rows + b.n_seqs) * c.hkv;
   const int64_t room = (int64_t)b.max_pages * c.tiles > 1 ? (int64_t)b.max_pages * c.tiles : 1;
   // Short tables: units are not cut, which saves the second launch.  One row a sequence, 32 heads over 8, cut / not, us:
   // 1 sequence of 1000 tokens (16 tiles) 9.5 / 8.8, of 2000 9.3 / 12.3; 16 of 1000 11.8 / 10.1, 64 of 1000 27.3 / 26.0.
   const bool whole = room <= 16;
   if (whole) p.grain = (int)room;
+  const auto units = [&](int r) { return (rows / r + seqs) * c.hkv; };
+  const auto work = [&](int r) { return (double)units(r) * (double)((room + p.grain - 1) / p.grain); };
   constexpr int kMost = 512;  // what the GPU holds at once: two a CU, of four waves with up to 256 registers
-  const double work = (double)units * (double)((room + p.grain - 1) / p.grain);
-  int64_t wgs = work < kMost || whole ? (int64_t)(work < 4096 ? work : 4096) : kMost;
+  // 128 rows halve the work of a product, but its fewer units are cut into more pieces, each with 128 rows of partial sums: from six
+  // grains a workgroup on.  32 heads over 8, 32 / 128 rows a unit, us, one sequence of 8k tokens: 128 rows 21.9 / 31.0, 512 33.2 / 38.1,
+  // 1024 (4.6 grains) 51.1 / 53.8, 1600 (6.7) 74.6 / 74.0; of 32k: 128 32.6 / 40.1, 256 (5.9) 46.4 / 48.7, 512 (9.8) 77.4 / 73.8, 1600 312 /
+  // 199.  Up to 32 rows three of four waves would have none (int8, whose codes cost more in each wave, 96): 32 sequences of
+  // 24 45.2 / 45.4, 40 59.5 / 53.7, 112 107 / 70.1; int8 24 42.6 / 54.7, 80 79.5 / 79.8, 112 107 / 86.5.
+  if (rows > (c.fmt == kCacheE4M3 ? 32 : 96) * seqs && work(kRowUnit) > 6 * kMost) p.rows = kRowUnit;
+  // About one unit a sequence and KV head: tiles are not read again, and the loads say so.  Plain / such loads, us: 48 rows
+  // over 0.3k to 8k tokens 93.6 / 83.6, one over 128k 37.5 / 33.5; in units of 32 rows, 32 sequences of 18 rows 96.6 / 83.6, of
+  // 27 109 / 106, of 38 44.3 / 46.8, of 54 73.3 / 84.2.
+  p.once = rows <= 32 * seqs;
+  const double w = work(p.rows);
+  int64_t wgs = w < kMost || whole ? (int64_t)(w < 4096 ? w : 4096) : kMost;
   wgs = (wgs + kNumXcd - 1) / kNumXcd * kNumXcd;
   p.workgroups = (int)wgs;
   p.cut_bytes = whole ? 0 : ((size_t)wgs * sizeof(Cut) + 255) / 256 * 256;
