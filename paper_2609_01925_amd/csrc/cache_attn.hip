@@ -226,6 +226,16 @@ struct Places {
   }
 };
 
+// The share of this workgroup, or a number of its own from `shares` on if there are fewer.  Workgroup i runs on XCD i % 8, and the
+// grid is a multiple of 8: neighbouring shares go to one XCD, whose L2 then serves the row groups that read the same keys,
+// and each XCD has an eighth of them, also where the grid, which the host sizes from bounds, has more workgroups than there are
+// shares: 32 sequences of 1000 tokens, one row, the idle ones last / so, 18.1 / 13.0 us, 64 29.8 / 23.1.
+__device__ __forceinline__ int share_of(int workgroups, int shares) {
+  const int xcd = (int)blockIdx.x % kNumXcd, i = (int)blockIdx.x / kNumXcd;
+  const int first = xcd * shares / kNumXcd, mine = (xcd + 1) * shares / kNumXcd - first;
+  return i < mine ? first + i : shares + xcd * (workgroups / kNumXcd) - first + i - mine;
+}
+
 // The cut, if any, that a share leaves behind it: it ends `done` grains into the unit.
 template <typename P>
 __device__ __forceinline__ Cut cut_of(const P& pl, const Unit& u, int done, int row, int rows, int row0) {
@@ -354,11 +364,9 @@ __global__ __launch_bounds__(kFewWaves* kWave, 2) void cache_attn(AttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 15, g = lane >> 4;
   const int wgs = gridDim.x;
-  // workgroup i runs on XCD i % 8: neighbouring shares go to one XCD, whose L2 then serves the row
-  // groups that read the same keys
-  const int wg = wgs % kNumXcd == 0 ? (int)blockIdx.x % kNumXcd * (wgs / kNumXcd) + (int)blockIdx.x / kNumXcd : (int)blockIdx.x;
   Places<kRows, NW> pl;
   pl.count(a, wgs, lds);
+  const int wg = share_of(wgs, pl.shares);
   if (wg >= pl.shares) {
     if (a.cut && tid == 0) a.cut[wg].cuts = 0;
     return;
@@ -659,9 +667,9 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, h = lane >> 5;
   const int wgs = gridDim.x;
-  const int wg = (int)blockIdx.x % kNumXcd * (wgs / kNumXcd) + (int)blockIdx.x / kNumXcd;
   Places<kRows, NW> pl;
   pl.count(a, wgs, lds);
+  const int wg = share_of(wgs, pl.shares);
   if (wg >= pl.shares) {
     if (a.cut && tid == 0) a.cut[wg].cuts = 0;
     return;
@@ -1007,15 +1015,19 @@ CacheAttnPlan cache_attn_plan(const CacheDims& c, const BatchDims& b, int hq) {
   // 128 rows halve the work of a product, but its fewer units are cut into more pieces, each with 128 rows of partial sums: from six
   // grains a workgroup on.  32 heads over 8, 32 / 128 rows a unit, us, one sequence of 8k tokens: 128 rows 21.9 / 31.0, 512 33.2 / 38.1,
   // 1024 (4.6 grains) 51.1 / 53.8, 1600 (6.7) 74.6 / 74.0; of 32k: 128 32.6 / 40.1, 256 (5.9) 46.4 / 48.7, 512 (9.8) 77.4 / 73.8, 1600 312 /
-  // 199.  Up to 32 rows three of four waves would have none (int8, whose codes cost more in each wave, 96): 32 sequences of
-  // 24 45.2 / 45.4, 40 59.5 / 53.7, 112 107 / 70.1; int8 24 42.6 / 54.7, 80 79.5 / 79.8, 112 107 / 86.5.
-  if (rows > (c.fmt == kCacheE4M3 ? 32 : 96) * seqs && work(kRowUnit) > 6 * kMost) p.rows = kRowUnit;
+  // 199.  Up to 64 rows half of its waves or more would have none (int8, whose codes cost more in each wave, 96), which gains little
+  // where it gains and costs much where sequences are short in a wide table: 32 sequences of 2k tokens, 40 rows 59.5 / 53.7, 80
+  // 71.3 / 63.5, 112 107 / 70.1; int8 80 79.5 / 79.8, 112 107 / 86.5; 2 of 3k, 64 rows 18.2 / 26.1.
+  if (rows > (c.fmt == kCacheE4M3 ? 64 : 96) * seqs && work(kRowUnit) > 6 * kMost) p.rows = kRowUnit;
   // About one unit a sequence and KV head: tiles are not read again, and the loads say so.  Plain / such loads, us: 48 rows
   // over 0.3k to 8k tokens 93.6 / 83.6, one over 128k 37.5 / 33.5; in units of 32 rows, 32 sequences of 18 rows 96.6 / 83.6, of
   // 27 109 / 106, of 38 44.3 / 46.8, of 54 73.3 / 84.2.
   p.once = rows <= 32 * seqs;
   const double w = work(p.rows);
-  int64_t wgs = w < kMost || whole ? (int64_t)(w < 4096 ? w : 4096) : kMost;
+  // Whole units of 32 rows and more take a workgroup each; of 16, whose work is much the same, 512 workgroups take them in turn,
+  // us: 256 sequences of 500 tokens, one row, 51.7 / 45.6, of 200 37.8 / 28.7; 32 sequences of 500, 40 rows, 36.7 / 39.0 (int8 37.6 / 43.5).
+  const int most = whole && p.rows > 16 ? 4096 : kMost;
+  int64_t wgs = (int64_t)(w < most ? w : most);
   wgs = (wgs + kNumXcd - 1) / kNumXcd * kNumXcd;
   p.workgroups = (int)wgs;
   p.cut_bytes = whole ? 0 : ((size_t)wgs * sizeof(Cut) + 255) / 256 * 256;
