@@ -1006,7 +1006,7 @@ CacheAttnPlan cache_attn_plan(const CacheDims& c, const BatchDims& b, int hq) {
   // units, and tiles of one, that the table has room for: upper bounds of what the lengths say on the device
   const int64_t room = (int64_t)b.max_pages * c.tiles > 1 ? (int64_t)b.max_pages * c.tiles : 1;
   // Short tables: units are not cut, which saves the second launch.  One row a sequence, 32 heads over 8, cut / not, us:
-  // 1 sequence of 1000 tokens (16 tiles) 9.5 / 8.8, of 2000 9.3 / 12.3; 16 of 1000 11.8 / 10.1, 64 of 1000 27.3 / 26.0.
+  // 1 sequence of 1000 tokens (16 tiles) 11.0 / 9.5, 16 12.5 / 10.9, 64 25.2 / 23.1, 256 88.5 / 86.6; 1 of 2000 (alone on the GPU) 9.3 / 12.3.
   const bool whole = room <= 16;
   if (whole) p.grain = (int)room;
   const auto units = [&](int r) { return (rows / r + seqs) * c.hkv; };
