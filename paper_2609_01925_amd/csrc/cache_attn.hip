@@ -303,9 +303,11 @@ __device__ __forceinline__ float form_eight(const float (&p)[8], bf16x8& P) {
 // at most 2^8, so that every p is, where its bf16 rounding is that of one below 1 and the 32-bit sums have
 // room.  Otherwise, and for a column without a reference, M is raised to the maximum, O and L are
 // rescaled, and P is formed again.  L sums the rounded p's, which are what PV adds.
+// A column without a reference is one that has seen no key yet, unless the tile, whose first position is `first`, holds one that it
+// sees: then every product of it so far is NaN or -infinity (a query that is not finite), and what it forms, NaN, stands.
 template <int C>
-__device__ __forceinline__ void softmax_step(const acc4 (&S)[C][4], float kc, int ev, float (&M)[C], float (&L)[C],
-                                             acc4 (&O)[C][8], bf16x8 (&P)[C][2]) {
+__device__ __forceinline__ void softmax_step(const acc4 (&S)[C][4], float kc, int ev, int first, const int (&see)[C],
+                                             float (&M)[C], float (&L)[C], acc4 (&O)[C][8], bf16x8 (&P)[C][2]) {
   const float inv_v = pow2f(-ev);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
@@ -340,7 +342,7 @@ __device__ __forceinline__ void softmax_step(const acc4 (&S)[C][4], float kc, in
         M[c] = m;
       }
       sum = form();
-      if (M[c] == -__builtin_inff()) {  // this column has seen no key yet
+      if (M[c] == -__builtin_inff() && first > see[c]) {
         sum = 0.f;
         P[c][0] = P[c][1] = bf16x8{};
       }
@@ -465,7 +467,7 @@ __global__ __launch_bounds__(kFewWaves* kWave, 2) void cache_attn(AttnArgs a) {
       }
       __builtin_amdgcn_sched_barrier(0);
       bf16x8 P[C][2];
-      softmax_step<C>(S, now.kc, now.ev, M, L, O, P);
+      softmax_step<C>(S, now.kc, now.ev, now.t * kTile, see, M, L, O, P);
 #pragma unroll
       for (int st = 0; st < 2; ++st)
 #pragma unroll
@@ -824,7 +826,7 @@ __global__ __launch_bounds__(kRowWaves* kWave, 2) void cache_attn_rows(AttnArgs 
             M = top;
           }
           sum = form();
-          if (M == -__builtin_inff()) {
+          if (M == -__builtin_inff() && now.t * kTile > see) {
             sum = 0.f;
             P[0][0] = P[0][1] = P[1][0] = P[1][1] = bf16x8{};
           }
