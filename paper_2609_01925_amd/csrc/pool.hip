@@ -189,8 +189,8 @@ __global__ __launch_bounds__(kThreads) void pool_reserve(int n_pages, int B, int
     }
   };
   Slots x;
-  for (int p0 = 0; p0 < total; p0 += kRound) {
-    read(p0, x);
+  for (int64_t p0 = 0; p0 < total; p0 += kRound) {  // 64 bits: total may be 2^31 - 1
+    read((int)p0, x);
     int n = 0;  // missing pages of one sequence among the thread's slots
 #pragma unroll
     for (int k = 0; k < kEach; ++k) {
@@ -239,8 +239,8 @@ __global__ __launch_bounds__(kThreads) void pool_reserve(int n_pages, int B, int
       collect_free(bits, n_pages, now, &word, l);
     }
     int rank = 0;
-    for (int p0 = 0; p0 < total && rank < now; p0 += kRound) {
-      if (total > kRound) read(p0, x);  // otherwise x is still that of the only round
+    for (int64_t p0 = 0; p0 < total && rank < now; p0 += kRound) {
+      if (total > kRound) read((int)p0, x);  // otherwise x is still that of the only round
       int mine = 0;
 #pragma unroll
       for (int k = 0; k < kEach; ++k) {
