@@ -310,7 +310,7 @@ typedef struct {
   int32_t format;
 } crisp_cache_shape;
 
-/* n_seqs, max_pages, n_rows >= 0; max_pages * block <= 2^30, n_seqs * max_pages < 2^31, n_rows <= 2^24.
+/* n_seqs, max_pages, n_rows >= 0; max_pages * block <= 2^30, n_seqs * max_pages < 2^31, n_seqs and n_rows <= 2^24.
  * Without sequences or rows a call returns CRISP_OK and launches nothing. */
 typedef struct {
   int32_t n_seqs;

@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kMaxPages = 1 << 24;
 constexpr int kMaxRows = 1 << 24;         // with all query heads: rows of a sequence x G stays in int32
+constexpr int kMaxSeqs = 1 << 24;         // of a call on a cache: each workgroup of the attention looks them all over
 constexpr int64_t kMaxTokens = 1 << 30;   // of one sequence's table
 
 crisp_status fail(crisp_status s, const char* fmt, ...) {
@@ -73,6 +74,7 @@ crisp_status check_batch(const crisp_cache_batch* b, const CacheDims& c, BatchDi
   if (b->n_rows < 0) return fail(CRISP_EINVAL, "bad batch: n_rows=%d", b->n_rows);
   CHECK(check_table(c.B, b->n_seqs, b->max_pages));
   if (b->n_rows > kMaxRows) return fail(CRISP_EUNSUPPORTED, "n_rows %d above the supported %d", b->n_rows, kMaxRows);
+  if (b->n_seqs > kMaxSeqs) return fail(CRISP_EUNSUPPORTED, "n_seqs %d above the supported %d", b->n_seqs, kMaxSeqs);
   *d = BatchDims{b->n_seqs, b->max_pages, b->n_rows};
   return CRISP_OK;
 }

@@ -1,8 +1,22 @@
 """The cache's entry points at the largest sizes that they take, and their refusals beyond."""
+import ctypes
+
 import pytest
 import torch
 
 from paper_2609_01925_amd import crisp as C
+from tests.test_cache_abi import REF, _append, _attn, _shape
+
+
+@pytest.mark.parametrize("n_seqs,code", [(1 << 24, C.CRISP_OK), ((1 << 24) + 1, C.CRISP_EUNSUPPORTED), (2 ** 31 - 1, C.CRISP_EUNSUPPORTED)])
+def test_sequences_of_a_call(n_seqs, code):
+    """A search for a row's sequence steps through the sequences in 64 parts: past 2^31 - 64 of them the step left 32 bits."""
+    n = ctypes.c_size_t()
+    for wide in (0, 1, 100):
+        b = (n_seqs, wide, 3)
+        assert C.lib.crisp_cache_attn_workspace_size(REF(_shape()), REF(C.CrispCacheBatch(*b)), 4, REF(n)) == code
+        if code:
+            assert _append(b=b) == code and _attn(b=b) == code
 
 
 @pytest.mark.gpu
