@@ -13,6 +13,7 @@ attend to is nothing (o is 0), and advance() does not count them.
 """
 from __future__ import annotations
 
+import math
 from typing import Optional
 
 import torch
@@ -54,12 +55,16 @@ class KVCache:
     def prefill(self, layer: int, seq: int, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                 params: Optional[C.CrispParams] = None) -> torch.Tensor:
         """One layer of a prompt, sequence `seq` holding nothing yet and its pages reserved: sparse prefill
-        attention over q [H_q, n, 128], k and v [H_kv, n, 128] as they are, then k and v into the cache -> o."""
+        attention over q [H_q, n, 128], k and v [H_kv, n, 128] as they are, then k and v into the cache -> o.  If the
+        sequence holds tokens (attend() is for rows behind those) nothing is stored and o's first and last rows are NaN."""
         if not 0 <= seq < self.table.shape[0]:
             raise ValueError(f"sequence {seq} outside [0, {self.table.shape[0]})")
         o = C.crisp_prefill_attn(q, k, v, C.make_params() if params is None else params)
-        C.crisp_cache_append(self.layers[layer], self._open[seq:seq + 1], self.seq_len[seq:seq + 1],
-                             self._all * k.shape[1], k, v)
+        n = k.shape[1]
+        held = self.seq_len[seq] > 0
+        o[:, ::max(n - 1, 1)].masked_fill_(held, math.nan)
+        C.crisp_cache_append(self.layers[layer], torch.where(held, self._none, self._open[seq:seq + 1]),
+                             self.seq_len[seq:seq + 1], self._all * n, k, v)
         return o
 
     def attend(self, layer: int, row_ptr: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,

@@ -200,3 +200,23 @@ def test_refusals_in_a_graph():
     kv.free(_ints([2]))
     del mirror.seqs[2], mirror.len[2]
     replay([1, 1, 0], (), 5)
+
+
+@pytest.mark.parametrize("n", [1, 2, 150])
+def test_prompt_of_a_sequence_that_holds_tokens(n):
+    """prefill attends to the prompt alone: of a sequence that holds tokens it stores nothing, and its result says so."""
+    print(f"[gpu-case] prompt of a sequence that holds tokens n={n}", flush=True)
+    from paper_2609_01925_amd import crisp as C
+    kv, mirror = _kv(8, 2, 640)
+    _step(kv, mirror, [70, 3], (), 1)
+    kv.reserve(_ints([n, 0]))
+    q, k, v = (_rand(h, n, i).to(DEV) for i, h in enumerate((4, 2, 2)))
+    for layer in range(2):
+        o = kv.prefill(layer, 0, q, k, v)
+        assert o[:, [0, n - 1]].isnan().all()
+        assert torch.equal(o[:, 1:n - 1], C.crisp_prefill_attn(q, k, v, C.make_params())[:, 1:n - 1])
+    _held(kv, mirror)
+    _step(kv, mirror, [2, 1], (), 2)
+    kv.free(_ints([0]))
+    kv.reserve(_ints([n, 0]))
+    assert torch.equal(kv.prefill(0, 0, q, k, v), C.crisp_prefill_attn(q, k, v, C.make_params()))
