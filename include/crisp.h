@@ -336,7 +336,8 @@ crisp_status crisp_cache_append(const crisp_cache_shape* cache, const crisp_cach
                                 const crisp_bf16* v, int64_t v_head_stride, int64_t v_row_stride,
                                 crisp_stream stream);
 
-/* Host only.  Bytes of workspace (256-byte aligned, any contents) of crisp_cache_attn. */
+/* Host only.  Bytes of workspace (256-byte aligned, any contents) of crisp_cache_attn: enough for n_rows and max_pages that
+ * are smaller as well. */
 crisp_status crisp_cache_attn_workspace_size(const crisp_cache_shape* cache, const crisp_cache_batch* batch,
                                              int32_t n_q_heads, size_t* bytes);
 

@@ -440,7 +440,8 @@ def crisp_cache_attn_workspace_size(cache: Cache, n_q_heads: int, n_seqs: int, m
 
 
 def cache_workspace(cache: Cache, n_q_heads: int, n_seqs: int, n_rows: int, max_pages: Optional[int] = None) -> torch.Tensor:
-    """A workspace for crisp_cache_attn; without max_pages one that is enough for any table width."""
+    """A workspace for crisp_cache_attn calls of n_seqs sequences and up to n_rows rows in a table of up to max_pages pages
+    a sequence; without max_pages of any width."""
     wide = (1 << 30) // cache.block if max_pages is None else max_pages
     if max_pages is None and n_seqs:
         wide = min(wide, ((1 << 31) - 1) // n_seqs)

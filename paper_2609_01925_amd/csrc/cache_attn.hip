@@ -1002,6 +1002,10 @@ CacheAttnPlan cache_attn_plan(const CacheDims& c, const BatchDims& b, int hq) {
   // Rows of a unit: 16, 32 or 128.  By the rows of an average sequence and KV head; sequences of 4k to 8k tokens, 16 / 32 / 128 rows a
   // unit, us: 32 of 10 rows 77.5 / 77.3 / 113, of 18 103 / 81.6 / 115, of 27 122 / 105 / 135; 64 of 4 rows, 2k tokens, 57.5 / 58.5 / 89.4, of
   // 16 each 22.6 / 24.3 / 26.8.
+  // Between 8 and 16 rows on average it depends on how they are spread, which only the device knows.  A step of as many tokens for each
+  // sequence (drafts of one length) has n_rows a multiple of n_seqs, so that is taken for one.  32 heads over 8, three tokens each / one
+  // to five / one or nine, units of 16 and of 32, us: 32 sequences of 4k to 8k tokens 71.8 and 76.3 / 79.6 and 77.2 / 96.3 and 91.5, 64 of 1k
+  // to 3k 54.4 and 58.3 / 59.2 and 59.4 / 68.9 and 69.1: gained where the guess holds, 0 to 5% lost where it does not.
   const int64_t rows = (int64_t)b.n_rows * G, seqs = b.n_seqs;
   const bool even16 = b.n_rows % seqs == 0 && rows <= 16 * seqs;
   p.rows = rows <= 8 * seqs || even16 ? 16 : 32;
@@ -1025,15 +1029,24 @@ CacheAttnPlan cache_attn_plan(const CacheDims& c, const BatchDims& b, int hq) {
   // over 0.3k to 8k tokens 93.6 / 83.6, one over 128k 37.5 / 33.5; in units of 32 rows, 32 sequences of 18 rows 96.6 / 83.6, of
   // 27 109 / 106, of 38 44.3 / 46.8, of 54 73.3 / 84.2.
   p.once = rows <= 32 * seqs;
-  const double w = work(p.rows);
-  // Whole units of 32 rows and more take a workgroup each; of 16, whose work is much the same, 512 workgroups take them in turn,
-  // us: 256 sequences of 500 tokens, one row, 51.7 / 45.6, of 200 37.8 / 28.7; 32 sequences of 500, 40 rows, 36.7 / 39.0 (int8 37.6 / 43.5).
-  const int most = whole && p.rows > 16 ? 4096 : kMost;
-  int64_t wgs = (int64_t)(w < most ? w : most);
-  wgs = (wgs + kNumXcd - 1) / kNumXcd * kNumXcd;
-  p.workgroups = (int)wgs;
-  p.cut_bytes = whole ? 0 : ((size_t)wgs * sizeof(Cut) + 255) / 256 * 256;
-  p.bytes = whole ? 256 : p.cut_bytes + (size_t)wgs * 2 * p.rows * (kHeadDim + 2) * sizeof(float);
+  const auto workgroups = [&](int r) {
+    const double w = work(r);
+    // Whole units of 32 rows and more take a workgroup each; of 16, whose work is much the same, 512 workgroups take them in turn,
+    // us: 256 sequences of 500 tokens, one row, 51.7 / 45.6, of 200 37.8 / 28.7; 32 sequences of 500, 40 rows, 36.7 / 39.0 (int8 37.6 / 43.5).
+    const int most = whole && r > 16 ? 4096 : kMost;
+    const int64_t wgs = (int64_t)(w < most ? w : most);
+    return (size_t)((wgs + kNumXcd - 1) / kNumXcd * kNumXcd);
+  };
+  const auto cut_bytes = [&](int r) { return (workgroups(r) * sizeof(Cut) + 255) / 256 * 256; };
+  p.workgroups = (int)workgroups(p.rows);
+  if (whole) {
+    p.bytes = 256;
+  } else {
+    p.cut_bytes = cut_bytes(p.rows);
+    // even16 counts as units of 32 here: so a workspace is enough for fewer rows of the same sequences too
+    const int r = even16 && rows > 8 * seqs ? 32 : p.rows;
+    p.bytes = cut_bytes(r) + workgroups(r) * 2 * r * (kHeadDim + 2) * sizeof(float);
+  }
   return p;
 }
 

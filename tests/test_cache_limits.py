@@ -33,3 +33,22 @@ def test_reservation_over_a_table_of_2_31_entries():
     assert torch.equal(table[0], torch.arange(wide, dtype=torch.int32, device="cuda:0"))
     assert (table[1:] == -1).all()
     assert (pool[:wide] == 1).all() and (pool[wide:n_pages] == 0).all()
+
+
+def test_workspace_of_a_batch_is_enough_for_less():
+    """What cache_workspace gives for a batch serves the same sequences with fewer rows and in a narrower table."""
+    def size(hq, hkv, fmt, seqs, wide, rows):
+        n = ctypes.c_size_t()
+        b = C.CrispCacheBatch(seqs, wide, rows)
+        assert C.lib.crisp_cache_attn_workspace_size(REF(_shape(heads=hkv, fmt=fmt)), REF(b), hq, REF(n)) == C.CRISP_OK
+        return n.value
+
+    for hq, hkv in ((32, 8), (28, 4), (7, 1), (4, 4)):
+        for fmt in (0, 1):
+            for seqs in (1, 2, 3, 7, 32, 64, 100):
+                before = None
+                for wide in (1, 10, 16, 17, 40, 200, 700, 2048, 20000):
+                    at = [size(hq, hkv, fmt, seqs, wide, rows) for rows in range(1, 40 * seqs, 1 + seqs // 4)]
+                    assert at == sorted(at), (hq, hkv, fmt, seqs, wide)
+                    assert before is None or all(a <= b for a, b in zip(before, at)), (hq, hkv, fmt, seqs, wide)
+                    before = at
