@@ -163,6 +163,27 @@ def test_units_of_128_rows_and_outliers(fmt):
     _check(C, c, oracle, table, lens, counts, _rand(4, rows, 7), 128, scale=1e-42)
 
 
+@pytest.mark.parametrize("rows,width,unit", [(3, 30, 32), (60, 30, 32), (120, 3200, 128)])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_small_codes(fmt, rows, width, unit):
+    """Elements of K and V 2^12 and 2^15 times the others, where every query is 0: scores and results come from the smallest codes
+    (subnormal ones of e4m3)."""
+    C = _crisp()
+    _say(f"small codes fmt={fmt} rows={rows}")
+    lens, counts = np.array([500]), np.array([rows])
+    table = _wide(_table(lens + counts, 64, np.random.default_rng(1))[0], width)
+    c, oracle = _new(C, 12, 1, 64, fmt)
+    big = 2.0 ** (12 if fmt == O.E4M3 else 5)
+    k, v = _rand(1, 500 + rows, 1), _rand(1, 500 + rows, 2)
+    k[:, :, :5] *= big
+    k[:, 100:300, 5:9] *= 8 * big
+    v[:, :, 77] *= 8 * big
+    _append(C, c, oracle, table, [0], [500 + rows], k, v)
+    q = _rand(4, rows, 3, 2.0)
+    q[:, :, :9] = 0
+    _check(C, c, oracle, table, lens, counts, q, unit)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_units_of_128_rows_that_are_not_finite(fmt):
     """A NaN or an infinity makes its row NaN and no other, in the first, a middle and the last row group."""
