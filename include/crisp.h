@@ -346,9 +346,11 @@ crisp_status crisp_cache_attn_workspace_size(const crisp_cache_shape* cache, con
  * over the positions j that have a page; a row that sees none gets 0.  Query head h reads KV
  * head h / (H_q / H_kv).  softmax_scale 0 means 1/sqrt(128).  The work is split evenly over the GPU
  * whatever the lengths, also along a sequence; partial results are joined in a fixed order, so
- * that a call with the same arguments gives the same bits.  In calls of many rows on e4m3 caches, elements of q below
- * 2^-14 of their row's largest count to 2^-22 of that; all others are exact.  Scores and sums are 32-bit floats; the sums over v are divided
- * last, so |v| is to stay below 2^80.  The heads of o lie behind one another or between its rows (one stride covers
+ * that a call with the same arguments gives the same bits.  Scores and sums are 32-bit floats, the probabilities
+ * are rounded to bf16 before they meet v, and their sum is that of the rounded ones.  In calls of many rows on e4m3
+ * caches, elements of q below 2^-14 of their row's largest count to 2^-22 of that; all others are exact.  |q| is to stay
+ * below 2^112 (products with codes), |v| below 2^80 (its sums are divided last).  A row with a NaN or an infinity is NaN if
+ * it sees a token.  The heads of o lie behind one another or between its rows (one stride covers
  * the other's whole extent). */
 crisp_status crisp_cache_attn(const crisp_cache_shape* cache, const crisp_cache_batch* batch, int32_t n_q_heads,
                               float softmax_scale, const uint8_t* pages, const float* scales, const int32_t* table,

@@ -392,9 +392,6 @@ __global__ __launch_bounds__(kThreads) void cache_copy(CacheDims c, const int32_
 hipError_t launch_cache_append(const CacheDims& c, const BatchDims& b, const Seqs& s, const uint16_t* k, Strides ks,
                                const uint16_t* v, Strides vs, uint8_t* pages, float* scales, hipStream_t stream) {
   const AppendArgs a{c, b, s, k, v, ks, vs, pages, scales};
-  // Few rows a sequence: a wave for each row and head.  8 heads, e4m3, the page kernel / this one, us: 64 sequences of one row
-  // 5.7 / 3.9, of 2.8 on average 6.8 / 6.4, of 4.0 7.0 / 7.8; past 64 sequences, which the page kernel has to count, 1000
-  // of one 37.3 / 10.3, of 4.5 57.1 / 30.2; 4000 of one 201 / 27.3.
   // Few rows a sequence on average: no list of pages is needed, a wave looks at each row.  8 heads, e4m3, the page kernel / this
   // one, us: 256 sequences of one row 10.6 / 7.6, of 4 13.4 / 13.4, of 8 13.3 / 20.9, 255 of one and one of 512 13.6 / 11.0, one of
   // 2000 7.9 / 14.3; past that the page kernel has to count for long: 1000 of one 38.5 / 11.2, of 4.5 56.1 / 39.7, of 10 62.5 / 62.7;

@@ -303,6 +303,9 @@ __device__ __forceinline__ float form_eight(const float (&p)[8], bf16x8& P) {
 // at most 2^8, so that every p is, where its bf16 rounding is that of one below 1 and the 32-bit sums have
 // room.  Otherwise, and for a column without a reference, M is raised to the maximum, O and L are
 // rescaled, and P is formed again.  L sums the rounded p's, which are what PV adds.
+// P is rounded to bf16, as in the prefill: products of 32 bits would take 16 times the matrix cycles, and fp16's range does not hold
+// 2^ev p.  A p is off by up to 2^-8 of itself.  Against 64 bits the listed cases' results are off by 0.0022 to 0.0023 of their
+// size, with P in 32 bits by 0.0016 to 0.0017 (the rounding of the result).
 // A column without a reference is one that has seen no key yet, unless the tile, whose first position is `first`, holds one that it
 // sees: then every product of it so far is NaN or -infinity (a query that is not finite), and what it forms, NaN, stands.
 template <int C>
@@ -545,7 +548,8 @@ __global__ __launch_bounds__(kFewWaves* kWave, 2) void cache_attn(AttnArgs a) {
 // are their own, so nothing is joined inside the workgroup.  Two workgroups share a CU: while a wave of one
 // forms probabilities, one of the other feeds the matrix unit.
 // Bound by the issue of the two: chunks of 75 to 450 rows of three sequences of 15k to 23k tokens, 28 heads over 4, e4m3: matrix unit
-// busy on 47% of the cycles, vector unit on 49%, both on 15%; with the join 243 us, 1.04 PFLOP/s.
+// busy on 47% of the cycles, vector unit on 49%, both on 15%; with the join 237 to 258 us from card to card, 0.98 to 1.07 PFLOP/s, once
+// the clock has settled (a burst's first milliseconds have up to 330).
 //
 // The products are v_mfma_f32_32x32x16_bf16 (layouts in crisp_device.h): beside these the other wave's vector
 // instructions run 1.45 times as long as alone, beside the 16 x 16 ones 1.9 times.  The tile's chunks serve them as

@@ -21,7 +21,8 @@ constexpr int kWavesPool = kThreads / kWave;
 constexpr int kBuf = 4096;  // free pages collected at a time
 // Up to so many row entries a fork fills the new rows in its own launch.  A free and a fork of 16, in a second launch / here,
 // us, called from a host program and replayed from a graph: 64 slots 18.1 / 15.2 and 11.1 / 9.9; 256 (the limit) 18.0 / 15.1 and
-// 11.6 / 13.3; 512 18.1 / 17.0 and 12.8 / 16.7; 1024 18.0 / 27.1 and 15.0 / 26.6.
+// 11.6 / 13.3; 512 18.1 / 17.0 and 12.8 / 16.7; 1024 18.0 / 27.1 and 15.0 / 26.6.  The limit is where a program that calls gains still; a
+// replayed graph, whose launches cost less, gains up to about half of it and loses up to 1.7 us there.
 constexpr int64_t kShareHere = 4096;
 constexpr int kPerThread = kPoolMaxSeqs / kThreads;
 constexpr int kMostFree = 1 << 16;  // workgroups of a free; each takes every so-many-th sequence
