@@ -23,7 +23,8 @@ from . import crisp as C
 
 class KVCache:
     """table int32 [max_seqs, pages of max_tokens], seq_len int32 [max_seqs] (tokens that all layers hold), room int32
-    [max_seqs] (rows that each sequence may still take), pool (C.crisp_pool_init) and layers (a C.Cache each)."""
+    [max_seqs] (rows that each sequence may still take), pool (C.crisp_pool_init) and layers (a C.Cache each).  The
+    methods change them; they are there to be read."""
 
     def __init__(self, n_layers: int, n_pages: int, n_kv_heads: int, max_seqs: int, max_tokens: int, block: int = 64,
                  fmt: int = C.CACHE_E4M3, device="cuda"):
@@ -88,7 +89,7 @@ class KVCache:
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor) -> torch.Tensor:
         """Empty sequences dst[i] become copies of src[i], sharing full pages -> copies int32 [n, 2], (-2, -2) where
-        a fork was refused."""
+        a fork was refused: that dst[i] is what it was, and rows that it is granted later are its first."""
         copies = C.crisp_pool_fork(self.pool, self.block, self.table, self.seq_len, src, dst)
         for cache in self.layers:
             C.crisp_cache_copy(cache, copies)
