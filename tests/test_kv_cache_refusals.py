@@ -220,3 +220,57 @@ def test_prompt_of_a_sequence_that_holds_tokens(n):
     kv.free(_ints([0]))
     kv.reserve(_ints([n, 0]))
     assert torch.equal(kv.prefill(0, 0, q, k, v), C.crisp_prefill_attn(q, k, v, C.make_params()))
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_histories(seed):
+    """Steps with and without reservations, forks, ends, tokens taken back and compactions in a random order on few pages: what is
+    granted, room, pages, tables, lengths and every held token after each of them."""
+    print(f"[gpu-case] KVCache histories seed={seed}", flush=True)
+    rng = np.random.default_rng(seed)
+    S, block = int(rng.integers(2, 7)), int(rng.choice([64, 128]))
+    n_pages = int(rng.integers(3, 16))
+    kv, mirror = _kv(n_pages, S, int(rng.integers(2, 6)) * block, int(rng.integers(2)), block)
+    pool, room = O.Pool(n_pages, block, kv.table.cpu().numpy(), [0] * S), np.zeros(S, dtype=int)
+    for step in range(25):
+        pool.seq_len = [mirror.len.get(s, 0) for s in range(S)]
+        op = rng.choice(["step"] * 5 + ["fork", "free", "back", "compact"])
+        if op == "step":
+            counts = rng.integers(0, rng.choice([2, 6, block + 10]), S) * (rng.random(S) < 0.8)
+            if rng.random() < 0.85:
+                want = np.array(pool.reserve(counts.tolist()))
+                assert kv.reserve(_ints(counts)).tolist() == want.tolist(), step
+                room = np.where(want < counts, 0, np.maximum(room, want))
+            else:
+                counts = np.where(room > 0, np.minimum(counts, room), counts)
+            refused = [s for s in range(S) if counts[s] and not room[s]]
+            if counts.sum():
+                _step(kv, mirror, counts, refused, 100 * seed + step, reserve=False)
+            room = np.maximum(room - counts, 0)
+        elif op == "fork":
+            src, dst = rng.integers(0, S, (2, int(rng.integers(1, 4))))
+            want, seqs, lens = pool.fork(src.tolist(), dst.tolist()), copy.deepcopy(mirror.seqs), dict(mirror.len)
+            assert [tuple(x) for x in kv.fork(_ints(src), _ints(dst)).tolist()] == want, step
+            for s, d, pair in zip(src, dst, want):
+                if pair != (-2, -2):
+                    mirror.seqs[d], mirror.len[d] = copy.deepcopy(seqs.get(s, mirror.new())), lens.get(s, 0)
+        elif op == "free":
+            ids = rng.integers(-1, S + 1, 2)
+            pool.free(ids.tolist())
+            kv.free(_ints(ids))
+            for s in ids[(ids >= 0) & (ids < S)]:
+                mirror.seqs.pop(s, None), mirror.len.pop(s, None)
+                room[s] = 0
+        elif op == "back":
+            back = rng.integers(0, block, S) * (rng.random(S) < 0.4)
+            kv.advance(_ints(-back))
+            for s in np.nonzero(back)[0]:
+                mirror.len[s] = max(0, mirror.len.get(s, 0) - int(back[s]))
+                mirror.seqs.setdefault(s, mirror.new())
+                room[s] = 0
+        else:
+            pool.compact()
+            kv.compact()
+        assert kv.table.tolist() == [list(r) for r in pool.table], (step, op)
+        assert kv.pool.tolist() == pool.words().tolist() and kv.room.tolist() == room.tolist(), (step, op)
+        _held(kv, mirror)
