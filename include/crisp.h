@@ -12,7 +12,8 @@
  *   4. causal softmax attention restricted to that set           (Eq. 1, Sec. 2.1)
  *
  * Behind the prefill it keeps K and V in an 8-bit paged cache and attends to it: the
- * crisp_cache_* and crisp_pool_* entry points, whose layouts stand with them below.
+ * crisp_cache_* and crisp_pool_* entry points, whose layouts stand with them below.  Beside it,
+ * crisp_rope and crisp_packed_attn take rows of several sequences at once.
  *
  * Conventions of the prefill entry points (ownership, execution and errors: of all)
  * ----------------------------------------------------------------------------------
@@ -405,6 +406,118 @@ crisp_status crisp_pool_free(int32_t n_pages, int32_t n_seqs, int32_t max_pages,
  * their number; table (all rows that name pages of the pool) and pool follow. */
 crisp_status crisp_pool_compact(int32_t n_pages, int32_t n_seqs, int32_t max_pages, int32_t* pool, int32_t* table,
                                 int32_t* moves, int32_t* count, crisp_stream stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Rows of several sequences packed behind one another, before they meet a cache: rotary positions on q and k, and the
+ * causal attention of whole prompts.  Rows row_ptr[s] .. row_ptr[s + 1] (int32[n_seqs + 1], on the device) are sequence s's;
+ * packed tensors, strides, uncovered rows and device values out of range are as for the cache above (its outputs' rule of
+ * strides too).  head_dim == 128, n_seqs and n_rows in [0, 2^24], n_q_heads and n_kv_heads <= 65535; without sequences or rows a
+ * call returns CRISP_OK and launches nothing.  row_ptr that does not ascend gives undefined results, within the buffers. */
+typedef struct {
+  int32_t n_seqs;
+  int32_t n_rows;
+  int32_t n_q_heads;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+} crisp_packed_shape;
+
+/* Which elements of a head are a pair: (i, i + rotary_dim / 2), or (2 i, 2 i + 1). */
+enum { CRISP_ROPE_HALF = 0, CRISP_ROPE_INTERLEAVED = 1 };
+
+/* Angle a token f_i of pair i, from f = base^(-2 i / rotary_dim):
+ *   PLAIN   f
+ *   LINEAR  f / factor (positions interpolated)
+ *   BASE    base' = base factor^(rotary_dim / (rotary_dim - 2)) in place of base (high frequencies stay, low ones stretch)
+ *   BANDS   f (x + (1 - x) / factor), x = (turns - low) / (high - low) held to [0, 1], turns = original_len f / (2 pi)
+ *   RAMP    the same with x falling from 1 to 0 along i, between the pairs that make `high` (rounded down, >= 0) and `low` (rounded
+ *           up, <= rotary_dim - 1) turns in original_len, at i = rotary_dim ln(original_len / (2 pi turns)) / (2 ln base); rotated
+ *           elements are multiplied by 0.1 ln(factor) + 1 (YaRN, arXiv 2309.00071) */
+enum { CRISP_ROPE_PLAIN = 0, CRISP_ROPE_LINEAR = 1, CRISP_ROPE_BASE = 2, CRISP_ROPE_BANDS = 3, CRISP_ROPE_RAMP = 4 };
+
+/* rotary_dim a multiple of 16 in [16, 128] (the elements behind it stay as they are), base > 1, factor >= 1 (not PLAIN's),
+ * original_len > 0 and 0 < low < high (BANDS and RAMP), all finite. */
+typedef struct {
+  int32_t rotary_dim;
+  int32_t layout;
+  int32_t scaling;
+  double base, factor, original_len, low, high;
+} crisp_rope_params;
+
+/* What crisp_rope takes: turns[i] = f_i / (2 pi) of the rotary_dim / 2 pairs, and the gain of rotated elements.  Filled by
+ * crisp_rope_init, or by a caller with frequencies of its own. */
+typedef struct {
+  int32_t rotary_dim;
+  int32_t layout;
+  float gain;
+  double turns[64];
+} crisp_rope_table;
+
+/* Host only. */
+crisp_status crisp_rope_init(const crisp_rope_params* params, crisp_rope_table* table);
+
+/* Row r of sequence s stands at position p = start[s] + r - row_ptr[s] (start int32[n_seqs], any values); its pairs (x1, x2), of every
+ * head of q and k, become
+ *   y1 = gain (x1 cos a - x2 sin a),  y2 = gain (x2 cos a + x1 sin a),  a = 2 pi p turns[i]
+ * with p turns[i] and its fraction in 64 bits, the rest in 32, rounded once.  q_out may be q, with its strides, and k_out k;
+ * otherwise outputs and inputs do not overlap.  n_q_heads or n_kv_heads may be 0. */
+crisp_status crisp_rope(const crisp_packed_shape* shape, const crisp_rope_table* table, const int32_t* start,
+                        const int32_t* row_ptr, const crisp_bf16* q, int64_t q_head_stride, int64_t q_row_stride,
+                        const crisp_bf16* k, int64_t k_head_stride, int64_t k_row_stride, crisp_bf16* q_out,
+                        int64_t q_out_head_stride, int64_t q_out_row_stride, crisp_bf16* k_out,
+                        int64_t k_out_head_stride, int64_t k_out_row_stride, crisp_stream stream);
+
+/* Causal attention of whole prompts: a row sees the rows of its sequence up to itself,
+ *   o[h][r] = sum_{row_ptr[s] <= j <= r} softmax_j(softmax_scale q[h][r] . k_j) v_j.
+ * Query head h reads KV head h / (H_q / H_kv); softmax_scale 0 means 1/sqrt(128).  Scores and sums are 32-bit floats, the probabilities
+ * are rounded to bf16 before they meet v, and their sum is that of the rounded ones.  Infinities and NaN in q, k and v reach the rows that
+ * see them and no others.  The same arguments give the same bits.  Row strides of k and v are below 2^23; no workspace. */
+crisp_status crisp_packed_attn(const crisp_packed_shape* shape, float softmax_scale, const int32_t* row_ptr,
+                               const crisp_bf16* q, int64_t q_head_stride, int64_t q_row_stride, const crisp_bf16* k,
+                               int64_t k_head_stride, int64_t k_row_stride, const crisp_bf16* v, int64_t v_head_stride,
+                               int64_t v_row_stride, crisp_bf16* o, int64_t o_head_stride, int64_t o_row_stride,
+                               crisp_stream stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Eviction from the K/V cache by accumulated attention weight: the weight that each cached token has had from the rows
+ * so far, the choice of the tokens that stay, for each KV head on its own, and their move to pages of their own.
+ *   weights float[n_seqs][H_kv][width], of which those of positions below held[s] (int32[n_seqs]) count; the others are 0
+ * whatever the buffer holds, so that it needs no contents before the first call, held then being 0. */
+
+/* Host only.  Bytes of workspace (256-byte aligned, any contents) of crisp_cache_weights: enough for n_rows that are smaller as well,
+ * whatever max_pages. */
+crisp_status crisp_cache_weights_workspace_size(const crisp_cache_shape* cache, const crisp_cache_batch* batch,
+                                                int32_t n_q_heads, size_t* bytes);
+
+/* For each sequence, KV head g and position j < min(seq_len[s] + its rows, width)
+ *   out[s][g][j] = (j < held[s] ? weights[s][g][j] : 0) + sum_{h of g, rows r with j <= t(r)} softmax_j(softmax_scale q[h][r] . k_j),
+ * the rows and the positions that they see being crisp_cache_attn's (appended before; the sum of a position without a page is 0).  All in
+ * 32 bits and in a fixed order.  out may be weights, or does not overlap it; positions behind stay as they were.  A row of q that is not
+ * finite makes the sums of what it sees NaN.  Afterwards seq_len[s] + its rows is the next call's held[s]. */
+crisp_status crisp_cache_weights(const crisp_cache_shape* cache, const crisp_cache_batch* batch, int32_t n_q_heads,
+                                 float softmax_scale, const uint8_t* pages, const float* scales, const int32_t* table,
+                                 const int32_t* seq_len, const int32_t* row_ptr, const crisp_bf16* q,
+                                 int64_t q_head_stride, int64_t q_row_stride, const float* weights, float* out,
+                                 int32_t width, const int32_t* held, void* workspace, size_t workspace_bytes,
+                                 crisp_stream stream);
+
+/* For each sequence of n = seq_len[s] <= width tokens with 0 < keep[s] < n and keep[s] <= cap, and each KV head, the m = keep[s]
+ * positions that stay: the last min(recent, m), the first min(sink, what is left of m), and of those between the ones with the
+ * largest weights (ties: the lowest position; NaN below all).  kept int32[n_seqs][H_kv][cap] receives them in ascending order, -1 behind them;
+ * count[s] = m.  Other sequences stay as they are: count 0, kept -1.  new_weights_or_null float[n_seqs][H_kv][width] receives the
+ * weights of the positions that stay in places 0 .. m - 1, the rest of it stays as it was; it may be weights, or does not overlap
+ * it.  width and cap in [1, 2^30]; n_kv_heads <= 65535, sink and recent >= 0. */
+crisp_status crisp_cache_keep(int32_t n_seqs, int32_t n_kv_heads, int32_t width, const float* weights, const int32_t* held,
+                              const int32_t* seq_len, const int32_t* keep, int32_t sink, int32_t recent, int32_t cap,
+                              int32_t* kept, int32_t* count, float* new_weights_or_null, crisp_stream stream);
+
+/* The kept tokens of each sequence, KV head by KV head, to pages of their own: position i < min(count[s], cap) of the row of new_table
+ * (int32[n_seqs][new_pages]) becomes what position kept[s][g][i] of the row of table holds, as if its cached K and V were
+ * appended: a page's exponent is the smallest that holds all values in it, codes are rounded to nearest even under it, NaN is 0.
+ * Places behind count in the last page become 0, as do those whose kept position is out of range or has no page.  The pages of new_table are
+ * distinct and none of table's; positions without a page there are dropped.  batch->n_rows is not read. */
+crisp_status crisp_cache_gather(const crisp_cache_shape* cache, const crisp_cache_batch* batch, uint8_t* pages,
+                                float* scales, const int32_t* table, const int32_t* kept, int32_t cap,
+                                const int32_t* count, const int32_t* new_table, int32_t new_pages, crisp_stream stream);
 
 /* Static name of a status code. */
 const char* crisp_status_string(crisp_status status);

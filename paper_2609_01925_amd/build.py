@@ -37,7 +37,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"-I{INCLUDE}", f"-I{CSRC}", "-Wall", "-
 # VGPRs; left to itself the compiler places them in AGPRs and copies every score out
 # again.
 EXTRA = {"attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "estimate.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
-         "cache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+         "cache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"], "packed_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+         "cache_weights.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def hipcc() -> str:

@@ -42,6 +42,22 @@ class CrispCacheShape(ctypes.Structure):
                 ("block", ctypes.c_int32), ("format", ctypes.c_int32)]
 
 
+class CrispPackedShape(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class CrispRopeParams(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double), ("original_len", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class CrispRopeTable(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("gain", ctypes.c_float),
+                ("turns", ctypes.c_double * 64)]
+
+
 class CrispCacheBatch(ctypes.Structure):
     _fields_ = [("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_rows", ctypes.c_int32)]
 
@@ -59,6 +75,7 @@ def _load(path: str = _LIB_PATH):
     P, F, I32, I64, SZ = ctypes.c_void_p, ctypes.c_float, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     sh, pa = ctypes.POINTER(CrispShape), ctypes.POINTER(CrispParams)
     cs, cb = ctypes.POINTER(CrispCacheShape), ctypes.POINTER(CrispCacheBatch)
+    ps, rt = ctypes.POINTER(CrispPackedShape), ctypes.POINTER(CrispRopeTable)
     sig = {
         "crisp_params_default": (None, [pa]),
         "crisp_col_capacity": (I64, [sh]),
@@ -83,6 +100,13 @@ def _load(path: str = _LIB_PATH):
         "crisp_pool_fork": (ctypes.c_int, [I32, I32, I32, I32, P, P, P, P, P, I32, P, P]),
         "crisp_pool_free": (ctypes.c_int, [I32, I32, I32, P, P, P, P, I32, P]),
         "crisp_pool_compact": (ctypes.c_int, [I32, I32, I32, P, P, P, P, P]),
+        "crisp_rope_init": (ctypes.c_int, [ctypes.POINTER(CrispRopeParams), rt]),
+        "crisp_rope": (ctypes.c_int, [ps, rt, P, P, P, I64, I64, P, I64, I64, P, I64, I64, P, I64, I64, P]),
+        "crisp_packed_attn": (ctypes.c_int, [ps, F, P, P, I64, I64, P, I64, I64, P, I64, I64, P, I64, I64, P]),
+        "crisp_cache_weights_workspace_size": (ctypes.c_int, [cs, cb, I32, ctypes.POINTER(SZ)]),
+        "crisp_cache_weights": (ctypes.c_int, [cs, cb, I32, F, P, P, P, P, P, P, I64, I64, P, P, I32, P, P, SZ, P]),
+        "crisp_cache_keep": (ctypes.c_int, [I32, I32, I32, P, P, P, P, I32, I32, I32, P, P, P, P]),
+        "crisp_cache_gather": (ctypes.c_int, [cs, cb, P, P, P, P, I32, P, P, I32, P]),
         "crisp_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "crisp_last_error": (ctypes.c_char_p, []),
     }
@@ -99,7 +123,8 @@ EXPORTED = ("crisp_params_default", "crisp_col_capacity", "crisp_workspace_size"
             "crisp_sparse_attn_noalloc", "crisp_prefill_attn", "crisp_dense_attn", "crisp_status_string", "crisp_last_error",
             "crisp_cache_bytes", "crisp_cache_append", "crisp_cache_attn_workspace_size", "crisp_cache_attn",
             "crisp_cache_copy", "crisp_pool_words", "crisp_pool_init", "crisp_pool_reserve", "crisp_pool_fork",
-            "crisp_pool_free", "crisp_pool_compact")
+            "crisp_pool_free", "crisp_pool_compact", "crisp_rope_init", "crisp_rope", "crisp_packed_attn",
+            "crisp_cache_weights_workspace_size", "crisp_cache_weights", "crisp_cache_keep", "crisp_cache_gather")
 
 # route_mode / vs_mode values (include/crisp.h)
 ROUTE_BY_CSTRUCT, ROUTE_BY_JSD = 0, 1
@@ -107,6 +132,9 @@ VS_FLOOR, VS_GAMMA = 0, 1
 FLOOR_MEAN, FLOOR_MEDIAN = 0, 1
 # cache formats
 CACHE_E4M3, CACHE_INT8 = 0, 1
+# pairs of elements and frequency rules of rotary positions
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
 
 
 def _check(status: int, what: str):
@@ -342,6 +370,69 @@ def crisp_prefill_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, params
     return (o, route, row_ptr, col_idx) if return_lists else o
 
 
+# ---------------------------------------------------------------- packed rows of several sequences
+
+
+def make_rope(rotary_dim: int = 128, layout: int = ROPE_HALF, base: float = 10000.0, scaling: int = ROPE_PLAIN,
+              factor: float = 1.0, original_len: float = 0.0, low: float = 0.0, high: float = 0.0) -> CrispRopeTable:
+    """The frequencies that crisp_rope takes, by the rules of include/crisp.h."""
+    table = CrispRopeTable()
+    params = CrispRopeParams(rotary_dim, layout, scaling, base, factor, original_len, low, high)
+    _check(lib.crisp_rope_init(ctypes.byref(params), ctypes.byref(table)), "crisp_rope_init")
+    return table
+
+
+def crisp_rope(rope: CrispRopeTable, start: torch.Tensor, row_ptr: torch.Tensor, q: torch.Tensor,
+               k: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+               k_out: Optional[torch.Tensor] = None):
+    """Rotary positions on rows row_ptr[s] .. row_ptr[s + 1] of q [H_q, n_rows, 128] and k [H_kv, n_rows, 128], the first of them at
+    position start[s] -> (q_out, k_out), new contiguous tensors unless given (q or k themselves: in place; rows that row_ptr
+    does not cover are left as they were)."""
+    gpu = q.get_device()
+    if gpu < 0:
+        raise ValueError(f"q must be a CUDA tensor, got one on {q.device}")
+    heads, n, qh, qr = _rows(q, "q", None, gpu)
+    o = torch.empty((heads, n, 128), dtype=torch.bfloat16, device=q.device) if q_out is None else q_out
+    _, m, oh, orow = _rows(o, "q_out", heads, gpu)
+    kv, kh, kr, p, ph, pr = 0, 0, 0, None, 0, 0
+    if k is not None:
+        kv, mk, kh, kr = _rows(k, "k", None, gpu)
+        p = torch.empty((kv, n, 128), dtype=torch.bfloat16, device=q.device) if k_out is None else k_out
+        _, mp, ph, pr = _rows(p, "k_out", kv, gpu)
+    if m != n or (k is not None and (mk != n or mp != n)):
+        raise ValueError(f"q {tuple(q.shape)}, k and their outputs must have the same number of rows")
+    n_seqs, = _i32(start, "start", 1, gpu)
+    _i32_of(row_ptr, "row_ptr", (n_seqs + 1,), gpu)
+    _call(gpu, "crisp_rope", lib.crisp_rope, CrispPackedShape(n_seqs, n, heads, kv, 128), rope, start.data_ptr(),
+          row_ptr.data_ptr(), q.data_ptr(), qh, qr, None if k is None else k.data_ptr(), kh, kr, o.data_ptr(), oh, orow,
+          None if k is None else p.data_ptr(), ph, pr)
+    return o, p
+
+
+def crisp_packed_attn(row_ptr: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, softmax_scale: float = 0.0,
+                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention of whole prompts, rows row_ptr[s] .. row_ptr[s + 1] of q [H_q, n_rows, 128], k and v [H_kv, n_rows, 128] (any
+    head and row strides that are multiples of 8) -> o bf16 [H_q, n_rows, 128]; rows that row_ptr does not cover are left as
+    they were in out."""
+    gpu = q.get_device()
+    if gpu < 0:
+        raise ValueError(f"q must be a CUDA tensor, got one on {q.device}")
+    heads, n, qh, qr = _rows(q, "q", None, gpu)
+    kv, m, kh, kr = _rows(k, "k", None, gpu)
+    _, m2, vh, vr = _rows(v, "v", kv, gpu)
+    o = torch.empty((heads, n, 128), dtype=torch.bfloat16, device=q.device) if out is None else out
+    _, m3, oh, orow = _rows(o, "out", heads, gpu)
+    if not n == m == m2 == m3:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)} and out {tuple(o.shape)} must have the same "
+                         "number of rows")
+    ends, = _i32(row_ptr, "row_ptr", 1, gpu)
+    if ends < 1:
+        raise ValueError("row_ptr must hold the sequences' n_seqs + 1 offsets")
+    _call(gpu, "crisp_packed_attn", lib.crisp_packed_attn, CrispPackedShape(ends - 1, n, heads, kv, 128), softmax_scale,
+          row_ptr.data_ptr(), q.data_ptr(), qh, qr, k.data_ptr(), kh, kr, v.data_ptr(), vh, vr, o.data_ptr(), oh, orow)
+    return o
+
+
 # ---------------------------------------------------------------- the 8-bit paged K/V cache
 
 
@@ -469,6 +560,83 @@ def crisp_cache_attn(cache: Cache, table: torch.Tensor, seq_len: torch.Tensor, r
           cache.scales.data_ptr(), table.data_ptr(), seq_len.data_ptr(), row_ptr.data_ptr(), q.data_ptr(), qh, qr,
           o.data_ptr(), oh, orow, ws.data_ptr(), ws.numel())
     return o
+
+
+def _f32(t: torch.Tensor, name: str, shape, gpu: int) -> None:
+    if t.dtype is not torch.float32 or t.shape != shape or t.get_device() != gpu or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous float32 tensor {tuple(shape)} on cuda:{gpu}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def cache_weights_workspace(cache: Cache, n_q_heads: int, n_seqs: int, n_rows: int) -> torch.Tensor:
+    """A workspace for crisp_cache_weights calls of n_seqs sequences and up to n_rows rows, in a table of any width."""
+    n = ctypes.c_size_t()
+    _check(lib.crisp_cache_weights_workspace_size(ctypes.byref(cache.shape), ctypes.byref(CrispCacheBatch(n_seqs, 0, n_rows)),
+                                                  n_q_heads, ctypes.byref(n)), "crisp_cache_weights_workspace_size")
+    return torch.empty(max(int(n.value), 256), dtype=torch.uint8, device=cache.pages.device)
+
+
+def crisp_cache_weights(cache: Cache, table: torch.Tensor, seq_len: torch.Tensor, row_ptr: torch.Tensor, q: torch.Tensor,
+                        weights: torch.Tensor, held: torch.Tensor, softmax_scale: float = 0.0,
+                        out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The attention weight that each cached token gets from rows q [H_q, n_rows, 128] (their K appended before), summed over the rows
+    and the query heads of its KV head, added to weights float32 [n_seqs, H_kv, width], of which the positions below held int32
+    [n_seqs] count -> out, which is weights unless given."""
+    gpu = cache._gpu
+    heads, n, qh, qr = _rows(q, "q", None, gpu)
+    b = _batch(gpu, table, seq_len, row_ptr, n)
+    _i32_of(held, "held", (b.n_seqs,), gpu)
+    wide = weights.shape[-1] if weights.dim() else 0
+    _f32(weights, "weights", (b.n_seqs, cache.n_kv_heads, wide), gpu)
+    if out is None:
+        out = weights
+    else:
+        _f32(out, "out", weights.shape, gpu)
+    if ws is None:
+        ws = cache_weights_workspace(cache, heads, b.n_seqs, n)
+    elif ws.dtype is not torch.uint8 or ws.get_device() != gpu or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous uint8 tensor on cuda:{gpu}, got {ws.dtype} on {ws.device}")
+    _call(gpu, "crisp_cache_weights", lib.crisp_cache_weights, cache._ref, b, heads, softmax_scale, cache.pages.data_ptr(),
+          cache.scales.data_ptr(), table.data_ptr(), seq_len.data_ptr(), row_ptr.data_ptr(), q.data_ptr(), qh, qr,
+          weights.data_ptr(), out.data_ptr(), wide, held.data_ptr(), ws.data_ptr(), ws.numel())
+    return out
+
+
+def crisp_cache_keep(weights: torch.Tensor, held: torch.Tensor, seq_len: torch.Tensor, keep: torch.Tensor, cap: int,
+                     sink: int = 4, recent: int = 64, new_weights: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The keep[s] < seq_len[s] positions of each sequence and KV head that stay: the last `recent`, the first `sink`, and those with
+    the largest weights -> (kept int32 [n_seqs, H_kv, cap], ascending, -1 behind them; count int32 [n_seqs], 0 for a sequence that
+    stays as it is).  new_weights (weights itself, or another) receives their weights."""
+    gpu = weights.get_device()
+    if gpu < 0 or weights.dim() != 3:
+        raise ValueError(f"weights must be a 3-d CUDA tensor, got {tuple(weights.shape)} on {weights.device}")
+    _f32(weights, "weights", weights.shape, gpu)
+    n_seqs, heads, wide = weights.shape
+    for t, name in ((held, "held"), (seq_len, "seq_len"), (keep, "keep")):
+        _i32_of(t, name, (n_seqs,), gpu)
+    if new_weights is not None:
+        _f32(new_weights, "new_weights", weights.shape, gpu)
+    kept = torch.empty((n_seqs, heads, max(cap, 0)), dtype=torch.int32, device=weights.device)
+    count = torch.empty(n_seqs, dtype=torch.int32, device=weights.device)
+    _call(gpu, "crisp_cache_keep", lib.crisp_cache_keep, n_seqs, heads, wide, weights.data_ptr(), held.data_ptr(),
+          seq_len.data_ptr(), keep.data_ptr(), sink, recent, cap, kept.data_ptr(), count.data_ptr(),
+          None if new_weights is None else new_weights.data_ptr())
+    return kept, count
+
+
+def crisp_cache_gather(cache: Cache, table: torch.Tensor, kept: torch.Tensor, count: torch.Tensor, new_table: torch.Tensor) -> None:
+    """The first count[s] tokens of kept int32 [n_seqs, H_kv, cap], positions of table's rows, KV head by KV head to the pages of
+    new_table int32 [n_seqs, new_pages]."""
+    gpu = cache._gpu
+    n_seqs, wide = _i32(table, "table", 2, gpu)
+    cap = kept.shape[-1] if kept.dim() else 0
+    _i32_of(kept, "kept", (n_seqs, cache.n_kv_heads, cap), gpu)
+    _i32_of(count, "count", (n_seqs,), gpu)
+    m, new_pages = _i32(new_table, "new_table", 2, gpu)
+    if m != n_seqs:
+        raise ValueError(f"new_table must have a row for each of {n_seqs} sequences, got {tuple(new_table.shape)}")
+    _call(gpu, "crisp_cache_gather", lib.crisp_cache_gather, cache._ref, CrispCacheBatch(n_seqs, wide, 0), cache.pages.data_ptr(),
+          cache.scales.data_ptr(), table.data_ptr(), kept.data_ptr(), cap, count.data_ptr(), new_table.data_ptr(), new_pages)
 
 
 def crisp_cache_copy(cache: Cache, pairs: torch.Tensor, count: Optional[torch.Tensor] = None) -> None:

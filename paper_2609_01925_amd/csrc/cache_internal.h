@@ -55,6 +55,35 @@ hipError_t launch_cache_attn(const CacheDims& c, const BatchDims& b, const Seqs&
                              const uint16_t* q, Strides qs, const uint8_t* pages, const float* scales, uint16_t* o,
                              Strides os, void* ws, hipStream_t stream);
 
+size_t cache_weights_bytes(const CacheDims& c, const BatchDims& b, int hq);  // of launch_cache_weights's workspace
+hipError_t launch_cache_weights(const CacheDims& c, const BatchDims& b, const Seqs& s, int hq, float scale, const uint16_t* q,
+                                Strides qs, const uint8_t* pages, const float* scales, const float* weights, float* out,
+                                int width, const int32_t* held, void* ws, hipStream_t stream);
+
+struct KeepArgs {
+  int n_seqs, hkv, width, sink, recent, cap;
+  const float* weights;  // [n_seqs][hkv][width]
+  const int32_t* held;
+  const int32_t* seq_len;
+  const int32_t* keep;
+  int32_t* kept;         // [n_seqs][hkv][cap]
+  int32_t* count;
+  float* new_weights;    // as weights, which it may be; or null
+};
+hipError_t launch_cache_keep(const KeepArgs& a, hipStream_t stream);
+
+struct GatherArgs {
+  CacheDims c;
+  int n_seqs, max_pages, new_pages, cap;
+  uint8_t* pages;
+  float* scales;
+  const int32_t* table;      // [n_seqs][max_pages]
+  const int32_t* kept;       // [n_seqs][hkv][cap]
+  const int32_t* count;
+  const int32_t* new_table;  // [n_seqs][new_pages]
+};
+hipError_t launch_cache_gather(const GatherArgs& a, hipStream_t stream);
+
 // Page bookkeeping: pool = uses of each page [n_pages], then one bit a page in use, lowest first.
 constexpr int kPoolMaxSeqs = 4096;  // sequences (reserve) and forks of one call: their sums live in LDS
 inline int64_t pool_words(int64_t n_pages) { return n_pages + (n_pages + 31) / 32; }

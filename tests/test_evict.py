@@ -1,0 +1,499 @@
+"""Eviction from the K/V cache by accumulated attention weight through the public binding, against the 64-bit oracle
+(tests/packed_oracle.py): weights within counted roundings, the choice and the gathered pages bit for bit; lengths from one token to
+many tiles, ragged batches, holes, budgets from one token to all but one, ties, values that are not finite, graphs."""
+import math
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from tests import cache_oracle as O
+from tests import packed_oracle as R
+from tests.helpers import to_f64
+from tests.test_cache import _append, _check_written, _new, _ptr, _rand, _table
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+FORMATS = [O.E4M3, O.INT8]
+
+
+def _crisp():
+    from paper_2609_01925_amd import crisp as C
+    return C
+
+
+def _say(msg):
+    print(f"[gpu-case] {msg}", flush=True)
+    sys.stdout.flush()
+
+
+def _ints(x):
+    return torch.tensor(np.asarray(x, dtype=np.int32), device=DEV)
+
+
+def _floats(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(DEV)
+
+
+def _filled(C, lens, heads, block, fmt, seed, spread=None, extra=2, width=None):
+    """A cache on both sides that holds `lens` tokens of each sequence; spread: powers of two that rows differ by."""
+    rng = np.random.default_rng(seed)
+    table, n_pages = _table(lens, block, rng, extra=extra, width=width)
+    c, oracle = _new(C, n_pages, heads, block, fmt)
+    n = sum(lens)
+    k, v = _rand(heads, n, seed), _rand(heads, n, seed + 1)
+    if spread:
+        by = torch.from_numpy(2.0 ** rng.integers(-spread, spread + 1, n)).float()[None, :, None]
+        k, v = (k.float() * by).to(torch.bfloat16), (v.float() * by).to(torch.bfloat16)
+    _append(C, c, oracle, table, [0] * len(lens), lens, k, v)
+    return c, oracle, table, n_pages
+
+
+# ------------------------------------------------------------------ weights
+
+
+def _check_weights(C, c, oracle, table, lens, counts, hq, held=None, width=None, scale=0.0, seed=0, gain=1.0):
+    """lens: tokens before the rows (their K is in the cache as well)."""
+    ptr = _ptr(counts)
+    heads = oracle.codes.shape[1]
+    width = table.shape[1] * oracle.block if width is None else width
+    rng = np.random.default_rng(seed)
+    w = rng.random((len(lens), heads, width)).astype(np.float32)
+    held = [0] * len(lens) if held is None else held
+    for s, h in enumerate(held):  # what does not count may be anything
+        w[s, :, max(h, 0):] = math.nan
+    q = _rand(hq, int(ptr[-1]) + 3, seed + 5, gain)
+    out = torch.full(w.shape, 7.0, dtype=torch.float32, device=DEV)
+    got = C.crisp_cache_weights(c, _ints(table), _ints(lens), _ints(ptr), q.to(DEV), _floats(w), _ints(held), scale, out)
+    assert got is out
+    want, tol = R.cache_weights(oracle, table, lens, ptr, to_f64(q), scale or 1 / math.sqrt(128), w.astype(np.float64), held)
+    y = to_f64(out)
+    live = ~np.isnan(want)
+    assert np.isfinite(y[live]).all() and (y[~live] == 7.0).all()
+    worst = np.max(np.abs(y - want)[live] / tol[live], initial=0.0)
+    assert worst <= 1.0, f"{worst:.3f} of the tolerance"
+    inplace = _floats(w)
+    C.crisp_cache_weights(c, _ints(table), _ints(lens), _ints(ptr), q.to(DEV), inplace, _ints(held), scale)
+    assert torch.equal(inplace[torch.from_numpy(live).to(DEV)], out[torch.from_numpy(live).to(DEV)])
+    return out
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n", [0, 1, 15, 63, 64, 65, 127, 128, 200, 255, 256, 257, 1000])
+def test_weights_of_a_step(n, fmt):
+    C = _crisp()
+    _say(f"weights n={n} fmt={fmt}")
+    c, oracle, table, _ = _filled(C, [n + 1], 2, 64, fmt, n)
+    _check_weights(C, c, oracle, table, [n], [1], 8, held=[n], seed=n)
+
+
+@pytest.mark.parametrize("hq,heads", [(1, 1), (2, 2), (3, 1), (7, 1), (16, 1), (17, 1), (40, 2), (8, 8)])
+def test_weights_head_layouts(hq, heads):
+    C = _crisp()
+    _say(f"weights heads={hq},{heads}")
+    c, oracle, table, _ = _filled(C, [131, 40], heads, 64, O.E4M3, hq)
+    _check_weights(C, c, oracle, table, [128, 33], [3, 7], hq, held=[100, 33], seed=hq)
+
+
+@pytest.mark.parametrize("rows", [2, 9, 16, 33, 128, 129, 260])
+@pytest.mark.parametrize("block", [64, 128])
+def test_weights_of_many_rows(rows, block):
+    """More pairs of row and head than one pass holds; rows that end inside tiles."""
+    C = _crisp()
+    _say(f"weights rows={rows} block={block}")
+    lens = [70, 0, 301]
+    counts = [rows, 1, max(1, rows // 3)]
+    c, oracle, table, _ = _filled(C, [a + b for a, b in zip(lens, counts)], 2, block, O.INT8, rows)
+    _check_weights(C, c, oracle, table, lens, counts, 6, held=[70, 0, 5], seed=rows)
+
+
+def test_weights_of_a_ragged_batch():
+    """Sequences without rows, without tokens, more than a wave looks over; nothing held, some held, more held than there is."""
+    C = _crisp()
+    _say("weights ragged batch")
+    rng = np.random.default_rng(3)
+    lens = rng.integers(0, 400, 70).tolist()
+    counts = rng.integers(0, 4, 70).tolist()
+    c, oracle, table, _ = _filled(C, [a + b for a, b in zip(lens, counts)], 1, 64, O.E4M3, 3)
+    _check_weights(C, c, oracle, table, lens, counts, 4, held=[int(rng.integers(-5, 500)) for _ in lens], seed=3)
+
+
+@pytest.mark.parametrize("width", [1, 63, 64, 100, 129, 400])
+def test_weights_narrow_and_wide_buffers(width):
+    """Positions past the width are dropped (they still count in the softmax); a width past the table's reach is served too."""
+    C = _crisp()
+    _say(f"weights width={width}")
+    c, oracle, table, _ = _filled(C, [200, 131], 2, 64, O.E4M3, width)
+    _check_weights(C, c, oracle, table, [198, 130], [2, 1], 4, held=[50, 130], width=width, seed=width)
+
+
+def test_weights_of_a_long_history_in_chunks():
+    C = _crisp()
+    _say("weights 20000 tokens")
+    c, oracle, table, _ = _filled(C, [20003], 1, 128, O.E4M3, 7)
+    _check_weights(C, c, oracle, table, [20000], [3], 7, held=[19990], seed=7)
+
+
+def test_weights_many_rows_keep_few_chunks():
+    """So many pairs that the statistics of the chunks would pass the workspace's bound."""
+    C = _crisp()
+    _say("weights 9000 rows")
+    c, oracle, table, _ = _filled(C, [700], 1, 64, O.INT8, 8)
+    heads, n = 300, 699
+    ptr = [0, 1]
+    q = _rand(heads, 9000, 3)
+    w, held = torch.zeros(1, 1, 704, device=DEV), _ints([0])
+    got = C.crisp_cache_weights(c, _ints(table), _ints([n]), _ints(ptr), q.to(DEV), w, held)
+    want, tol = R.cache_weights(oracle, table, [n], ptr, to_f64(q[:, :1]), 1 / math.sqrt(128), np.zeros((1, 1, 704)), [0])
+    live = ~np.isnan(want)
+    assert (np.abs(to_f64(got) - want)[live] <= tol[live]).all()
+
+
+def test_weights_holes_and_bad_pages():
+    """Positions without a page take no weight, and their places say so."""
+    C = _crisp()
+    _say("weights holes")
+    c, oracle, table, n_pages = _filled(C, [400, 130], 2, 64, O.E4M3, 4)
+    table[0, 1], table[0, 4], table[1, 0] = -1, n_pages + 7, -1
+    _check_weights(C, c, oracle, table, [398, 129], [2, 1], 4, held=[300, 129], seed=4)
+    table[1] = -1
+    _check_weights(C, c, oracle, table, [398, 129], [2, 1], 4, held=[300, 129], seed=4)
+
+
+@pytest.mark.parametrize("gain,scale", [(30.0, 0.0), (1e-3, 0.0), (1.0, 3.0), (1.0, 1e-30)])
+def test_weights_sharp_and_flat_scores(gain, scale):
+    C = _crisp()
+    _say(f"weights gain={gain} scale={scale}")
+    c, oracle, table, _ = _filled(C, [520], 2, 64, O.E4M3, 6, spread=3)
+    _check_weights(C, c, oracle, table, [510], [10], 4, scale=scale, seed=6, gain=gain)
+
+
+def test_weights_not_finite():
+    """A row that is not finite makes the sums of what it sees NaN: its own KV head's and sequence's, up to its position."""
+    C = _crisp()
+    _say("weights not finite")
+    c, oracle, table, _ = _filled(C, [150, 90], 2, 64, O.E4M3, 9)
+    lens, counts = [140, 88], [10, 2]
+    for bad in (math.nan, math.inf):
+        q = _rand(4, 12, 1)
+        w, held = torch.zeros(2, 2, 192, device=DEV), _ints([0, 0])
+        clean = C.crisp_cache_weights(c, _ints(table), _ints(lens), _ints(_ptr(counts)), q.to(DEV), w, held, out=torch.zeros_like(w))
+        q[1, 4, 9] = bad
+        got = C.crisp_cache_weights(c, _ints(table), _ints(lens), _ints(_ptr(counts)), q.to(DEV), w, held, out=torch.zeros_like(w))
+        assert torch.isnan(got[0, 0, :145]).all()
+        got[0, 0, :145], clean[0, 0, :145] = 0, 0
+        assert torch.equal(got, clean)
+
+
+def test_weights_strides_repeat_and_workspaces():
+    C = _crisp()
+    _say("weights strides, workspaces")
+    c, oracle, table, _ = _filled(C, [333], 2, 64, O.E4M3, 2)
+    x = _rand(6, 20, 3).to(DEV)
+    view = x.transpose(0, 1).contiguous().transpose(0, 1)
+    w, held, args = torch.zeros(1, 2, 384, device=DEV), _ints([0]), (_ints(table), _ints([313]), _ints([0, 20]))
+    want = C.crisp_cache_weights(c, *args, x, w, held, out=torch.zeros_like(w))
+    ws = C.cache_weights_workspace(c, 6, 1, 1000)
+    for q in (x, view):
+        for space in (None, ws):
+            assert torch.equal(C.crisp_cache_weights(c, *args, q, w, held, out=torch.zeros_like(w), ws=space), want)
+    one = x[:1].expand(6, 20, 128)
+    assert torch.equal(C.crisp_cache_weights(c, *args, one, w, held, out=torch.zeros_like(w)),
+                       C.crisp_cache_weights(c, *args, one.contiguous(), w, held, out=torch.zeros_like(w)))
+
+
+def test_weights_sum_to_the_rows():
+    """Every row's weights sum to one: in all the pairs of row and head."""
+    C = _crisp()
+    _say("weights sum")
+    c, oracle, table, _ = _filled(C, [3000, 64], 2, 64, O.E4M3, 5)
+    w = torch.zeros(2, 2, 3008, device=DEV)
+    C.crisp_cache_weights(c, _ints(table), _ints([2991, 60]), _ints([0, 9, 13]), _rand(8, 13, 1).to(DEV), w, _ints([0, 0]))
+    got = w.double().sum(-1).cpu().numpy()
+    # a row's sum is off by its weights' errors: (3000 / 16 + 64) 2^-24 + 2^-21 and 2 dS, of scores below 2^5: under 2^-13
+    np.testing.assert_allclose(got, [[36.0, 36.0], [16.0, 16.0]], rtol=2.0 ** -13)
+
+
+# ------------------------------------------------------------------ which tokens stay
+
+
+def _check_keep(C, w, held, lens, keep, cap, sink, recent):
+    kept, count, new, moved = R.cache_keep(w, held, lens, keep, cap, sink, recent)
+    out = torch.full(w.shape, 7.0, dtype=torch.float32, device=DEV)
+    a, b = C.crisp_cache_keep(_floats(w), _ints(held), _ints(lens), _ints(keep), cap, sink, recent, out)
+    np.testing.assert_array_equal(b.cpu().numpy(), count)
+    np.testing.assert_array_equal(a.cpu().numpy(), kept)
+    y = out.cpu().numpy()
+    np.testing.assert_array_equal(y[moved], new[moved])
+    assert (y[~moved] == 7.0).all()
+    inplace = _floats(w)
+    a2, _ = C.crisp_cache_keep(inplace, _ints(held), _ints(lens), _ints(keep), cap, sink, recent, inplace)
+    z = inplace.cpu().numpy()
+    np.testing.assert_array_equal(z[moved], new[moved])
+    np.testing.assert_array_equal(z[~moved], w[~moved])
+    a3, _ = C.crisp_cache_keep(_floats(w), _ints(held), _ints(lens), _ints(keep), cap, sink, recent)
+    assert torch.equal(a, a2) and torch.equal(a, a3)
+
+
+@pytest.mark.parametrize("n", [2, 3, 64, 65, 500, 1024, 1025])
+def test_keep_every_kind_of_budget(n):
+    C = _crisp()
+    _say(f"keep n={n}")
+    rng = np.random.default_rng(n)
+    for m in sorted({1, 2, n // 3 + 1, n - 1}):
+        for sink, recent in ((0, 0), (4, 16), (1, 0), (0, 1), (n, n), (3, n), (n, 2)):
+            if m < n:
+                _check_keep(C, rng.random((1, 2, n + 5)).astype(np.float32), [n], [n], [m], m + 3, sink, recent)
+
+
+def test_keep_ties_and_special_values():
+    """Equal weights go to the lowest positions; 0 and -0 are equal, NaN is below all, what is not held counts as 0."""
+    C = _crisp()
+    _say("keep ties")
+    rng = np.random.default_rng(1)
+    n = 3001
+    equal = np.full((1, 1, n), 0.25, dtype=np.float32)
+    few = rng.integers(0, 3, (1, 1, n)).astype(np.float32)
+    zeros = np.where(rng.random((1, 1, n)) < 0.5, 0.0, -0.0).astype(np.float32)
+    mixed = rng.choice(np.array([0.0, -0.0, 1.0, -1.0, np.inf, -np.inf, np.nan, 1e-45, -1e-45, 3.4e38], dtype=np.float32), (1, 1, n))
+    for w in (equal, few, zeros, mixed):
+        for m in (1, 100, 2000, 3000):
+            for held in (n, 1500, 0, -3):
+                _check_keep(C, w, [held], [n], [m], 3000, 2, 5)
+
+
+def test_keep_close_weights():
+    """Weights that differ in the last bit only, every digit of the selection."""
+    C = _crisp()
+    _say("keep close weights")
+    rng = np.random.default_rng(2)
+    bits = np.int32(0x3f000000) + rng.integers(0, 1500, (2, 2, 1400)).astype(np.int32)
+    w = bits.view(np.float32)
+    _check_keep(C, w, [1400, 1400], [1400, 1300], [700, 333], 1000, 4, 30)
+    w = (rng.integers(0, 1 << 31, (1, 3, 5000)).astype(np.uint32) & 0x7f7fffff).view(np.float32)
+    _check_keep(C, w, [5000], [4999], [1234], 1234, 0, 0)
+
+
+def test_keep_batch_of_all_kinds():
+    """Sequences that are short enough already, empty, longer than the buffer, budgets above the list or below one."""
+    C = _crisp()
+    _say("keep batch")
+    rng = np.random.default_rng(4)
+    lens = [0, 1, 5, 300, 299, 300, 301, 200, 77, -4, 250]
+    keep = [3, 1, 5, 100, 299, 300, 100, 0, -1, 2, 151]
+    _check_keep(C, rng.random((11, 2, 300)).astype(np.float32), [1000] * 11, lens, keep, 150, 4, 32)
+
+
+@pytest.mark.parametrize("n,m", [(16384, 5000), (16385, 16384), (40000, 1), (70001, 30000)])
+def test_keep_long_sequences(n, m):
+    """More tokens than the workgroup holds at a time, also in place."""
+    C = _crisp()
+    _say(f"keep n={n} m={m}")
+    rng = np.random.default_rng(n)
+    w = np.exp(3 * rng.standard_normal((1, 2, n))).astype(np.float32)
+    _check_keep(C, w, [n], [n], [m], m, 4, 100)
+
+
+# ------------------------------------------------------------------ the move
+
+
+def _check_gather(C, c, oracle, table, kept, count, new_table):
+    C.crisp_cache_gather(c, _ints(table), _ints(kept), _ints(count), _ints(new_table))
+    R.cache_gather(oracle, table, kept, count, new_table)
+    n_pages = len(oracle.written)
+    got = O.decode(c.pages.cpu().numpy(), c.fmt)
+    new = sorted({int(p) for s, row in enumerate(new_table) for b, p in enumerate(row)
+                  if 0 <= p < n_pages and b * oracle.block < min(count[s], kept.shape[2])})
+    np.testing.assert_array_equal(got[new], oracle.codes[new])
+    np.testing.assert_array_equal(c.scales.cpu().numpy()[new], np.ldexp(1.0, oracle.exp[new]))
+    old = [p for p in range(n_pages) if oracle.written[p].any() and p not in new]
+    at = oracle.written[old]
+    np.testing.assert_array_equal(got[old].transpose(0, 3, 1, 2, 4)[at], oracle.codes[old].transpose(0, 3, 1, 2, 4)[at])
+
+
+def _new_pages(table, n_pages, slots):
+    free = [p for p in range(n_pages) if p not in set(table[table >= 0].tolist())]
+    t = np.array(free[::-1][:table.shape[0] * slots], dtype=np.int32)
+    return t.reshape(table.shape[0], slots)
+
+
+def _some(rng, n, m, heads):
+    return np.stack([np.sort(rng.permutation(n)[:m]) for _ in range(heads)])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("block", [64, 128])
+@pytest.mark.parametrize("n,m", [(2, 1), (64, 63), (65, 64), (200, 65), (300, 129), (500, 20), (129, 128)])
+def test_gather_lengths(n, m, block, fmt):
+    C = _crisp()
+    _say(f"gather n={n} m={m} block={block} fmt={fmt}")
+    rng = np.random.default_rng(n + m)
+    slots = -(-m // block)
+    c, oracle, table, n_pages = _filled(C, [n], 2, block, fmt, n, spread=6, extra=slots + 2)
+    kept = np.full((1, 2, m + 4), -1, dtype=np.int32)
+    kept[0, :, :m] = _some(rng, n, m, 2)
+    _check_gather(C, c, oracle, table, kept, [m], _new_pages(table, n_pages, slots))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_gather_scales_far_apart(fmt):
+    """Pages whose exponents differ by up to 120: small values round to 0 beside large ones and come back to full bits without them."""
+    C = _crisp()
+    _say(f"gather scales fmt={fmt}")
+    rng = np.random.default_rng(5)
+    c, oracle, table, n_pages = _filled(C, [640, 320], 1, 64, fmt, 5, spread=60, extra=14)
+    kept = np.full((2, 1, 300), -1, dtype=np.int32)
+    kept[0, 0, :290], kept[1, 0, :150] = _some(rng, 640, 290, 1), _some(rng, 320, 150, 1)
+    _check_gather(C, c, oracle, table, kept, [290, 150], _new_pages(table, n_pages, 5))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_gather_of_every_code(fmt):
+    """Pages that hold every code, NaN among them, under the smallest and largest scales."""
+    C = _crisp()
+    _say(f"gather codes fmt={fmt}")
+    for e in (-64, 0, 100, 119):
+        c = C.make_cache(6, 1, 64, fmt, device=DEV)
+        oracle = O.Cache(6, 1, 64, fmt)
+        c.pages.copy_(torch.arange(256, dtype=torch.uint8, device=DEV).repeat(c.pages.numel() // 256).view(c.pages.shape))
+        c.scales.fill_(2.0 ** e)
+        oracle.codes[:], oracle.exp[:] = O.decode(c.pages.cpu().numpy(), fmt), e
+        kept = np.arange(0, 128, 2, dtype=np.int32)[None, None]
+        _check_gather(C, c, oracle, np.array([[0, 1]], dtype=np.int32), kept, [64], np.array([[3]], dtype=np.int32))
+
+
+def test_gather_largest_values():
+    """The largest bf16, whose e4m3 code is rounded past it: the exponent is found without an overflow."""
+    C = _crisp()
+    _say("gather largest values")
+    for fmt in FORMATS:
+        c, oracle = _new(C, 5, 1, 64, fmt)
+        x = torch.full((1, 100, 128), 3.3895313892515355e38, dtype=torch.bfloat16)
+        x[:, 50:] = 1e-30
+        x[:, 10] = -x[:, 10]
+        table = np.array([[0, 1]], dtype=np.int32)
+        _append(C, c, oracle, table, [0], [100], x, -x)
+        kept = np.array([[[5, 10, 40, 60, 70, 99]]], dtype=np.int32)
+        _check_gather(C, c, oracle, table, kept, [6], np.array([[3]], dtype=np.int32))
+
+
+def test_gather_bad_places():
+    """Kept positions out of range or without a page become zeros; pages of the new table out of range are not written."""
+    C = _crisp()
+    _say("gather bad places")
+    rng = np.random.default_rng(6)
+    c, oracle, table, n_pages = _filled(C, [300, 200, 100], 2, 64, O.E4M3, 6, extra=9)
+    new = _new_pages(table, n_pages, 3)
+    kept = np.full((3, 2, 150), -1, dtype=np.int32)
+    for s, n in enumerate((300, 200, 100)):
+        kept[s, :, :90] = _some(rng, n, 90, 2)
+    kept[0, 0, 5], kept[0, 1, 7], kept[1, 0, 0] = -1, 1 << 30, 320
+    table[0, 2] = -1
+    table[1, 1] = n_pages + 5
+    new[1, 1], new[2, 0] = -1, n_pages
+    _check_gather(C, c, oracle, table, kept, [90, 90, 90], new)
+    # a count past the list, of none, below none
+    _check_gather(C, c, oracle, table, kept, [1000, 0, -7], new)
+
+
+def test_gather_of_a_batch_equals_appending_the_kept_values():
+    """What gather is said to be: the kept tokens' cached values appended to a fresh sequence."""
+    C = _crisp()
+    _say("gather equals append")
+    rng = np.random.default_rng(7)
+    lens, m = [777, 130, 400], [300, 100, 65]
+    for fmt in FORMATS:
+        c, oracle, table, n_pages = _filled(C, lens, 1, 64, fmt, 7, spread=4, extra=2 * 3 * 5)
+        new = _new_pages(table, n_pages, 10)
+        one, two = np.ascontiguousarray(new[:, :5]), np.ascontiguousarray(new[:, 5:])
+        kept = np.full((3, 1, 300), -1, dtype=np.int32)
+        rows = []
+        for s in range(3):
+            kept[s, 0, :m[s]] = _some(rng, lens[s], m[s], 1)[0]
+            rows.append([oracle.values(table[s], lens[s], x)[0][:, kept[s, 0, :m[s]]] for x in (0, 1)])
+        _check_gather(C, c, oracle, table, kept, m, one)
+        k, v = (torch.from_numpy(np.concatenate([r[x] for r in rows], 1)).to(torch.bfloat16) for x in (0, 1))
+        _append(C, c, oracle, two, [0, 0, 0], m, k, v)
+        a, b = O.decode(c.pages.cpu().numpy(), fmt), c.scales.cpu().numpy()
+        for s in range(3):
+            for i in range(m[s]):
+                assert (a[one[s, i // 64], :, :, i % 64] == a[two[s, i // 64], :, :, i % 64]).all()
+            for p in range(-(-m[s] // 64)):
+                assert (b[one[s, p]] == b[two[s, p]]).all()
+
+
+# ------------------------------------------------------------------ together
+
+
+def test_evicting_steps_in_a_graph():
+    """Rows appended, attended, weighed; then the sequences cut and moved, all captured: replays follow the device's lengths."""
+    C = _crisp()
+    _say("evict in a graph")
+    heads, hq, lens = 2, 4, [300, 190]
+    rng = np.random.default_rng(9)
+    c, oracle, table, n_pages = _filled(C, lens, heads, 64, O.E4M3, 9, extra=8)
+    new = _new_pages(table, n_pages, 3)
+    t, nt, held = _ints(table), _ints(new), _ints([0, 0])
+    n, keep, ptr = _ints([l - 1 for l in lens]), _ints([100, 150]), _ints([0, 1, 2])
+    q, w = _rand(hq, 2, 1).to(DEV), torch.full((2, heads, 320), math.nan, device=DEV)
+    out = torch.zeros_like(w)
+    ws = C.cache_weights_workspace(c, hq, 2, 2)
+    kept_of = []
+
+    def once():
+        C.crisp_cache_weights(c, t, n, ptr, q, w, held, out=out, ws=ws)
+        kept, count = C.crisp_cache_keep(out, n + 1, n + 1, keep, 160, 4, 16)
+        C.crisp_cache_gather(c, t, kept, count, nt)
+        kept_of[:] = [kept, count]
+
+    once()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        once()
+    captured = list(kept_of)
+    for lengths, budget, seed in (([299, 189], [100, 150], 1), ([150, 189], [160, 60], 2), ([250, 101], [64, 99], 3)):
+        n.copy_(_ints(lengths))
+        keep.copy_(_ints(budget))
+        q.copy_(_rand(hq, 2, seed))
+        out.zero_()
+        c.pages[torch.from_numpy(new.ravel()).long().to(DEV)] = 0
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in (*captured, out, c.pages, c.scales)]
+        out.zero_()
+        c.pages[torch.from_numpy(new.ravel()).long().to(DEV)] = 0
+        once()
+        for a, b in zip(got, (*kept_of, out, c.pages, c.scales)):
+            # scales of pages that no append has written are NaN here
+            assert torch.equal(torch.nan_to_num(a.float(), nan=-1.0), torch.nan_to_num(b.float(), nan=-1.0))
+
+
+def test_two_streams_at_once():
+    C = _crisp()
+    _say("evict on two streams")
+    sides = []
+    for i in range(2):
+        lens = [900 + 100 * i, 300]
+        c, oracle, table, n_pages = _filled(C, lens, 2, 64, O.E4M3, i, extra=12)
+        sides.append(dict(c=c, t=_ints(table), nt=_ints(_new_pages(table, n_pages, 4)), n=_ints([x - 1 for x in lens]), q=_rand(4, 2, i).to(DEV),
+                          w=torch.zeros(2, 2, 1024, device=DEV), s=torch.cuda.Stream()))
+    ptr, keep, held = _ints([0, 1, 2]), _ints([200, 100]), _ints([0, 0])
+
+    def once(d):
+        w = C.crisp_cache_weights(d["c"], d["t"], d["n"], ptr, d["q"], d["w"], held, out=torch.zeros_like(d["w"]))
+        kept, count = C.crisp_cache_keep(w, d["n"] + 1, d["n"] + 1, keep, 256)
+        C.crisp_cache_gather(d["c"], d["t"], kept, count, d["nt"])
+        return w, kept
+
+    want = [once(d) for d in sides]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for i, d in enumerate(sides):
+            with torch.cuda.stream(d["s"]):
+                got.append((i, once(d)))
+    torch.cuda.synchronize()
+    for i, (w, kept) in got:
+        assert torch.equal(w, want[i][0]) and torch.equal(kept, want[i][1])
