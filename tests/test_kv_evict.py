@@ -1,0 +1,385 @@
+"""KVCache with rotary positions, packed prompts, accumulated weights and eviction: against the single calls, and against a 64-bit
+mirror of each sequence (tests/cache_oracle.py, tests/packed_oracle.py); what is refused or given back; a serving loop in graphs."""
+import copy
+import math
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from tests import cache_oracle as O
+from tests import packed_oracle as R
+from tests.helpers import to_f64
+from tests.test_kv_cache import Mirror, _ints, _rand, _same_tokens
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def _say(msg):
+    print(f"[gpu-case] {msg}", flush=True)
+    sys.stdout.flush()
+
+
+def _ptr(counts):
+    return _ints(np.concatenate([[0], np.cumsum(counts)]))
+
+
+def _qkv(n, seed, hq=4, hkv=2, scale=1.0):
+    return tuple(_rand(h, n, 10 * seed + i, scale).to(DEV) for i, h in enumerate((hq, hkv, hkv)))
+
+
+def _caches(a, b):
+    for x, y in zip(a.layers, b.layers):
+        used = (a.pool[:x.n_pages] > 0).nonzero()[:, 0]
+        assert torch.equal(x.scales[used], y.scales[used]) and torch.equal(a.table, b.table) and torch.equal(a.seq_len, b.seq_len)
+        _same_tokens(a, x, y, 0)
+
+
+def test_rope_turns_every_call():
+    """A cache with rope equals one without that is given turned q and k: prompts, packed prompts, steps, forks, tokens taken back."""
+    from paper_2609_01925_amd import crisp as C
+    from paper_2609_01925_amd.cache import KVCache
+    _say("KVCache rope")
+    rope = C.make_rope(64, C.ROPE_INTERLEAVED, 500000.0, C.ROPE_BANDS, 8.0, 8192.0, 1.0, 4.0)
+    a, b = (KVCache(1, 60, 2, max_seqs=5, max_tokens=640, device=DEV, rope=r) for r in (rope, None))
+    pos = [0] * 5
+
+    def turned(row_ptr, start, q, k):
+        return C.crisp_rope(rope, _ints(start), row_ptr, q, k)
+
+    def reserve(counts):
+        assert a.reserve(_ints(counts)).tolist() == counts and b.reserve(_ints(counts)).tolist() == counts
+
+    def advance(counts):
+        a.advance(_ints(counts))
+        b.advance(_ints(counts))
+        pos[:] = [p + c for p, c in zip(pos, counts)]
+        assert a.pos.tolist() == pos and b.pos is None
+
+    def attend(counts, seed):
+        reserve(counts)
+        q, k, v = _qkv(sum(counts), seed)
+        tq, tk = turned(_ptr(counts), pos, q, k)
+        assert torch.equal(a.attend(0, _ptr(counts), q, k, v), b.attend(0, _ptr(counts), tq, tk, v))
+        advance(counts)
+
+    reserve([300, 0, 0, 0, 0])
+    q, k, v = _qkv(300, 1)
+    tq, tk = turned(_ptr([300]), [0], q, k)
+    assert torch.equal(a.prefill(0, 0, q, k, v), b.prefill(0, 0, tq, tk, v))
+    advance([300, 0, 0, 0, 0])
+    counts = [0, 90, 0, 130, 1]
+    reserve(counts)
+    q, k, v = _qkv(sum(counts), 2)
+    tq, tk = turned(_ptr(counts), pos, q, k)
+    assert torch.equal(a.prefill_packed(0, _ptr(counts), q, k, v), b.prefill_packed(0, _ptr(counts), tq, tk, v))
+    advance(counts)
+    attend([1, 1, 0, 1, 1], 3)
+    for kv in (a, b):
+        kv.free(_ints([4]))
+        kv.fork(_ints([0, 3, 7]), _ints([2, 4, 4]))
+    pos[2], pos[4] = pos[0], pos[3]
+    assert a.pos.tolist() == pos
+    attend([1, 5, 2, 0, 40], 4)
+    advance([0, -3, -1, 0, -20])
+    attend([1, 1, 1, 1, 1], 5)
+    _caches(a, b)
+    a.free(_ints([0, 1, 2, 3, 4]))
+    assert a.pos.tolist() == [0] * 5
+
+
+@pytest.mark.parametrize("fused", [False, True])
+def test_packed_prompts(fused):
+    """Packed prompts equal the dense attention of each, and what is stored equals what single appends store; a sequence that
+    holds tokens, or was granted none, stores nothing."""
+    from paper_2609_01925_amd import crisp as C
+    from paper_2609_01925_amd.cache import KVCache
+    _say(f"KVCache packed prompts fused={fused}")
+    kv, one = (KVCache(2, 20, 2, max_seqs=5, max_tokens=512, device=DEV) for _ in range(2))
+    counts = [100, 0, 333, 1, 5000]  # the last is refused
+    for c in (kv, one):
+        assert c.reserve(_ints(counts)).tolist() == [100, 0, 333, 1, 0]
+    ptr = np.concatenate([[0], np.cumsum(counts)])
+    n = int(ptr[-1])
+    for layer in range(2):
+        q, k, v = _qkv(n, layer)
+        if fused:
+            q, k, v = torch.cat((q, k, v)).transpose(0, 1).contiguous().transpose(0, 1).split([4, 2, 2])
+        o = kv.prefill_packed(layer, _ints(ptr), q, k, v)
+        for s, c in enumerate(counts):
+            at = slice(ptr[s], ptr[s + 1])
+            if c:
+                alone = C.crisp_packed_attn(_ints([0, c]), q[:, at], k[:, at], v[:, at])
+                assert (o[:, at].float() - alone.float()).abs().max() <= 6 * 2.0 ** -8 * v.float().abs().max()
+        C.crisp_cache_append(one.layers[layer], one._open, one.seq_len, _ints(ptr), k, v)
+    for c in (kv, one):
+        c.advance(_ints(counts))
+        assert c.seq_len.tolist() == [100, 0, 333, 1, 0]
+    _caches(kv, one)
+    # a second prompt for sequences that hold tokens: nothing changes and the result says so
+    more = [50, 60, 0, 0, 0]
+    kv.reserve(_ints(more))
+    before = [(c.pages.clone(), c.scales.clone()) for c in kv.layers]
+    q, k, v = _qkv(110, 9)
+    o = kv.prefill_packed(0, _ptr(more), q, k, v)
+    assert torch.isnan(o[:, 0]).all() and torch.isfinite(o[:, 1:]).all()
+    row = kv.table[1, 0].item()
+    keep = [p for p in range(20) if p != row]
+    assert torch.equal(kv.layers[0].pages[keep], before[0][0][keep]) and not torch.equal(kv.layers[0].pages[row], before[0][0][row])
+    assert kv.prefill_packed(0, _ptr([0] * 5), q[:, :0], k[:, :0], v[:, :0]).shape == (4, 0, 128)
+
+
+class Evicting(Mirror):
+    """A Mirror whose sequences are cut as evict() cuts them, by the weights that the device holds."""
+
+    def evict(self, kv, count, keep, sink, recent):
+        for s, m in enumerate(count):
+            if not m:
+                continue
+            n = self.len[s]
+            for layer, cache in enumerate(self.seqs[s]):
+                w = kv["weights"][layer][s:s + 1]
+                kept, _, _, _ = R.cache_keep(w, [kv["held"][s]], [n], [m], m, sink, recent)
+                slots = cache.codes.shape[0]
+                both = O.Cache(2 * slots, cache.codes.shape[1], cache.block, cache.fmt)
+                both.codes[:slots], both.exp[:slots], both.written[:slots] = cache.codes, cache.exp, cache.written
+                new = np.arange(slots, 2 * slots, dtype=np.int32)[None]
+                R.cache_gather(both, self.table, kept, [m], new)
+                cache.codes, cache.exp = both.codes[slots:].copy(), both.exp[slots:].copy()
+                cache.written = both.written[slots:].copy()
+            self.len[s] = m
+
+
+def _weights_of(kv):
+    return dict(weights=[w.cpu().numpy().copy() for w in kv.weights], held=kv.held.tolist())
+
+
+def _check_weights(kv, mirror, layer, before, q, counts, lens):
+    """The device's weights of a step against 64 bits, from the ones that it held before."""
+    ptr = np.concatenate([[0], np.cumsum(counts)])
+    got = to_f64(kv.weights[layer])
+    for s, c in enumerate(counts):
+        if c:
+            old = before["weights"][layer][s:s + 1].astype(np.float64)
+            want, tol = R.cache_weights(mirror.seqs[s][layer], mirror.table, [lens[s]], [0, c], to_f64(q[:, ptr[s]:ptr[s + 1]]),
+                                        1 / math.sqrt(128), old, [before["held"][s]])
+            live = ~np.isnan(want[0])
+            assert (np.abs(got[s] - want[0])[live] <= tol[0][live]).all(), f"sequence {s} layer {layer}"
+
+
+def _step(kv, mirror, counts, seed):
+    assert kv.reserve(_ints(counts)).tolist() == counts
+    ptr = np.concatenate([[0], np.cumsum(counts)])
+    before, lens = _weights_of(kv), [mirror.len.get(s, 0) for s in range(len(counts))]
+    for layer in range(len(kv.layers)):
+        q, k, v = _qkv(int(ptr[-1]), 50 * seed + layer)
+        o = to_f64(kv.attend(layer, _ints(ptr), q, k, v, weigh=True))
+        for s, c in enumerate(counts):
+            if c:
+                a, b = ptr[s], ptr[s + 1]
+                mirror.append(s, layer, k[:, a:b], v[:, a:b])
+                want, tol = mirror.attention(s, layer, q[:, a:b])
+                assert (np.abs(o[:, a:b] - want) <= tol).all(), f"sequence {s} layer {layer}"
+        _check_weights(kv, mirror, layer, before, q, counts, lens)
+    kv.advance(_ints(counts), weighed=True)
+    for s, c in enumerate(counts):
+        if c:
+            mirror.len[s] += c
+
+
+@pytest.mark.parametrize("fmt,block", [(O.E4M3, 64), (O.INT8, 128)])
+def test_prompts_steps_and_evictions(fmt, block):
+    """Prompts whose tokens are weighed, steps, cuts, more steps over what stayed, forks that part, a second cut."""
+    from paper_2609_01925_amd.cache import KVCache
+    _say(f"KVCache evict fmt={fmt} block={block}")
+    kv = KVCache(2, 40, 2, max_seqs=4, max_tokens=640, block=block, fmt=fmt, device=DEV, weights=True)
+    mirror = Evicting(2, 2, block, fmt, 640 // block)
+    counts = [200, 0, 150, 0]
+    assert kv.reserve(_ints(counts)).tolist() == counts
+    before = _weights_of(kv)
+    for layer in range(2):
+        q, k, v = _qkv(350, layer)
+        kv.prefill_packed(layer, _ptr(counts), q, k, v, weigh=True)
+        mirror.append(0, layer, k[:, :200], v[:, :200])
+        mirror.append(2, layer, k[:, 200:], v[:, 200:])
+        _check_weights(kv, mirror, layer, before, q, counts, [0] * 4)
+    kv.advance(_ints(counts), weighed=True)
+    mirror.len.update({0: 200, 2: 150})
+    assert kv.held.tolist() == [200, 0, 150, 0]
+    counts = [0, 300, 0, 0]
+    assert kv.reserve(_ints(counts)).tolist() == counts
+    for layer in range(2):
+        q, k, v = _qkv(300, 7 + layer)
+        kv.prefill(layer, 1, q, k, v, weigh=32)
+        mirror.append(1, layer, k, v)
+        want, tol = R.cache_weights(mirror.seqs[1][layer], mirror.table, [268], [0, 32], to_f64(q[:, 268:]), 1 / math.sqrt(128),
+                                    np.zeros((1, 2, 640)), [0])
+        live = ~np.isnan(want[0])
+        assert (np.abs(to_f64(kv.weights[layer])[1] - want[0])[live] <= tol[0][live]).all()
+    kv.advance(_ints(counts), weighed=True)
+    mirror.len[1] = 300
+    assert kv.held.tolist() == [200, 300, 150, 0]
+    for i in range(3):
+        _step(kv, mirror, [1, 2, 1, 0], 2 + i)
+
+    def evict(keep, cap, sink, recent):
+        before, lens, pos = _weights_of(kv), [mirror.len.get(s, 0) for s in range(4)], kv.pos.tolist()
+        want = [m if 0 < m < n and m <= cap else 0 for m, n in zip(keep, lens)]
+        assert kv.evict(_ints(keep), cap, sink, recent).tolist() == want
+        mirror.evict(before, want, keep, sink, recent)
+        assert kv.seq_len.tolist() == [mirror.len.get(s, 0) for s in range(4)] and kv.pos.tolist() == pos
+        held = [sum(-(-n // block) for n in mirror.len.values())]
+        assert [int((kv.pool[:40] > 0).sum())] == held or kv.pool[:40].max() > 1
+
+    evict([100, 64, 1000, 5], 128, 4, 16)
+    _step(kv, mirror, [1, 1, 1, 0], 6)
+    evict([3, 200, 100, 0], 100, 0, 1)  # the second is above the cap
+    _step(kv, mirror, [1, 3, 70, 0], 7)
+    kv.fork(_ints([1]), _ints([3]))
+    mirror.seqs[3], mirror.len[3] = copy.deepcopy(mirror.seqs[1]), mirror.len[1]
+    assert torch.equal(kv.weights[0][3, :, :mirror.len[3]], kv.weights[0][1, :, :mirror.len[1]]) and kv.held[3] == kv.held[1]
+    _step(kv, mirror, [1, 1, 1, 1], 8)
+    evict([0, 40, 0, 0], 64, 2, 8)      # one of the two that share pages
+    for i in range(2):
+        _step(kv, mirror, [1, 1, 1, 1], 9 + i)
+    assert kv.compact().item() >= 0
+    _step(kv, mirror, [2, 1, 60, 1], 12)
+    kv.free(_ints([0, 1, 2, 3]))
+    assert (kv.pool == 0).all() and kv.held.tolist() == [0] * 4 and kv.pos.tolist() == [0] * 4
+
+
+def test_evict_without_pages_and_of_granted_rows():
+    """No pages for what stays: nothing changes.  Rows that were granted and not taken are given back."""
+    from paper_2609_01925_amd.cache import KVCache
+    _say("KVCache evict without pages")
+    kv = KVCache(1, 10, 1, max_seqs=3, max_tokens=640, device=DEV, weights=True)
+    kv.reserve(_ints([400, 150, 0]))  # 7 + 3 pages: none is left
+    q, k, v = _qkv(550, 1, 2, 1)
+    kv.prefill_packed(0, _ptr([400, 150, 0]), q, k, v, weigh=True)
+    kv.advance(_ints([400, 150, 0]), weighed=True)
+    state = lambda: [t.clone() for t in (kv.table, kv.seq_len, kv.pool, kv.held, kv.room, kv.layers[0].pages, kv.layers[0].scales)]
+    before, w = state(), kv.weights[0][:, :, :150].clone()
+    assert kv.evict(_ints([100, 100, 100]), 100).tolist() == [0, 0, 0]
+    assert all(torch.equal(a, b) for a, b in zip(before, state())) and torch.equal(w[:2], kv.weights[0][:2, :, :150])
+    kv.free(_ints([1]))
+    assert kv.evict(_ints([100, 100, 100]), 100).tolist() == [100, 0, 0]
+    assert int((kv.pool[:10] > 0).sum()) == 2
+    assert kv.reserve(_ints([300, 0, 0])).tolist() == [300, 0, 0] and kv.room.tolist() == [300, 0, 0]
+    assert kv.evict(_ints([90, 0, 0]), 90).tolist() == [90, 0, 0]
+    assert kv.room.tolist() == [0, 0, 0] and int((kv.pool[:10] > 0).sum()) == 2 and kv.seq_len.tolist() == [90, 0, 0]
+    x, y, z = _qkv(1, 2, 2, 1)
+    assert (kv.attend(0, _ptr([1, 0, 0]), x, y, z) == 0).all()  # it takes rows again once some are granted
+
+
+def test_steps_that_are_not_weighed():
+    """Their tokens have weight 0, also where the buffer holds something else, until a step that is."""
+    from paper_2609_01925_amd.cache import KVCache
+    _say("KVCache steps not weighed")
+    kv = KVCache(1, 10, 1, max_seqs=1, max_tokens=320, device=DEV, weights=True)
+    kv.weights[0].fill_(math.nan)
+    kv.reserve(_ints([100]))
+    kv.prefill(0, 0, *_qkv(100, 1, 2, 1))
+    kv.advance(_ints([100]))
+    assert kv.held.tolist() == [0]
+    kv.reserve(_ints([10]))
+    kv.attend(0, _ptr([10]), *_qkv(10, 2, 2, 1))
+    kv.advance(_ints([10]))
+    assert kv.evict(_ints([50]), 50, 4, 6).tolist() == [50]  # all equal: the first ones stay
+    assert kv.held.tolist() == [50] and (kv.weights[0][0, 0, :50] == 0).all()
+    kv.reserve(_ints([2]))
+    kv.attend(0, _ptr([2]), *_qkv(2, 3, 2, 1), weigh=True)
+    kv.advance(_ints([2]), weighed=True)
+    w = kv.weights[0][0, 0, :52]
+    assert kv.held.tolist() == [52] and abs(w.double().sum().item() - 4.0) < 4 * 2.0 ** -13
+    kv.advance(_ints([-1]))
+    assert kv.held.tolist() == [51] and kv.pos.tolist() == [111]
+
+
+def test_prefill_of_a_sequence_that_holds_tokens_keeps_its_weights():
+    from paper_2609_01925_amd.cache import KVCache
+    _say("KVCache refused prefill with weights")
+    kv = KVCache(1, 10, 1, max_seqs=2, max_tokens=320, device=DEV, weights=True)
+    kv.reserve(_ints([100, 0]))
+    kv.prefill(0, 0, *_qkv(100, 1, 2, 1), weigh=10)
+    kv.advance(_ints([100, 0]), weighed=True)
+    before = kv.weights[0].clone()
+    kv.reserve(_ints([50, 0]))
+    assert torch.isnan(kv.prefill(0, 0, *_qkv(50, 2, 2, 1), weigh=10)[:, 0]).all()
+    kv.prefill(0, 1, *_qkv(50, 3, 2, 1), weigh=10)  # no room
+    assert torch.equal(torch.nan_to_num(kv.weights[0]), torch.nan_to_num(before))
+
+
+def test_arguments():
+    from paper_2609_01925_amd.cache import KVCache
+    _say("KVCache arguments")
+    kv = KVCache(1, 4, 1, max_seqs=2, max_tokens=128, device=DEV)
+    q, k, v = _qkv(10, 0, 2, 1)
+    for call in (lambda: kv.evict(_ints([1, 1]), 4), lambda: kv.prefill(0, 0, q, k, v, weigh=4),
+                 lambda: kv.prefill_packed(0, _ptr([10, 0]), q, k, v, weigh=True),
+                 lambda: kv.attend(0, _ptr([10, 0]), q, k, v, weigh=True)):
+        with pytest.raises(ValueError):
+            call()
+    kv = KVCache(1, 4, 1, max_seqs=2, max_tokens=128, device=DEV, weights=True)
+    for call in (lambda: kv.evict(_ints([1, 1]), 0), lambda: kv.prefill(0, 0, q, k, v, weigh=11),
+                 lambda: kv.prefill(0, 0, q, k, v, weigh=-1), lambda: kv.evict(_ints([1, 1, 1]), 4)):
+        with pytest.raises((ValueError, RuntimeError)):
+            call()
+
+
+def test_serving_loop_in_graphs():
+    """A weighed step and an eviction captured once each and replayed in turn with other counts and budgets, beside the same calls
+    made eagerly on a second cache."""
+    from paper_2609_01925_amd import crisp as C
+    from paper_2609_01925_amd.cache import KVCache
+    _say("KVCache evicting loop in graphs")
+    n, hq, hkv, rows = 4, 4, 2, 60
+    make = lambda: KVCache(2, 40, hkv, max_seqs=n, max_tokens=384, device=DEV, rope=C.make_rope(), weights=True)
+    rng = np.random.default_rng(1)
+    counts, ptr, keep = (torch.zeros(m, dtype=torch.int32, device=DEV) for m in (n, n + 1, n))
+    q, k, v = (torch.zeros(2, h, rows, 128, dtype=torch.bfloat16, device=DEV) for h in (hq, hkv, hkv))
+    out = [torch.zeros(2, hq, rows, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+
+    def step(kv, o):
+        kv.reserve(counts)
+        for layer in range(2):
+            kv.attend(layer, ptr, q[layer], k[layer], v[layer], out=o[layer], weigh=True)
+        kv.advance(counts, weighed=True)
+
+    eager, other = make(), make()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step(other, out[1])
+        other.evict(keep, 100)
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()]
+    with torch.cuda.graph(graphs[0]):
+        step(other, out[1])
+    with torch.cuda.graph(graphs[1]):
+        other.evict(keep, 100)
+    for i in range(10):
+        c = rng.integers(0, 16, n)
+        counts.copy_(_ints(c))
+        ptr.copy_(_ints(np.concatenate([[0], np.cumsum(c)])))
+        keep.copy_(_ints(rng.integers(0, 60, n)))
+        for x in (q, k, v):
+            x.copy_(torch.stack([_rand(x.shape[1], rows, 10 * i + j) for j in range(2)]))
+        torch.cuda.synchronize()
+        step(eager, out[0])
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0][:, :, :c.sum()], out[1][:, :, :c.sum()]), i
+        if i % 2:
+            eager.evict(keep, 100)
+            graphs[1].replay()
+            torch.cuda.synchronize()
+        for x, y in ((eager.seq_len, other.seq_len), (eager.table, other.table), (eager.pool, other.pool), (eager.pos, other.pos),
+                     (eager.held, other.held), (eager.room, other.room)):
+            assert torch.equal(x, y), i
+        for layer in range(2):
+            _same_tokens(eager, eager.layers[layer], other.layers[layer], 0)
+            for s, m in enumerate(eager.held.tolist()):
+                assert torch.equal(eager.weights[layer][s, :, :m], other.weights[layer][s, :, :m])
+    assert eager.pos.tolist() != eager.seq_len.tolist()
