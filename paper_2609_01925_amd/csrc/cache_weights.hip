@@ -1,9 +1,10 @@
 // The attention weight that each cached token gets from new rows, summed over the rows and the query heads of its KV head:
 //   w_j = sum_p exp2(x_pj - lse_p),  x_pj = scale log2(e) q_p . k_j,  lse_p = log2 sum_j exp2(x_pj)
 // over the pairs p = i G + g of a sequence's rows i and the G query heads of the KV head.  A pair's sum over all keys has to be known
-// before any of its weights, so the products are formed twice: weigh_rows leaves each pair's maximum and sum over a chunk of the
-// tokens, weigh_join takes them together, and weigh_tokens forms the weights, a wave a tile of 64 tokens, and sums them over the pairs
-// in registers, in a fixed order and without atomics.
+// before any of its weights, so the keys are gone over twice: weigh_rows leaves each pair's maximum and sum over a chunk of the
+// tokens, and weigh_tokens takes the chunks' together and forms the weights, a wave a tile of 64 tokens, summed over the pairs in a
+// fixed order and without atomics.  Where a sequence has few pairs, x itself waits in the workspace, 4 bytes a pair and token where
+// the keys are 128; where it has many, the products are formed again and a launch between the two joins the chunks.
 #include "cache_device.h"
 
 namespace crisp {
@@ -12,8 +13,9 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kGroup = 16;                  // pairs of one product
-constexpr int kGroups = 8;                  // of a pass over the keys in weigh_rows
+constexpr int kGroups = 8;                  // of a pass over the keys
 constexpr int kPairs = kGroup * kGroups;
+constexpr int kScoreSeqs = 1024;            // sequences of a call whose scores may wait: each workgroup adds up those before its own
 
 struct WeightArgs {
   CacheDims c;
@@ -30,8 +32,11 @@ struct WeightArgs {
   int chunks;      // of a sequence, at most
   int token_wgs;   // workgroups of a sequence and KV head in weigh_tokens
   float c2;        // scale log2(e)
+  int waiting;     // pairs of a sequence whose scores may wait, at most (0: none do)
+  int64_t slots;   // tiles that there is room for
   float2* stats;   // [n_rows][hq][chunks]: maximum, sum
   float* lse;      // [n_rows][hq]
+  float* scores;   // [slots][hkv][waiting][64]: x
 };
 
 typedef __attribute__((__vector_size__(4 * sizeof(float)))) float acc4;
@@ -45,29 +50,68 @@ __device__ __forceinline__ int tiles_of(const WeightArgs& a, const SeqRows& r) {
 }
 __device__ __forceinline__ int chunks_of(const WeightArgs& a, int tiles) { return min(a.chunks, (tiles + kWaves - 1) / kWaves); }
 
-// K of a tile as the products' operands: k[4 t + kk] is 16 tokens t of elements 32 g + 8 kk + [0, 8).  kc takes products with codes
-// to the base-2 exponent; false if the tile has no page.
+// The first slot of a sequence's scores, -1 if they do not wait: the tiles of the sequences before it come first.
+__device__ __forceinline__ int64_t first_slot(const WeightArgs& a, int seq, int tiles, int pairs) {
+  if (pairs > a.waiting) return -1;
+  int64_t sum = 0;
+  for (int i = lane_id(); i < seq; i += kWave) sum += tiles_of(a, seq_rows(a.s, a.b, a.c.B, i));
+  sum = wave_scan(sum);
+  sum = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)sum, 63) |
+                  (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(sum >> 32), 63) << 32);
+  return sum + tiles <= a.slots ? sum : -1;
+}
+
+// Keeps a loaded chunk in its four registers up to here: left to itself the compiler splits what a loop carries into single
+// codes, a register each.
+__device__ __forceinline__ void keep_whole(u32x4 (&raw)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) asm("" : "+v"(raw[i]));
+}
+
+// The tiles t0, t0 + STEP, ... < t1 of one sequence and KV head, K alone.  64 are looked up in one round of loads, one a lane; the codes of
+// the next are loaded while those of the present one are worked on.
+template <int STEP>
+struct KeyTiles {
+  const int32_t* row;
+  int tb, end, pg;
+  float kc;
+
+  __device__ __forceinline__ KeyTiles(const WeightArgs& a, int seq, int t0, int t1)
+      : row(a.s.table + (int64_t)seq * a.b.max_pages), tb(t0 - STEP * kWave), end(t1), pg(-1), kc(0.f) {}
+
+  // Tile t, the one after the last that was asked for: its codes, and what takes products with them to the base-2 exponent;
+  // false if it has no page.
+  __device__ __forceinline__ bool load(const WeightArgs& a, int head, int t, u32x4 (&raw)[8], float& scale) {
+    if (t >= tb + STEP * kWave) {
+      tb = t;
+      const int mine = t + STEP * lane_id(), slot = a.c.tiles == 2 ? mine >> 1 : mine;
+      pg = mine < end && slot < a.b.max_pages ? row[slot] : -1;
+      if (pg >= a.c.n_pages) pg = -1;
+      // (not 0, which a masked -infinity must not meet)
+      if (pg >= 0) kc = fmaxf(pow2f(stored_exp(a.scales[((int64_t)pg * a.c.hkv + head) * 2])) * a.c2, 1.17549435e-38f);
+    }
+    const int i = (t - tb) / STEP, page = __builtin_amdgcn_readlane(pg, i);
+    scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kc), i));
+    if (page < 0) return false;
+    const u32x4* src = reinterpret_cast<const u32x4*>(
+        a.pages + (((int64_t)page * a.c.hkv + head) * a.c.tiles + (a.c.tiles == 2 ? t & 1 : 0)) * (2 * kTileBytes)) + lane_id();
+#pragma unroll
+    for (int x = 0; x < 8; ++x) raw[x] = src[x * kWave];
+    return true;
+  }
+};
+
+// A tile of K as the products' operands: k[4 t + kk] is 16 tokens t of elements 32 g + 8 kk + [0, 8).
 struct KeyTile {
   bf16x8 k[16];
-  float kc;
 };
 template <int FMT>
-__device__ __forceinline__ bool load_keys(const WeightArgs& a, int seq, int head, int t, KeyTile& x) {
-  const int slot = a.c.tiles == 2 ? t >> 1 : t;
-  const int page = slot < a.b.max_pages ? __builtin_amdgcn_readfirstlane(a.s.table[(int64_t)seq * a.b.max_pages + slot]) : -1;
-  if (page < 0 || page >= a.c.n_pages) return false;
-  const u32x4* src = reinterpret_cast<const u32x4*>(
-      a.pages + (((int64_t)page * a.c.hkv + head) * a.c.tiles + (a.c.tiles == 2 ? t & 1 : 0)) * (2 * kTileBytes)) + lane_id();
-  u32x4 raw[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) raw[i] = src[i * kWave];
-  x.kc = fmaxf(pow2f(stored_exp(a.scales[((int64_t)page * a.c.hkv + head) * 2])) * a.c2, 1.17549435e-38f);  // not 0, which a masked -inf must not meet
+__device__ __forceinline__ void convert(const u32x4 (&raw)[8], KeyTile& x) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     x.k[2 * i] = codes_to_bf16<FMT>(raw[i][0], raw[i][1]);
     x.k[2 * i + 1] = codes_to_bf16<FMT>(raw[i][2], raw[i][3]);
   }
-  return true;
 }
 
 __device__ __forceinline__ void products(const KeyTile& x, const bf16x8 (&q)[4], acc4 (&s)[4]) {
@@ -77,6 +121,21 @@ __device__ __forceinline__ void products(const KeyTile& x, const bf16x8 (&q)[4],
   for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
     for (int t = 0; t < 4; ++t) s[t] = mfma16(x.k[4 * t + kk], q[kk], s[t]);
+}
+
+// The same from the codes, for a product or two of a tile: the operands are not all held at once.
+template <int FMT>
+__device__ __forceinline__ void products(const u32x4 (&raw)[8], const bf16x8 (&q)[4], acc4 (&s)[4]) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    s[t] = acc4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const u32x4 x = raw[2 * t + half];
+      s[t] = mfma16(codes_to_bf16<FMT>(x[0], x[1]), q[2 * half], s[t]);
+      s[t] = mfma16(codes_to_bf16<FMT>(x[2], x[3]), q[2 * half + 1], s[t]);
+    }
+  }
 }
 
 // This lane's part of pair p's q: column lane % 16, elements 32 (lane / 16) + 8 kk + [0, 8); 0 past the last pair.
@@ -107,69 +166,147 @@ __device__ __forceinline__ Item item_of(const WeightArgs& a, int each) {
   return Item{sh / a.c.hkv, sh % a.c.hkv, (int)blockIdx.x - sh * each};
 }
 
-template <int FMT>
-__global__ __launch_bounds__(kThreads) void weigh_rows(WeightArgs a) {
-  __shared__ bf16x8 qs[kGroups][4][kWave];
-  __shared__ float2 part[kWaves][kPairs];
+// Pairs p0 .. of q as the products take them, in LDS; ends with a barrier.
+__device__ __forceinline__ int stage_pairs(const WeightArgs& a, const SeqRows& r, int head, int p0, int pairs, int w, int lane,
+                                           bf16x8 (&qs)[kGroups][4][kWave]) {
+  const int groups = min((pairs - p0 + kGroup - 1) / kGroup, kGroups);
+  for (int g = w; g < groups; g += kWaves) {
+    bf16x8 q[4];
+    load_pair(a, r, head, p0 + g * kGroup + (lane & 15), pairs, q);
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) qs[g][kk][lane] = q[kk];
+  }
+  __syncthreads();
+  return groups;
+}
+
+// A column's reference m and sum l of exp2(x - m) with a tile's 16 of this lane's, x = s kc, -infinity where masked.  The sums are
+// 32-bit floats, so the reference need not be the maximum: it is raised to it where a sum passes 2^60 (or is not a number) and
+// where there is none yet, and no maximum is looked for otherwise.
+__device__ __forceinline__ void add_tile(const acc4 (&s)[4], float kc, float& m, float& l) {
+  const auto sum = [&](float ref) {
+    float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 16; ++e) y[e & 3] += fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], kc, -ref));
+    return (y[0] + y[1]) + (y[2] + y[3]);
+  };
+  float more = sum(m == -__builtin_inff() ? 0.f : m);
+  if (__ballot(!(more <= 0x1p60f) || m == -__builtin_inff())) {
+    float top = s[0][0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) top = vmax(top, s[e >> 2][e & 3]);
+    top = vmax(m, top * kc);
+    const float ref = top == -__builtin_inff() ? 0.f : top;
+    l *= fast_exp2(m - ref);
+    m = top;
+    more = sum(ref);
+  }
+  l += more;
+}
+
+// NG groups of 16 pairs a pass over the keys: 1 where sequences have few pairs, with q in registers and room for more waves, or kGroups,
+// whose q is in LDS and which share the keys' conversion.
+template <int FMT, int NG>
+__global__ __launch_bounds__(kThreads, NG == 1 ? 4 : 2) void weigh_rows(WeightArgs a) {
+  __shared__ bf16x8 qs[NG == 1 ? 1 : kGroups][4][kWave];
+  __shared__ float2 part[kWaves][NG * kGroup];
+  __shared__ float2 state[NG == 1 ? 1 : kWaves][NG == 1 ? 1 : NG][kWave];  // each lane's maximum and sum of each group
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Item it = item_of(a, a.chunks);
   const SeqRows r = seq_rows(a.s, a.b, a.c.B, it.seq);
   const int T = tiles_of(a, r), n = chunks_of(a, T), pairs = r.n * a.G;
   if (pairs == 0 || it.i >= n) return;
   const int t0 = (int)((int64_t)it.i * T / n), t1 = (int)((int64_t)(it.i + 1) * T / n);
-  for (int p0 = 0; p0 < pairs; p0 += kPairs) {
-    const int groups = min((pairs - p0 + kGroup - 1) / kGroup, kGroups);
-    for (int g = w; g < groups; g += kWaves) {
-      bf16x8 q[4];
-      load_pair(a, r, it.head, p0 + g * kGroup + (lane & 15), pairs, q);
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk) qs[g][kk][lane] = q[kk];
+  int64_t slot = -1;
+  for (int p0 = 0; p0 < pairs; p0 += NG * kGroup) {
+    KeyTiles<kWaves> tiles(a, it.seq, t0 + w, t1);
+    u32x4 raw[8] = {}, next[8] = {};
+    float kc = 0.f, kc_next = 0.f;
+    bool ok = false, ok_next = false;
+    if (t0 + w < t1) ok = tiles.load(a, it.head, t0 + w, raw, kc);
+    int groups = 1;
+    bf16x8 q1[4];
+    if constexpr (NG == 1) {
+      load_pair(a, r, it.head, p0 + (lane & 15), pairs, q1);
+      if (p0 == 0) slot = first_slot(a, it.seq, T, pairs);
+    } else {
+      groups = stage_pairs(a, r, it.head, p0, pairs, w, lane, qs);
     }
-    __syncthreads();
-    float m[kGroups], l[kGroups];
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      m[g] = -__builtin_inff();
-      l[g] = 0.f;
-    }
+    float m = -__builtin_inff(), l = 0.f;
+    if constexpr (NG > 1)
+      for (int g = 0; g < groups; ++g) state[w][g][lane] = make_float2(m, l);
     for (int t = t0 + w; t < t1; t += kWaves) {
-      KeyTile x;
-      if (!load_keys<FMT>(a, it.seq, it.head, t, x)) continue;
-      const int first = t * kTile + 16 * (lane >> 4);  // position of this lane's first token
+      if (t + kWaves < t1) ok_next = tiles.load(a, it.head, t + kWaves, next, kc_next);
+      keep_whole(raw);
+      if (ok) {
+        const int first = t * kTile + 16 * (lane >> 4);  // position of this lane's first token
+        const auto finish = [&](int g, acc4 (&s)[4]) {
+          if (NG == 1 && slot >= 0 && (lane & 15) < pairs) {
+            f32x4* dst = reinterpret_cast<f32x4*>(
+                a.scores + (((slot + t) * a.c.hkv + it.head) * a.waiting + (lane & 15)) * kTile + 16 * (lane >> 4));
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        if (g >= groups) break;
-        bf16x8 q[4];
+            for (int e = 0; e < 4; ++e) dst[e] = s[e] * kc;
+          }
+          if (t * kTile + kTile - 1 > r.len + (p0 + g * kGroup) / a.G) {
+            const int see = r.len + (p0 + g * kGroup + (lane & 15)) / a.G;
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) q[kk] = qs[g][kk][lane];
-        acc4 s[4];
-        products(x, q, s);
-        if (t * kTile + kTile - 1 > r.len + (p0 + g * kGroup) / a.G) {
-          const int see = r.len + (p0 + g * kGroup + (lane & 15)) / a.G;
+            for (int e = 0; e < 16; ++e)
+              if (first + e > see) s[e >> 2][e & 3] = -__builtin_inff();
+          }
+          add_tile(s, kc, m, l);
+        };
+        if constexpr (NG == 1) {
+          acc4 s[4];
+          products<FMT>(raw, q1, s);
+          finish(0, s);
+        } else {
+          KeyTile x;
+          convert<FMT>(raw, x);
+          const auto group = [&](int g, acc4 (&s)[4]) {
+            bf16x8 q[4];
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (first + e > see) s[e >> 2][e & 3] = -__builtin_inff();
+            for (int kk = 0; kk < 4; ++kk) q[kk] = qs[g][kk][lane];
+            products(x, q, s);
+          };
+          if (t * kTile + kTile - 1 <= r.len) {  // every row sees the whole tile: the next group's products pass beside this one's sums
+            acc4 s[4], ahead[4];
+            group(0, s);
+            for (int g = 0; g < groups; ++g) {
+              group(min(g + 1, groups - 1), ahead);
+              float2 so_far = state[w][g][lane];
+              add_tile(s, kc, so_far.x, so_far.y);
+              state[w][g][lane] = so_far;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[e] = ahead[e];
+            }
+          } else {
+            for (int g = 0; g < groups; ++g) {
+              m = state[w][g][lane].x;
+              l = state[w][g][lane].y;
+              acc4 s[4];
+              group(g, s);
+              finish(g, s);
+              state[w][g][lane] = make_float2(m, l);
+            }
+          }
         }
-        float top = s[0][0];
-#pragma unroll
-        for (int e = 1; e < 16; ++e) top = vmax(top, s[e >> 2][e & 3]);
-        const float now = vmax(m[g], top * x.kc), ref = now == -__builtin_inff() ? 0.f : now;
-        float sum = 0.f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sum += fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], x.kc, -ref));
-        l[g] = l[g] * fast_exp2(m[g] - ref) + sum;
-        m[g] = now;
       }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) raw[i] = next[i];
+      kc = kc_next;
+      ok = ok_next;
     }
+    for (int g = 0; g < groups; ++g) {
+      if constexpr (NG > 1) {
+        m = state[w][g][lane].x;
+        l = state[w][g][lane].y;
+      }
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      if (g >= groups) break;
-#pragma unroll
-      for (int o = 16; o < kWave; o <<= 1) merge(m[g], l[g], __shfl_xor(m[g], o), __shfl_xor(l[g], o));
-      if (lane < kGroup) part[w][g * kGroup + lane] = make_float2(m[g], l[g]);
+      for (int o = 16; o < kWave; o <<= 1) merge(m, l, __shfl_xor(m, o), __shfl_xor(l, o));
+      if (lane < kGroup) part[w][g * kGroup + lane] = make_float2(m, l);
     }
     __syncthreads();
-    if (tid < kPairs && p0 + tid < pairs) {
+    if (tid < NG * kGroup && p0 + tid < pairs) {
       float2 x = part[0][tid];
 #pragma unroll
       for (int i = 1; i < kWaves; ++i) merge(x.x, x.y, part[i][tid].x, part[i][tid].y);
@@ -180,10 +317,21 @@ __global__ __launch_bounds__(kThreads) void weigh_rows(WeightArgs a) {
   }
 }
 
-// Each pair's log2 of the sum over all its chunks (+infinity if it sees no token): a wave a row, 16 lanes a head.
+// log2 of a pair's sum over all n chunks, by 16 lanes together; +infinity if it sees no token.
+__device__ __forceinline__ float joined(const float2* src, int n) {
+  float m = -__builtin_inff(), l = 0.f;
+  for (int i = lane_id() & 15; i < n; i += 16) merge(m, l, src[i].x, src[i].y);
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) merge(m, l, __shfl_xor(m, o), __shfl_xor(l, o));
+  return l == 0.f ? __builtin_inff() : m + log2f(l);
+}
+
+// Every pair's, a wave four heads of a row.
 __global__ __launch_bounds__(kThreads) void weigh_join(WeightArgs a) {
-  const int lane = threadIdx.x & 63, j = lane & 15;
-  for (int row = blockIdx.x * kWaves + (threadIdx.x >> 6); row < a.b.n_rows; row += gridDim.x * kWaves) {
+  const int lane = threadIdx.x & 63, quads = (a.hq + 3) / 4;
+  const int64_t items = (int64_t)a.b.n_rows * quads;
+  for (int64_t i = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6); i < items; i += (int64_t)gridDim.x * kWaves) {
+    const int row = (int)(i / quads), h = (int)(i - (int64_t)row * quads) * 4 + (lane >> 4);
     int s = 0;  // the last sequence that begins at or before the row
     for (int n = a.b.n_seqs; n > 1;) {
       const int step = (n + kWave - 1) / kWave, probe = lane * step;
@@ -194,86 +342,233 @@ __global__ __launch_bounds__(kThreads) void weigh_join(WeightArgs a) {
     }
     const SeqRows r = seq_rows(a.s, a.b, a.c.B, s);
     if (row < r.row0 || row >= r.row0 + r.n) continue;
-    const int n = chunks_of(a, tiles_of(a, r));
-    for (int h = lane >> 4; h < a.hq; h += kWave / 16) {
-      const float2* src = a.stats + ((int64_t)row * a.hq + h) * a.chunks;
-      float m = -__builtin_inff(), l = 0.f;
-      for (int i = j; i < n; i += 16) merge(m, l, src[i].x, src[i].y);
-#pragma unroll
-      for (int o = 1; o < 16; o <<= 1) merge(m, l, __shfl_xor(m, o), __shfl_xor(l, o));
-      if (j == 0) a.lse[(int64_t)row * a.hq + h] = l == 0.f ? __builtin_inff() : m + log2f(l);
-    }
+    const int64_t pair = (int64_t)row * a.hq + min(h, a.hq - 1);
+    const float x = joined(a.stats + pair * a.chunks, chunks_of(a, tiles_of(a, r)));
+    if ((lane & 15) == 0 && h < a.hq) a.lse[pair] = x;
   }
 }
 
+// A tile's sums over the lanes of a row of 16; lane c of them takes token c.
+__device__ __forceinline__ float row_sums(const float (&acc)[16], int lane) {
+  float sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    float y = acc[e];
+    y += __uint_as_float(row_move<0x128>(__float_as_uint(y)));
+    y += __uint_as_float(row_move<0x124>(__float_as_uint(y)));
+    y += __uint_as_float(row_move<0x122>(__float_as_uint(y)));
+    y += __uint_as_float(row_move<0x121>(__float_as_uint(y)));
+    if ((lane & 15) == e) sum = y;
+  }
+  return sum;
+}
+
+// acc += the weights of a group of 16 pairs from pg on: products s, taken to the exponent by kc, each column's logarithm sub.
+__device__ __forceinline__ void add_weights(const WeightArgs& a, const SeqRows& r, const acc4 (&s)[4], float kc, float sub, int t, int pg,
+                                            int pairs, int lane, float (&acc)[16]) {
+  if (t * kTile + kTile - 1 > r.len + pg / a.G) {
+    const int first = t * kTile + 16 * (lane >> 4), see = r.len + min(pg + (lane & 15), pairs - 1) / a.G;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] += first + e > see ? 0.f : fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], kc, -sub));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] += fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], kc, -sub));
+  }
+}
+
+// Calls of many pairs, whose sums are in a.lse: a wave a tile, whose operands stay in registers for all pairs.  q is staged kAll pairs
+// at a time, once for all of the workgroup's tiles where a sequence has no more.
 template <int FMT>
-__global__ __launch_bounds__(kThreads) void weigh_tokens(WeightArgs a) {
+__global__ __launch_bounds__(kThreads, 2) void weigh_tokens(WeightArgs a) {
+  constexpr int kAll = 256;
+  __shared__ bf16x8 qs[kAll / kGroup][4][kWave];
+  __shared__ float lse[kAll];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Item it = item_of(a, a.token_wgs);
   const SeqRows r = seq_rows(a.s, a.b, a.c.B, it.seq);
   // positions up to the width are written, whether or not the table reaches them
   const int end = (int)min((int64_t)r.len + r.n, (int64_t)a.width), T = (end + kTile - 1) / kTile, pairs = r.n * a.G;
+  // tiles i T / n .. (i + 1) T / n of the sequence
+  const int n = min(a.token_wgs, (T + kWaves - 1) / kWaves);
+  if (it.i >= n) return;
+  const int t0 = (int)((int64_t)it.i * T / n), t1 = (int)((int64_t)(it.i + 1) * T / n);
   const int held = a.held[it.seq];
   const int64_t row = ((int64_t)it.seq * a.c.hkv + it.head) * a.width;
-  for (int t = it.i * kWaves + w; t < T; t += a.token_wgs * kWaves) {
-    const int at = t * kTile + lane;
+  KeyTiles<kWaves> tiles(a, it.seq, t0 + w, t1);
+  u32x4 raw[8] = {};
+  float kc = 0.f;
+  bool ok = t0 + w < t1 && tiles.load(a, it.head, t0 + w, raw, kc);
+  for (int tw = t0; tw < t1; tw += kWaves) {
+    const int t = tw + w, at = t * kTile + lane;
     float old = 0.f;
-    if (at < end && at < held) old = a.weights[row + at];
+    if (t < t1 && at < end && at < held) old = a.weights[row + at];
+    keep_whole(raw);
     KeyTile x;
+    convert<FMT>(raw, x);
+    const float kc_now = kc;
+    const bool now = ok;
+    ok = t + kWaves < t1 && tiles.load(a, it.head, t + kWaves, raw, kc);
     float acc[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-    if (pairs > 0 && load_keys<FMT>(a, it.seq, it.head, t, x)) {
-      const int first = t * kTile + 16 * (lane >> 4);
-      for (int p0 = 0; p0 < pairs; p0 += kGroup) {
-        const int p = p0 + (lane & 15), i = min(p, pairs - 1) / a.G, g = min(p, pairs - 1) - i * a.G;
-        if (t * kTile > r.len + (min(p0 + kGroup, pairs) - 1) / a.G) continue;  // no pair of the group sees the tile
+    for (int p0 = 0; p0 < pairs; p0 += kAll) {
+      const int most = min(pairs - p0, kAll), groups = (most + kGroup - 1) / kGroup;
+      if (tw == t0 || pairs > kAll) {
+        __syncthreads();  // the pairs before are done with
+        if (tid < most) lse[tid] = a.lse[(int64_t)(r.row0 + (p0 + tid) / a.G) * a.hq + it.head * a.G + (p0 + tid) % a.G];
+        for (int g = w; g < groups; g += kWaves) {
+          bf16x8 q[4];
+          load_pair(a, r, it.head, p0 + g * kGroup + (lane & 15), pairs, q);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) qs[g][kk][lane] = q[kk];
+        }
+        __syncthreads();
+      }
+      if (!now) continue;
+      const auto group = [&](int g, acc4 (&s)[4]) {
         bf16x8 q[4];
-        load_pair(a, r, it.head, p, pairs, q);
-        const float lse = p < pairs ? a.lse[(int64_t)(r.row0 + i) * a.hq + it.head * a.G + g] : __builtin_inff();
-        acc4 s[4];
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) q[kk] = qs[g][kk][lane];
         products(x, q, s);
-        if (t * kTile + kTile - 1 > r.len + p0 / a.G) {
+      };
+      const auto sub_of = [&](int g) { return p0 + g * kGroup + (lane & 15) < pairs ? lse[g * kGroup + (lane & 15)] : __builtin_inff(); };
+      if (t * kTile + kTile - 1 <= r.len) {  // every row sees the whole tile: the next group's products pass beside this one's weights
+        acc4 s[4], next[4];
+        group(0, s);
+        for (int g = 0; g < groups; ++g) {
+          group(min(g + 1, groups - 1), next);
+          const float sub = sub_of(g);
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            acc[e] += first + e > r.len + i ? 0.f : fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], x.kc, -lse));
-        } else {
+          for (int e = 0; e < 16; ++e) acc[e] += fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], kc_now, -sub));
 #pragma unroll
-          for (int e = 0; e < 16; ++e) acc[e] += fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], x.kc, -lse));
+          for (int e = 0; e < 4; ++e) s[e] = next[e];
+        }
+      } else {
+        for (int g = 0; g < groups; ++g) {
+          const int pg = p0 + g * kGroup;
+          if (t * kTile > r.len + (min(pg + kGroup, pairs) - 1) / a.G) continue;  // no pair of the group sees the tile
+          acc4 s[4];
+          group(g, s);
+          add_weights(a, r, s, kc_now, sub_of(g), t, pg, pairs, lane, acc);
         }
       }
     }
-    // summed over the 16 lanes of a row; lane c of them takes token c
-    float sum = 0.f;
+    const float sum = row_sums(acc, lane);
+    if (t < t1 && at < end) a.out[row + at] = old + sum;
+  }
+}
+
+// Calls of few pairs a sequence: the workgroup joins the chunks of 16 pairs by itself.  Where the scores wait, a lane takes a token and
+// two tiles' loads are under way at once; otherwise the products are formed again.
+template <int FMT>
+__global__ __launch_bounds__(kThreads, 4) void weigh_tokens_few(WeightArgs a) {
+  __shared__ float lse[kGroup];
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const Item it = item_of(a, a.token_wgs);
+  const SeqRows r = seq_rows(a.s, a.b, a.c.B, it.seq);
+  const int end = (int)min((int64_t)r.len + r.n, (int64_t)a.width), T = (end + kTile - 1) / kTile, pairs = r.n * a.G;
+  if (it.i * kWaves >= T) return;
+  const int held = a.held[it.seq], in_table = tiles_of(a, r), n = chunks_of(a, in_table), step = a.token_wgs * kWaves;
+  const int64_t row = ((int64_t)it.seq * a.c.hkv + it.head) * a.width;
+  const auto stage_lse = [&](int p0) {
+    const int p = p0 + (tid >> 4);
+    const int64_t pair = (int64_t)(r.row0 + p / a.G) * a.hq + it.head * a.G + p % a.G;
+    const float x = p < pairs ? joined(a.stats + pair * a.chunks, n) : __builtin_inff();
+    if ((tid & 15) == 0) lse[tid >> 4] = x;
+  };
+  const int32_t* pages = a.s.table + (int64_t)it.seq * a.b.max_pages;
+  const auto page_of = [&](int t) {
+    const int slot = a.c.tiles == 2 ? t >> 1 : t;
+    return t < T && slot < a.b.max_pages ? pages[slot] : -1;
+  };
+  const int64_t slot = pairs > 0 ? first_slot(a, it.seq, in_table, pairs) : -1;
+  if (slot >= 0) {
+    // (scores of a tile without a page are whatever the workspace holds, and are not used; of one past the table none are read)
+    const auto load = [&](int t, float (&x)[kGroup], float& old, int& page) {
+      const float* src = a.scores + ((slot + min(t, in_table - 1)) * a.c.hkv + it.head) * a.waiting * kTile + lane;
+      const int at = t * kTile + lane;
+      page = page_of(t);
+      old = at < end && at < held ? a.weights[row + at] : 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float y = acc[e];
-      y += __uint_as_float(row_move<0x128>(__float_as_uint(y)));
-      y += __uint_as_float(row_move<0x124>(__float_as_uint(y)));
-      y += __uint_as_float(row_move<0x122>(__float_as_uint(y)));
-      y += __uint_as_float(row_move<0x121>(__float_as_uint(y)));
-      if ((lane & 15) == e) sum = y;
+      for (int p = 0; p < kGroup; ++p)
+        if (p < pairs) x[p] = src[p * kTile];
+    };
+    float x[kGroup], next[kGroup], old, old_next = 0.f;
+    int page, page_next = -1, t = it.i * kWaves + w;
+    load(t, x, old, page);
+    stage_lse(0);
+    __syncthreads();
+    for (; t < T; t += step) {
+      if (t + step < T) load(t + step, next, old_next, page_next);
+      const int at = t * kTile + lane;
+      float sum = 0.f;
+      if (page >= 0 && page < a.c.n_pages) {
+#pragma unroll
+        for (int p = 0; p < kGroup; ++p)
+          if (p < pairs) sum += at > r.len + p / a.G ? 0.f : fast_exp2(x[p] - lse[p]);
+      }
+      if (at < end) a.out[row + at] = old + sum;
+#pragma unroll
+      for (int p = 0; p < kGroup; ++p) x[p] = next[p];
+      old = old_next;
+      page = page_next;
     }
+    return;
+  }
+  for (int t0 = it.i * kWaves; t0 < T; t0 += step) {
+    const int t = t0 + w, at = t * kTile + lane;
+    const float old = at < end && at < held ? a.weights[row + at] : 0.f;
+    u32x4 raw[8] = {};
+    float kc = 0.f;
+    KeyTiles<kWaves> tiles(a, it.seq, t, t + 1);
+    const bool ok = t < T && tiles.load(a, it.head, t, raw, kc);
+    keep_whole(raw);
+    float acc[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+    for (int p0 = 0; p0 < pairs; p0 += kGroup) {
+      __syncthreads();  // the pairs before are done with
+      stage_lse(p0);
+      __syncthreads();
+      if (!ok || t * kTile > r.len + (min(p0 + kGroup, pairs) - 1) / a.G) continue;  // (no pair of the group sees the tile)
+      bf16x8 q[4];
+      load_pair(a, r, it.head, p0 + (lane & 15), pairs, q);
+      acc4 s[4];
+      keep_whole(raw);
+      products<FMT>(raw, q, s);
+      add_weights(a, r, s, kc, lse[lane & 15], t, p0, pairs, lane, acc);
+    }
+    const float sum = row_sums(acc, lane);
     if (at < end) a.out[row + at] = old + sum;
   }
 }
 
-// Chunks of a sequence's tokens whose statistics are kept apart, and the workspace.
+// Chunks of a sequence's tokens whose statistics are kept apart, room for scores, and the workspace.
 struct Plan {
-  int chunks;
-  size_t lse, bytes;  // where the pairs' sums over all chunks begin
+  int chunks, waiting;
+  int64_t slots;
+  size_t lse, scores, bytes;  // where they begin
 };
 Plan plan_of(const CacheDims& c, const BatchDims& b, int hq) {
-  const int64_t heads = (int64_t)b.n_seqs * c.hkv, pairs = (int64_t)b.n_rows * hq;
-  if (heads == 0 || pairs == 0) return Plan{1, 0, 0};
+  const int64_t heads = (int64_t)b.n_seqs * c.hkv, pairs = (int64_t)b.n_rows * hq, G = hq / c.hkv;
+  if (heads == 0 || pairs == 0) return Plan{1, 0, 0, 0, 0, 0};
   // Enough workgroups for the GPU, and 16 MB of statistics at most but for calls of very many rows.  The space for them
   // does not shrink as rows are added, so that a workspace is enough for fewer rows, too.
   constexpr int64_t kMost = (int64_t)1 << 21;
-  const int64_t want = heads < 128 ? (1024 + heads - 1) / heads : 8, fit = kMost / pairs;
+  const int64_t target = pairs > kGroup * (int64_t)c.hkv * b.n_seqs ? 512 : 1536;
+  const int64_t want = heads < target / 3 ? (target + heads - 1) / heads : 3, fit = kMost / pairs;
   const int64_t chunks = fit < 1 ? 1 : want < fit ? want : fit;
-  const int64_t space = pairs > kMost ? pairs : pairs * want < kMost ? pairs * want : kMost;
-  const size_t lse = ((size_t)space * sizeof(float2) + 255) & ~(size_t)255;
-  return Plan{(int)chunks, lse, lse + (size_t)pairs * sizeof(float)};
+  const int64_t wide = heads < 512 ? (1536 + heads - 1) / heads : 3, space = pairs > kMost ? pairs : pairs * wide < kMost ? pairs * wide : kMost;
+  // Scores of sequences of average rows or fewer wait, if that is one product's pairs, for as many tiles as the cache has (forks have
+  // more together) or 256 MB hold.
+  const int64_t rows = (b.n_rows + b.n_seqs - 1) / b.n_seqs, most = kGroup / G;
+  const int waiting = b.n_seqs > kScoreSeqs ? 0 : (int)(G * (rows < most ? rows : most));
+  const int64_t tiles = (int64_t)c.n_pages * c.tiles, slot = (int64_t)c.hkv * waiting * kTile * (int64_t)sizeof(float);
+  const int64_t room = slot == 0 ? 0 : ((int64_t)256 << 20) / slot, slots = slot == 0 ? 0 : tiles < room ? tiles : room;
+  const auto up = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const size_t lse = up((size_t)space * sizeof(float2)), scores = lse + up((size_t)pairs * sizeof(float));
+  const size_t area = slot == 0 ? 0 : (size_t)(tiles * slot < ((int64_t)256 << 20) ? tiles * slot : (int64_t)256 << 20);
+  return Plan{(int)chunks, rows <= most ? waiting : 0, slots, lse, scores, scores + area};
 }
 
 }  // namespace
@@ -285,18 +580,29 @@ hipError_t launch_cache_weights(const CacheDims& c, const BatchDims& b, const Se
                                 int width, const int32_t* held, void* ws, hipStream_t stream) {
   const Plan p = plan_of(c, b, hq);
   const int64_t heads = (int64_t)b.n_seqs * c.hkv;
-  int64_t wgs = (4096 + heads - 1) / heads;
+  const bool join = (int64_t)b.n_rows * (hq / c.hkv) > (int64_t)kGroup * b.n_seqs;
+  int64_t wgs = ((join ? 512 : 1536) + heads - 1) / heads;
   const int64_t most = ((int64_t)width + kTile * kWaves - 1) / (kTile * kWaves);
   wgs = wgs > most ? most : wgs;
+  char* w = reinterpret_cast<char*>(ws);
   const WeightArgs a{c, b, s, q, qs, pages, scales, weights, out, held, width, hq, hq / c.hkv, p.chunks, (int)wgs, scale * kLog2e,
-                     reinterpret_cast<float2*>(ws), reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + p.lse)};
-  const int64_t join = (b.n_rows + kWaves - 1) / kWaves;
+                     p.waiting, p.slots, reinterpret_cast<float2*>(w), reinterpret_cast<float*>(w + p.lse),
+                     reinterpret_cast<float*>(w + p.scores)};
   const dim3 rows((unsigned)(heads * p.chunks)), tokens((unsigned)(heads * wgs)), threads(kThreads);
-  if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_rows<kCacheE4M3>), rows, threads, 0, stream, a);
-  else hipLaunchKernelGGL((weigh_rows<kCacheInt8>), rows, threads, 0, stream, a);
-  hipLaunchKernelGGL(weigh_join, dim3((unsigned)(join < 4096 ? join : 4096)), threads, 0, stream, a);
-  if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_tokens<kCacheE4M3>), tokens, threads, 0, stream, a);
-  else hipLaunchKernelGGL((weigh_tokens<kCacheInt8>), tokens, threads, 0, stream, a);
+  if (join) {
+    const int64_t items = ((int64_t)b.n_rows * ((hq + 3) / 4) + kWaves - 1) / kWaves;
+    const dim3 joins((unsigned)(items < 4096 ? items : 4096));
+    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_rows<kCacheE4M3, kGroups>), rows, threads, 0, stream, a);
+    else hipLaunchKernelGGL((weigh_rows<kCacheInt8, kGroups>), rows, threads, 0, stream, a);
+    hipLaunchKernelGGL(weigh_join, joins, threads, 0, stream, a);
+    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_tokens<kCacheE4M3>), tokens, threads, 0, stream, a);
+    else hipLaunchKernelGGL((weigh_tokens<kCacheInt8>), tokens, threads, 0, stream, a);
+  } else {
+    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_rows<kCacheE4M3, 1>), rows, threads, 0, stream, a);
+    else hipLaunchKernelGGL((weigh_rows<kCacheInt8, 1>), rows, threads, 0, stream, a);
+    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_tokens_few<kCacheE4M3>), tokens, threads, 0, stream, a);
+    else hipLaunchKernelGGL((weigh_tokens_few<kCacheInt8>), tokens, threads, 0, stream, a);
+  }
   return hipGetLastError();
 }
 
