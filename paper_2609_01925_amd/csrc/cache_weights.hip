@@ -5,6 +5,8 @@
 // tokens, and weigh_tokens takes the chunks' together and forms the weights, a wave a tile of 64 tokens, summed over the pairs in a
 // fixed order and without atomics.  Where a sequence has few pairs, x itself waits in the workspace, 4 bytes a pair and token where
 // the keys are 128; where it has many, the products are formed again and a launch between the two joins the chunks.
+#include <type_traits>
+
 #include "cache_device.h"
 
 namespace crisp {
@@ -13,8 +15,8 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kGroup = 16;                  // pairs of one product
-constexpr int kGroups = 8;                  // of a pass over the keys
-constexpr int kPairs = kGroup * kGroups;
+constexpr int kOwn = 4;                     // groups of a wave in calls of many pairs
+constexpr int kPairs = kGroup * kWaves * kOwn;  // of a pass over the keys there
 constexpr int kScoreSeqs = 1024;            // sequences of a call whose scores may wait: each workgroup adds up those before its own
 
 struct WeightArgs {
@@ -81,7 +83,9 @@ struct KeyTiles {
 
   // Tile t, the one after the last that was asked for: its codes, and what takes products with them to the base-2 exponent;
   // false if it has no page.
-  __device__ __forceinline__ bool load(const WeightArgs& a, int head, int t, u32x4 (&raw)[8], float& scale) {
+  // N = 8: a wave takes the whole tile, chunk 64 x + lane its x-th; N = 2: a workgroup, thread's chunks tid and tid + 256.
+  template <int N>
+  __device__ __forceinline__ bool load(const WeightArgs& a, int head, int t, u32x4 (&raw)[N], float& scale) {
     if (t >= tb + STEP * kWave) {
       tb = t;
       const int mine = t + STEP * lane_id(), slot = a.c.tiles == 2 ? mine >> 1 : mine;
@@ -94,36 +98,14 @@ struct KeyTiles {
     scale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(kc), i));
     if (page < 0) return false;
     const u32x4* src = reinterpret_cast<const u32x4*>(
-        a.pages + (((int64_t)page * a.c.hkv + head) * a.c.tiles + (a.c.tiles == 2 ? t & 1 : 0)) * (2 * kTileBytes)) + lane_id();
+        a.pages + (((int64_t)page * a.c.hkv + head) * a.c.tiles + (a.c.tiles == 2 ? t & 1 : 0)) * (2 * kTileBytes)) + (N == 8 ? lane_id() : (int)threadIdx.x);
 #pragma unroll
-    for (int x = 0; x < 8; ++x) raw[x] = src[x * kWave];
+    for (int x = 0; x < N; ++x) raw[x] = src[x * (N == 8 ? kWave : kThreads)];
     return true;
   }
 };
 
-// A tile of K as the products' operands: k[4 t + kk] is 16 tokens t of elements 32 g + 8 kk + [0, 8).
-struct KeyTile {
-  bf16x8 k[16];
-};
-template <int FMT>
-__device__ __forceinline__ void convert(const u32x4 (&raw)[8], KeyTile& x) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    x.k[2 * i] = codes_to_bf16<FMT>(raw[i][0], raw[i][1]);
-    x.k[2 * i + 1] = codes_to_bf16<FMT>(raw[i][2], raw[i][3]);
-  }
-}
-
-__device__ __forceinline__ void products(const KeyTile& x, const bf16x8 (&q)[4], acc4 (&s)[4]) {
-#pragma unroll
-  for (int t = 0; t < 4; ++t) s[t] = acc4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-    for (int t = 0; t < 4; ++t) s[t] = mfma16(x.k[4 * t + kk], q[kk], s[t]);
-}
-
-// The same from the codes, for a product or two of a tile: the operands are not all held at once.
+// s[t] = the products of 16 tokens and 16 pairs, from the codes: K's operand (t, kk) is elements 32 g + 8 kk + [0, 8) of the tokens.
 template <int FMT>
 __device__ __forceinline__ void products(const u32x4 (&raw)[8], const bf16x8 (&q)[4], acc4 (&s)[4]) {
 #pragma unroll
@@ -150,6 +132,11 @@ __device__ __forceinline__ void load_pair(const WeightArgs& a, const SeqRows& r,
   }
 }
 
+// Where pair p's statistics are.
+__device__ __forceinline__ int64_t pair_of(const WeightArgs& a, const SeqRows& r, int head, int p) {
+  return (int64_t)(r.row0 + p / a.G) * a.hq + head * a.G + p % a.G;
+}
+
 // (m, l) of two disjoint sets of keys together.
 __device__ __forceinline__ void merge(float& m, float& l, float m2, float l2) {
   const float top = vmax(m, m2);
@@ -158,26 +145,27 @@ __device__ __forceinline__ void merge(float& m, float& l, float m2, float l2) {
   m = top;
 }
 
+// The four lanes of a column together.
+__device__ __forceinline__ void column(float& m, float& l) {
+#pragma unroll
+  for (int o = 16; o < kWave; o <<= 1) merge(m, l, __shfl_xor(m, o), __shfl_xor(l, o));
+}
+
+// Scores of a tile that the pairs from p0 on do not see become -infinity.
+__device__ __forceinline__ void mask_tile(const WeightArgs& a, const SeqRows& r, int t, int p0, int lane, acc4 (&s)[4]) {
+  if (t * kTile + kTile - 1 <= r.len + p0 / a.G) return;
+  const int see = r.len + (p0 + (lane & 15)) / a.G, first = t * kTile + 16 * (lane >> 4);
+#pragma unroll
+  for (int e = 0; e < 16; ++e)
+    if (first + e > see) s[e >> 2][e & 3] = -__builtin_inff();
+}
+
 struct Item {
   int seq, head, i;
 };
 __device__ __forceinline__ Item item_of(const WeightArgs& a, int each) {
   const int sh = blockIdx.x / each;
   return Item{sh / a.c.hkv, sh % a.c.hkv, (int)blockIdx.x - sh * each};
-}
-
-// Pairs p0 .. of q as the products take them, in LDS; ends with a barrier.
-__device__ __forceinline__ int stage_pairs(const WeightArgs& a, const SeqRows& r, int head, int p0, int pairs, int w, int lane,
-                                           bf16x8 (&qs)[kGroups][4][kWave]) {
-  const int groups = min((pairs - p0 + kGroup - 1) / kGroup, kGroups);
-  for (int g = w; g < groups; g += kWaves) {
-    bf16x8 q[4];
-    load_pair(a, r, head, p0 + g * kGroup + (lane & 15), pairs, q);
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) qs[g][kk][lane] = q[kk];
-  }
-  __syncthreads();
-  return groups;
 }
 
 // A column's reference m and sum l of exp2(x - m) with a tile's 16 of this lane's, x = s kc, -infinity where masked.  The sums are
@@ -204,13 +192,10 @@ __device__ __forceinline__ void add_tile(const acc4 (&s)[4], float kc, float& m,
   l += more;
 }
 
-// NG groups of 16 pairs a pass over the keys: 1 where sequences have few pairs, with q in registers and room for more waves, or kGroups,
-// whose q is in LDS and which share the keys' conversion.
-template <int FMT, int NG>
-__global__ __launch_bounds__(kThreads, NG == 1 ? 4 : 2) void weigh_rows(WeightArgs a) {
-  __shared__ bf16x8 qs[NG == 1 ? 1 : kGroups][4][kWave];
-  __shared__ float2 part[kWaves][NG * kGroup];
-  __shared__ float2 state[NG == 1 ? 1 : kWaves][NG == 1 ? 1 : NG][kWave];  // each lane's maximum and sum of each group
+// Calls of few pairs a sequence, 16 at a time: a wave takes every fourth tile of the chunk, with q in registers.
+template <int FMT>
+__global__ __launch_bounds__(kThreads, 4) void weigh_rows_few(WeightArgs a) {
+  __shared__ float2 part[kWaves][kGroup];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Item it = item_of(a, a.chunks);
   const SeqRows r = seq_rows(a.s, a.b, a.c.B, it.seq);
@@ -218,103 +203,137 @@ __global__ __launch_bounds__(kThreads, NG == 1 ? 4 : 2) void weigh_rows(WeightAr
   if (pairs == 0 || it.i >= n) return;
   const int t0 = (int)((int64_t)it.i * T / n), t1 = (int)((int64_t)(it.i + 1) * T / n);
   int64_t slot = -1;
-  for (int p0 = 0; p0 < pairs; p0 += NG * kGroup) {
+  for (int p0 = 0; p0 < pairs; p0 += kGroup) {
     KeyTiles<kWaves> tiles(a, it.seq, t0 + w, t1);
     u32x4 raw[8] = {}, next[8] = {};
     float kc = 0.f, kc_next = 0.f;
     bool ok = false, ok_next = false;
     if (t0 + w < t1) ok = tiles.load(a, it.head, t0 + w, raw, kc);
-    int groups = 1;
-    bf16x8 q1[4];
-    if constexpr (NG == 1) {
-      load_pair(a, r, it.head, p0 + (lane & 15), pairs, q1);
-      if (p0 == 0) slot = first_slot(a, it.seq, T, pairs);
-    } else {
-      groups = stage_pairs(a, r, it.head, p0, pairs, w, lane, qs);
-    }
+    bf16x8 q[4];
+    load_pair(a, r, it.head, p0 + (lane & 15), pairs, q);
+    if (p0 == 0) slot = first_slot(a, it.seq, T, pairs);
     float m = -__builtin_inff(), l = 0.f;
-    if constexpr (NG > 1)
-      for (int g = 0; g < groups; ++g) state[w][g][lane] = make_float2(m, l);
     for (int t = t0 + w; t < t1; t += kWaves) {
       if (t + kWaves < t1) ok_next = tiles.load(a, it.head, t + kWaves, next, kc_next);
       keep_whole(raw);
       if (ok) {
-        const int first = t * kTile + 16 * (lane >> 4);  // position of this lane's first token
-        const auto finish = [&](int g, acc4 (&s)[4]) {
-          if (NG == 1 && slot >= 0 && (lane & 15) < pairs) {
-            f32x4* dst = reinterpret_cast<f32x4*>(
-                a.scores + (((slot + t) * a.c.hkv + it.head) * a.waiting + (lane & 15)) * kTile + 16 * (lane >> 4));
+        acc4 s[4];
+        products<FMT>(raw, q, s);
+        if (slot >= 0 && (lane & 15) < pairs) {
+          f32x4* dst = reinterpret_cast<f32x4*>(
+              a.scores + (((slot + t) * a.c.hkv + it.head) * a.waiting + (lane & 15)) * kTile + 16 * (lane >> 4));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) dst[e] = s[e] * kc;
-          }
-          if (t * kTile + kTile - 1 > r.len + (p0 + g * kGroup) / a.G) {
-            const int see = r.len + (p0 + g * kGroup + (lane & 15)) / a.G;
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (first + e > see) s[e >> 2][e & 3] = -__builtin_inff();
-          }
-          add_tile(s, kc, m, l);
-        };
-        if constexpr (NG == 1) {
-          acc4 s[4];
-          products<FMT>(raw, q1, s);
-          finish(0, s);
-        } else {
-          KeyTile x;
-          convert<FMT>(raw, x);
-          const auto group = [&](int g, acc4 (&s)[4]) {
-            bf16x8 q[4];
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk) q[kk] = qs[g][kk][lane];
-            products(x, q, s);
-          };
-          if (t * kTile + kTile - 1 <= r.len) {  // every row sees the whole tile: the next group's products pass beside this one's sums
-            acc4 s[4], ahead[4];
-            group(0, s);
-            for (int g = 0; g < groups; ++g) {
-              group(min(g + 1, groups - 1), ahead);
-              float2 so_far = state[w][g][lane];
-              add_tile(s, kc, so_far.x, so_far.y);
-              state[w][g][lane] = so_far;
-#pragma unroll
-              for (int e = 0; e < 4; ++e) s[e] = ahead[e];
-            }
-          } else {
-            for (int g = 0; g < groups; ++g) {
-              m = state[w][g][lane].x;
-              l = state[w][g][lane].y;
-              acc4 s[4];
-              group(g, s);
-              finish(g, s);
-              state[w][g][lane] = make_float2(m, l);
-            }
-          }
+          for (int e = 0; e < 4; ++e) dst[e] = s[e] * kc;
         }
+        mask_tile(a, r, t, p0, lane, s);
+        add_tile(s, kc, m, l);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) raw[i] = next[i];
       kc = kc_next;
       ok = ok_next;
     }
-    for (int g = 0; g < groups; ++g) {
-      if constexpr (NG > 1) {
-        m = state[w][g][lane].x;
-        l = state[w][g][lane].y;
-      }
-#pragma unroll
-      for (int o = 16; o < kWave; o <<= 1) merge(m, l, __shfl_xor(m, o), __shfl_xor(l, o));
-      if (lane < kGroup) part[w][g * kGroup + lane] = make_float2(m, l);
-    }
+    column(m, l);
+    if (lane < kGroup) part[w][lane] = make_float2(m, l);
     __syncthreads();
-    if (tid < NG * kGroup && p0 + tid < pairs) {
+    if (tid < kGroup && p0 + tid < pairs) {
       float2 x = part[0][tid];
 #pragma unroll
       for (int i = 1; i < kWaves; ++i) merge(x.x, x.y, part[i][tid].x, part[i][tid].y);
-      const int row = (p0 + tid) / a.G, h = it.head * a.G + (p0 + tid) % a.G;
-      a.stats[((int64_t)(r.row0 + row) * a.hq + h) * a.chunks + it.i] = x;
+      a.stats[pair_of(a, r, it.head, p0 + tid) * a.chunks + it.i] = x;
     }
     __syncthreads();
   }
+}
+
+// Calls of many pairs: the workgroup converts a tile of K once, into LDS, and each wave has NI groups of 16 pairs for all tiles, q and
+// what it gathers in registers (group w + 4 i is its i-th).  The next tile's codes are loaded and converted beside the products of this one.
+template <int FMT, int NI, typename Work>
+__device__ __forceinline__ void over_tiles(const WeightArgs& a, const SeqRows& r, const Item& it, int p0, int pairs, int t0, int t1,
+                                           bf16x8 (&kst)[2][16][kWave], Work work) {
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  bf16x8 q[NI][4];
+#pragma unroll
+  for (int i = 0; i < NI; ++i) load_pair(a, r, it.head, p0 + (w + kWaves * i) * kGroup + (lane & 15), pairs, q[i]);
+  KeyTiles<1> tiles(a, it.seq, t0, t1);
+  u32x4 raw[2] = {};  // chunks tid and tid + 256 of the tile
+  float kc = 0.f;
+  const auto stage = [&](int buf) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      asm("" : "+v"(raw[x]));
+      kst[buf][2 * (w + kWaves * x)][lane] = codes_to_bf16<FMT>(raw[x][0], raw[x][1]);
+      kst[buf][2 * (w + kWaves * x) + 1][lane] = codes_to_bf16<FMT>(raw[x][2], raw[x][3]);
+    }
+  };
+  bool ok = tiles.load(a, it.head, t0, raw, kc);
+  stage(0);
+  for (int t = t0, buf = 0; t < t1; ++t, buf ^= 1) {
+    const float kc_now = kc;
+    const bool now = ok;
+    ok = t + 1 < t1 && tiles.load(a, it.head, t + 1, raw, kc);
+    __syncthreads();  // this tile is staged, and the other buffer free
+    work(t, now, kc_now, q, kst[buf]);
+    if (t + 1 < t1) stage(buf ^ 1);
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ void products(const bf16x8 (&k)[16][kWave], const bf16x8 (&q)[4], int lane, acc4 (&s)[4]) {
+#pragma unroll
+  for (int t = 0; t < 4; ++t) s[t] = acc4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+    for (int t = 0; t < 4; ++t) s[t] = mfma16(k[4 * t + kk][lane], q[kk], s[t]);
+}
+
+// fn(std::integral_constant of the groups that a wave has), 1 .. kOwn.
+template <typename Fn>
+__device__ __forceinline__ void by_groups(int groups, Fn fn) {
+  const int own = (groups + kWaves - 1) / kWaves;
+  if (own == 1) fn(std::integral_constant<int, 1>{});
+  else if (own == 2) fn(std::integral_constant<int, 2>{});
+  else if (own == 3) fn(std::integral_constant<int, 3>{});
+  else fn(std::integral_constant<int, kOwn>{});
+}
+
+template <int FMT>
+__global__ __launch_bounds__(kThreads, 2) void weigh_rows(WeightArgs a) {
+  __shared__ bf16x8 kst[2][16][kWave];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Item it = item_of(a, a.chunks);
+  const SeqRows r = seq_rows(a.s, a.b, a.c.B, it.seq);
+  const int T = tiles_of(a, r), n = chunks_of(a, T), pairs = r.n * a.G;
+  if (pairs == 0 || it.i >= n) return;
+  const int t0 = (int)((int64_t)it.i * T / n), t1 = (int)((int64_t)(it.i + 1) * T / n);
+  for (int p0 = 0; p0 < pairs; p0 += kPairs)
+    by_groups((min(pairs - p0, kPairs) + kGroup - 1) / kGroup, [&](auto groups) {
+      constexpr int NI = decltype(groups)::value;
+      float m[NI], l[NI];
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        m[i] = -__builtin_inff();
+        l[i] = 0.f;
+      }
+      over_tiles<FMT, NI>(a, r, it, p0, pairs, t0, t1, kst, [&](int t, bool ok, float kc, const bf16x8 (&q)[NI][4], const bf16x8 (&k)[16][kWave]) {
+        if (!ok) return;
+        acc4 s[NI][4];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) products(k, q[i], lane, s[i]);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          mask_tile(a, r, t, p0 + (w + kWaves * i) * kGroup, lane, s[i]);
+          add_tile(s[i], kc, m[i], l[i]);
+        }
+      });
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        column(m[i], l[i]);
+        const int p = p0 + (w + kWaves * i) * kGroup + lane;
+        if (lane < kGroup && p < pairs) a.stats[pair_of(a, r, it.head, p) * a.chunks + it.i] = make_float2(m[i], l[i]);
+      }
+    });
 }
 
 // log2 of a pair's sum over all n chunks, by 16 lanes together; +infinity if it sees no token.
@@ -376,92 +395,77 @@ __device__ __forceinline__ void add_weights(const WeightArgs& a, const SeqRows& 
   }
 }
 
-// Calls of many pairs, whose sums are in a.lse: a wave a tile, whose operands stay in registers for all pairs.  q is staged kAll pairs
-// at a time, once for all of the workgroup's tiles where a sequence has no more.
+// The weights of calls of many pairs, whose sums are in a.lse.  Each wave's part of a tile waits in LDS for the next tile's barrier; pairs past
+// kPairs are added to what the ones before have left.
 template <int FMT>
 __global__ __launch_bounds__(kThreads, 2) void weigh_tokens(WeightArgs a) {
-  constexpr int kAll = 256;
-  __shared__ bf16x8 qs[kAll / kGroup][4][kWave];
-  __shared__ float lse[kAll];
+  __shared__ bf16x8 kst[2][16][kWave];
+  __shared__ float parts[2][kWaves][kTile];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Item it = item_of(a, a.token_wgs);
   const SeqRows r = seq_rows(a.s, a.b, a.c.B, it.seq);
   // positions up to the width are written, whether or not the table reaches them
   const int end = (int)min((int64_t)r.len + r.n, (int64_t)a.width), T = (end + kTile - 1) / kTile, pairs = r.n * a.G;
-  // tiles i T / n .. (i + 1) T / n of the sequence
-  const int n = min(a.token_wgs, (T + kWaves - 1) / kWaves);
+  const int n = min(a.token_wgs, T);
   if (it.i >= n) return;
   const int t0 = (int)((int64_t)it.i * T / n), t1 = (int)((int64_t)(it.i + 1) * T / n);
   const int held = a.held[it.seq];
   const int64_t row = ((int64_t)it.seq * a.c.hkv + it.head) * a.width;
-  KeyTiles<kWaves> tiles(a, it.seq, t0 + w, t1);
-  u32x4 raw[8] = {};
-  float kc = 0.f;
-  bool ok = t0 + w < t1 && tiles.load(a, it.head, t0 + w, raw, kc);
-  for (int tw = t0; tw < t1; tw += kWaves) {
-    const int t = tw + w, at = t * kTile + lane;
-    float old = 0.f;
-    if (t < t1 && at < end && at < held) old = a.weights[row + at];
-    keep_whole(raw);
-    KeyTile x;
-    convert<FMT>(raw, x);
-    const float kc_now = kc;
-    const bool now = ok;
-    ok = t + kWaves < t1 && tiles.load(a, it.head, t + kWaves, raw, kc);
-    float acc[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[e] = 0.f;
-    for (int p0 = 0; p0 < pairs; p0 += kAll) {
-      const int most = min(pairs - p0, kAll), groups = (most + kGroup - 1) / kGroup;
-      if (tw == t0 || pairs > kAll) {
-        __syncthreads();  // the pairs before are done with
-        if (tid < most) lse[tid] = a.lse[(int64_t)(r.row0 + (p0 + tid) / a.G) * a.hq + it.head * a.G + (p0 + tid) % a.G];
-        for (int g = w; g < groups; g += kWaves) {
-          bf16x8 q[4];
-          load_pair(a, r, it.head, p0 + g * kGroup + (lane & 15), pairs, q);
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk) qs[g][kk][lane] = q[kk];
-        }
-        __syncthreads();
-      }
-      if (!now) continue;
-      const auto group = [&](int g, acc4 (&s)[4]) {
-        bf16x8 q[4];
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) q[kk] = qs[g][kk][lane];
-        products(x, q, s);
-      };
-      const auto sub_of = [&](int g) { return p0 + g * kGroup + (lane & 15) < pairs ? lse[g * kGroup + (lane & 15)] : __builtin_inff(); };
-      if (t * kTile + kTile - 1 <= r.len) {  // every row sees the whole tile: the next group's products pass beside this one's weights
-        acc4 s[4], next[4];
-        group(0, s);
-        for (int g = 0; g < groups; ++g) {
-          group(min(g + 1, groups - 1), next);
-          const float sub = sub_of(g);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) acc[e] += fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], kc_now, -sub));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[e] = next[e];
-        }
-      } else {
-        for (int g = 0; g < groups; ++g) {
-          const int pg = p0 + g * kGroup;
-          if (t * kTile > r.len + (min(pg + kGroup, pairs) - 1) / a.G) continue;  // no pair of the group sees the tile
-          acc4 s[4];
-          group(g, s);
-          add_weights(a, r, s, kc_now, sub_of(g), t, pg, pairs, lane, acc);
-        }
-      }
-    }
-    const float sum = row_sums(acc, lane);
-    if (t < t1 && at < end) a.out[row + at] = old + sum;
+  if (pairs == 0) {
+    for (int at = t0 * kTile + tid; at < min(t1 * kTile, end); at += kThreads) a.out[row + at] = at < held ? a.weights[row + at] : 0.f;
+    return;
   }
+  for (int p0 = 0; p0 < pairs; p0 += kPairs)
+    by_groups((min(pairs - p0, kPairs) + kGroup - 1) / kGroup, [&](auto groups) {
+      constexpr int NI = decltype(groups)::value;
+      float sub[NI];
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const int p = p0 + (w + kWaves * i) * kGroup + (lane & 15);
+        sub[i] = p < pairs ? a.lse[pair_of(a, r, it.head, p)] : __builtin_inff();
+      }
+      float old = 0.f;
+      const auto start = [&](int t) {  // of a tile that this wave writes
+        const int at = t * kTile + lane;
+        if (p0 > 0) old = at < end ? a.out[row + at] : 0.f;
+        else old = at < end && at < held ? a.weights[row + at] : 0.f;
+      };
+      const auto write = [&](int t) {
+        const int at = t * kTile + lane, buf = (t - t0) & 1;
+        if (at < end) a.out[row + at] = old + ((parts[buf][0][lane] + parts[buf][1][lane]) + (parts[buf][2][lane] + parts[buf][3][lane]));
+      };
+      over_tiles<FMT, NI>(a, r, it, p0, pairs, t0, t1, kst, [&](int t, bool ok, float kc, const bf16x8 (&q)[NI][4], const bf16x8 (&k)[16][kWave]) {
+        if (t > t0 && w == ((t - 1) & 3)) write(t - 1);
+        if (w == (t & 3)) start(t);
+        float acc[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+        if (ok) {
+          acc4 s[NI][4];
+#pragma unroll
+          for (int i = 0; i < NI; ++i) products(k, q[i], lane, s[i]);
+          if (t * kTile + kTile - 1 <= r.len + p0 / a.G) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) acc[e] += fast_exp2(__builtin_fmaf(s[i][e >> 2][e & 3], kc, -sub[i]));
+          } else {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) add_weights(a, r, s[i], kc, sub[i], t, p0 + (w + kWaves * i) * kGroup, pairs, lane, acc);
+          }
+        }
+        parts[(t - t0) & 1][w][lane] = row_sums(acc, lane);
+      });
+      if (w == ((t1 - 1) & 3)) write(t1 - 1);
+      __syncthreads();
+    });
 }
 
-// Calls of few pairs a sequence: the workgroup joins the chunks of 16 pairs by itself.  Where the scores wait, a lane takes a token and
-// two tiles' loads are under way at once; otherwise the products are formed again.
-template <int FMT>
-__global__ __launch_bounds__(kThreads, 4) void weigh_tokens_few(WeightArgs a) {
+// Calls of few pairs a sequence: the workgroup joins the chunks of 16 pairs by itself.  Where scores wait (SCORES: they do for most
+// sequences), a lane takes a token: all latency, so registers are held to what lets a CU have eight workgroups, at the cost of
+// spills where the products are formed again for the others.
+template <int FMT, bool SCORES>
+__global__ __launch_bounds__(kThreads, SCORES ? 8 : 4) void weigh_tokens_few(WeightArgs a) {
   __shared__ float lse[kGroup];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Item it = item_of(a, a.token_wgs);
@@ -472,8 +476,7 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_tokens_few(WeightArgs a) {
   const int64_t row = ((int64_t)it.seq * a.c.hkv + it.head) * a.width;
   const auto stage_lse = [&](int p0) {
     const int p = p0 + (tid >> 4);
-    const int64_t pair = (int64_t)(r.row0 + p / a.G) * a.hq + it.head * a.G + p % a.G;
-    const float x = p < pairs ? joined(a.stats + pair * a.chunks, n) : __builtin_inff();
+    const float x = p < pairs ? joined(a.stats + pair_of(a, r, it.head, p) * a.chunks, n) : __builtin_inff();
     if ((tid & 15) == 0) lse[tid >> 4] = x;
   };
   const int32_t* pages = a.s.table + (int64_t)it.seq * a.b.max_pages;
@@ -481,8 +484,8 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_tokens_few(WeightArgs a) {
     const int slot = a.c.tiles == 2 ? t >> 1 : t;
     return t < T && slot < a.b.max_pages ? pages[slot] : -1;
   };
-  const int64_t slot = pairs > 0 ? first_slot(a, it.seq, in_table, pairs) : -1;
-  if (slot >= 0) {
+  const int64_t slot = SCORES && pairs > 0 ? first_slot(a, it.seq, in_table, pairs) : -1;
+  if (SCORES && slot >= 0) {
     // (scores of a tile without a page are whatever the workspace holds, and are not used; of one past the table none are read)
     const auto load = [&](int t, float (&x)[kGroup], float& old, int& page) {
       const float* src = a.scores + ((slot + min(t, in_table - 1)) * a.c.hkv + it.head) * a.waiting * kTile + lane;
@@ -581,7 +584,7 @@ hipError_t launch_cache_weights(const CacheDims& c, const BatchDims& b, const Se
   const Plan p = plan_of(c, b, hq);
   const int64_t heads = (int64_t)b.n_seqs * c.hkv;
   const bool join = (int64_t)b.n_rows * (hq / c.hkv) > (int64_t)kGroup * b.n_seqs;
-  int64_t wgs = ((join ? 512 : 1536) + heads - 1) / heads;
+  int64_t wgs = ((join ? 512 : 2048) + heads - 1) / heads;
   const int64_t most = ((int64_t)width + kTile * kWaves - 1) / (kTile * kWaves);
   wgs = wgs > most ? most : wgs;
   char* w = reinterpret_cast<char*>(ws);
@@ -592,16 +595,21 @@ hipError_t launch_cache_weights(const CacheDims& c, const BatchDims& b, const Se
   if (join) {
     const int64_t items = ((int64_t)b.n_rows * ((hq + 3) / 4) + kWaves - 1) / kWaves;
     const dim3 joins((unsigned)(items < 4096 ? items : 4096));
-    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_rows<kCacheE4M3, kGroups>), rows, threads, 0, stream, a);
-    else hipLaunchKernelGGL((weigh_rows<kCacheInt8, kGroups>), rows, threads, 0, stream, a);
+    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_rows<kCacheE4M3>), rows, threads, 0, stream, a);
+    else hipLaunchKernelGGL((weigh_rows<kCacheInt8>), rows, threads, 0, stream, a);
     hipLaunchKernelGGL(weigh_join, joins, threads, 0, stream, a);
     if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_tokens<kCacheE4M3>), tokens, threads, 0, stream, a);
     else hipLaunchKernelGGL((weigh_tokens<kCacheInt8>), tokens, threads, 0, stream, a);
   } else {
-    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_rows<kCacheE4M3, 1>), rows, threads, 0, stream, a);
-    else hipLaunchKernelGGL((weigh_rows<kCacheInt8, 1>), rows, threads, 0, stream, a);
-    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_tokens_few<kCacheE4M3>), tokens, threads, 0, stream, a);
-    else hipLaunchKernelGGL((weigh_tokens_few<kCacheInt8>), tokens, threads, 0, stream, a);
+    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_rows_few<kCacheE4M3>), rows, threads, 0, stream, a);
+    else hipLaunchKernelGGL((weigh_rows_few<kCacheInt8>), rows, threads, 0, stream, a);
+    if (p.waiting > 0) {
+      if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_tokens_few<kCacheE4M3, true>), tokens, threads, 0, stream, a);
+      else hipLaunchKernelGGL((weigh_tokens_few<kCacheInt8, true>), tokens, threads, 0, stream, a);
+    } else {
+      if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_tokens_few<kCacheE4M3, false>), tokens, threads, 0, stream, a);
+      else hipLaunchKernelGGL((weigh_tokens_few<kCacheInt8, false>), tokens, threads, 0, stream, a);
+    }
   }
   return hipGetLastError();
 }
