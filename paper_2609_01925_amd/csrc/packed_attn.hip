@@ -210,59 +210,67 @@ __device__ __forceinline__ int key_of(int key0, int sub, int i, int l) {
   return key0 + 32 * sub + 8 * (i >> 2) + 4 * (l >> 5) + (i & 3);
 }
 
-// add_values for an edge tile in which some value is not finite: a masked one, whose p is 0, must not reach the row.  The finite ones
-// are summed as ever; a row gets an infinity of each sign that it sees in an element, NaN counting as both.
-__device__ __forceinline__ void add_mixed_values(int tile, const Operands& at, const Probs& p, int key0, int lo, int row, int l,
-                                                 f32x16 (&o)[4]) {
-#pragma unroll
-  for (int db = 0; db < 4; ++db) {
-    f32x16 up = zero16(), down = zero16();
-#pragma unroll
-    for (int y = 0; y < 2 * kSubs; ++y) {
-      bf16x8 seen;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int key = key_of(key0, y >> 1, 8 * (y & 1) + e, l);
-        seen[e] = (__bf16)(key >= lo && key <= row ? 1.f : 0.f);
-      }
-      u32x4 raw = __builtin_bit_cast(u32x4, at.value(tile, 4 * y + db)), pos, neg;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t keep = 0, plus = 0, minus = 0;
-#pragma unroll
-        for (int z = 0; z < 32; z += 16) {
-          const uint32_t x = (raw[i] >> z) & 0xffffu;
-          const bool fin = (x & 0x7f80u) != 0x7f80u;
-          if (fin) keep |= x << z;
-          if (!fin && x != 0xff80u) plus |= 0x3f80u << z;
-          if (!fin && x != 0x7f80u) minus |= 0x3f80u << z;
-        }
-        raw[i] = keep;
-        pos[i] = plus;
-        neg[i] = minus;
-      }
-      o[db] = mfma32(__builtin_bit_cast(bf16x8, raw), p[y >> 1][y & 1], o[db]);
-      up = mfma32(__builtin_bit_cast(bf16x8, pos), seen, up);
-      down = mfma32(__builtin_bit_cast(bf16x8, neg), seen, down);
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      o[db][i] += (up[i] > 0.f ? __builtin_inff() : 0.f) - (down[i] > 0.f ? __builtin_inff() : 0.f);
-  }
-}
-
-// Whether this wave's part of a tile, the rows that it fetched itself, holds a value that is not finite.
-__device__ __forceinline__ bool odd_values(int tile, int w, int l) {
+// A masked value that is not finite must not reach a row whose p it meets is 0.  In an edge tile, which rows see in part, a wave
+// makes such values of the rows that it fetched itself 0; whether there were any.
+__device__ __forceinline__ bool only_finite(int tile, int w, int l) {
   typedef __attribute__((__vector_size__(2 * sizeof(uint16_t)))) uint16_t u16x2;
+  typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
   asm volatile("" ::: "memory");  // behind the wait for the loads
+  u32x4 x[kKeys / 16];
   u16x2 top = {0, 0};
 #pragma unroll
   for (int i = 0; i < kKeys / 16; ++i) {
-    const u32x4 x = __builtin_bit_cast(u32x4, lds_chunk(tile + (16 * i + 4 * w) * 256 + 16 * l));
+    x[i] = __builtin_bit_cast(u32x4, lds_chunk(tile + (16 * i + 4 * w) * 256 + 16 * l));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[e] & 0x7fff7fffu));
+    for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[i][e] & 0x7fff7fffu));
   }
-  return __ballot(top[0] >= 0x7f80 || top[1] >= 0x7f80) != 0;
+  if (__ballot(top[0] >= 0x7f80 || top[1] >= 0x7f80) == 0) return true;
+#pragma unroll
+  for (int i = 0; i < kKeys / 16; ++i) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if ((x[i][e] & 0x7f80u) == 0x7f80u) x[i][e] &= 0xffff0000u;
+      if ((x[i][e] & 0x7f800000u) == 0x7f800000u) x[i][e] &= 0xffffu;
+    }
+    *(lds_u32x4*)(uint32_t)(tile + (16 * i + 4 * w) * 256 + 16 * l) = x[i];
+  }
+  return false;
+}
+
+// What only_finite left out of the wave's 32 rows, from row0 on and stored already: an element becomes an infinity for each sign that the row
+// sees among keys [kd, row] of V, NaN counting as both.  A lane has two elements and goes over the keys once, with the rows.
+__device__ __forceinline__ void add_infinities(const PackedArgs& a, int head, int kd, int row0, int lo, bool covered, int l) {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");  // the rows as other lanes have stored them
+  const uint16_t* v = a.v + head / a.G * a.vs.head + 2 * l;
+  const unsigned long long rows = __ballot(covered);
+  int from = -1, key = 0;
+  float up[2] = {0.f, 0.f}, down[2] = {0.f, 0.f};
+  for (int r = 0; r < 32; ++r) {
+    if ((rows >> r & 1) == 0) continue;
+    const int begin = __builtin_amdgcn_readlane(lo, r);
+    if (begin != from) {
+      from = begin;
+      key = max(kd, begin);
+      up[0] = up[1] = down[0] = down[1] = 0.f;
+    }
+    for (; key <= row0 + r; ++key) {
+      const uint32_t x = *reinterpret_cast<const uint32_t*>(v + key * a.vs.row);
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const uint32_t y = z == 0 ? x & 0xffffu : x >> 16;
+        if ((y & 0x7f80u) == 0x7f80u) {
+          if (y != 0xff80u) up[z] = __builtin_inff();
+          if (y != 0x7f80u) down[z] = __builtin_inff();
+        }
+      }
+    }
+    if (__ballot(up[0] + up[1] + down[0] + down[1] != 0.f)) {
+      uint32_t* dst = reinterpret_cast<uint32_t*>(a.o + head * a.os.head + (int64_t)(row0 + r) * a.os.row + 2 * l);
+      const uint32_t x = *dst;
+      const bf16x2 y = pack_bf16(__uint_as_float(x << 16) + up[0] - down[0], __uint_as_float(x & 0xffff0000u) + up[1] - down[1]);
+      *dst = __builtin_bit_cast(uint32_t, y);
+    }
+  }
 }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -272,7 +280,7 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 __global__ __launch_bounds__(kThreads, 2) void packed_attn(PackedArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __shared__ __attribute__((aligned(1024))) char smem[4 * kStage + kWaves * sizeof(int)];
-  int* odd_wave = reinterpret_cast<int*>(smem + 4 * kStage);
+  int* odd_wave = reinterpret_cast<int*>(smem + 4 * kStage);  // whether a wave has met values that are not finite
   const int lds0 = uniform((int)(size_t)smem);
   const auto kst = [&](int i) { return lds0 + i * kStage; };
   const auto vst = [&](int i) { return lds0 + (2 + i) * kStage; };
@@ -280,25 +288,6 @@ __global__ __launch_bounds__(kThreads, 2) void packed_attn(PackedArgs a) {
   int head, qb;
   if (!unit_of(a, blockIdx.x, head, qb)) return;
   const int q0 = qb * kRows, row = q0 + 32 * w + (l & 31);
-
-  // The begin of the first row's sequence, then of this lane's: the last begin at or before its row.
-  const int n_seqs = a.d.n_seqs;
-  const int s0 = uniform(seq_of_row(a.row_ptr, n_seqs, q0));
-  const int end = min(uniform(a.row_ptr[n_seqs]), a.d.n_rows), q_end = min(q0 + kRows, end);
-  if (s0 >= n_seqs || q_end <= q0) return;
-  const int head_lo = s0 < 0 ? q0 : min(max(uniform(a.row_ptr[s0]), 0), q0);
-  int lo = s0 < 0 ? 0x7fffffff : head_lo;
-  for (int from = s0 + 1; from < n_seqs; from += kWave) {
-    const int begin = from + l < n_seqs ? a.row_ptr[from + l] : 0x7fffffff;
-    const bool near = begin < q_end;
-    for (unsigned long long todo = __ballot(near); todo != 0; todo &= todo - 1) {
-      const int b = __builtin_amdgcn_readlane(begin, __builtin_ctzll(todo));
-      if (b <= row) lo = b;
-    }
-    if (~__ballot(near) != 0) break;
-  }
-  lo = max(lo, 0);
-  const bool covered = row < q_end && lo <= row;
 
   const int g = head / a.G;
   const Operands at(l);
@@ -309,13 +298,76 @@ __global__ __launch_bounds__(kThreads, 2) void packed_attn(PackedArgs a) {
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(src + 16 * kk);
   }
+
+  // The begin of the first row's sequence, then of this lane's: the last begin at or before its row.  Up to 63 sequences all
+  // of it comes from one load, a begin a lane.
+  const int n_seqs = a.d.n_seqs;
+  const bool few = n_seqs < kWave;
+  const int mine = few ? a.row_ptr[min(l, n_seqs)] : 0;
+  int s0, end, head_lo;
+  if (few) {
+    s0 = __popcll(__ballot(l <= n_seqs && mine <= q0)) - 1;
+    end = __builtin_amdgcn_readlane(mine, n_seqs);
+    head_lo = __builtin_amdgcn_readlane(mine, max(s0, 0));
+  } else {
+    s0 = uniform(seq_of_row(a.row_ptr, n_seqs, q0));
+    end = uniform(a.row_ptr[n_seqs]);
+    head_lo = uniform(a.row_ptr[max(s0, 0)]);
+  }
+  const int q_end = min(q0 + kRows, min(end, a.d.n_rows));
+  if (s0 >= n_seqs || q_end <= q0) return;
+  head_lo = s0 < 0 ? q0 : min(max(head_lo, 0), q0);
+  int lo = s0 < 0 ? 0x7fffffff : head_lo;
+  for (int from = few ? 0 : s0 + 1; from < n_seqs; from += kWave) {
+    const int begin = few ? mine : from + l < n_seqs ? a.row_ptr[from + l] : 0x7fffffff;
+    const bool near = begin < q_end && from + l < n_seqs;
+    for (unsigned long long todo = __ballot(near && from + l > s0); todo != 0; todo &= todo - 1) {
+      const int b = __builtin_amdgcn_readlane(begin, __builtin_ctzll(todo));
+      if (b <= row) lo = b;
+    }
+    if (~__ballot(near) != 0) break;
+  }
+  lo = max(lo, 0);
+  const bool covered = row < q_end && lo <= row;
+
   f32x16 o[4];
 #pragma unroll
   for (int db = 0; db < 4; ++db) o[db] = zero16();
   float m = -__builtin_inff(), sum = 0.f;
   f32x16 s[kSubs];
 
-  const int T = (q0 - head_lo) / kKeys, kd = head_lo + T * kKeys;
+  // Tiles of 64 keys from head_lo on: T whole ones, then the edge tiles, the last ending at q_end.
+  const int T = (q0 - head_lo) / kKeys, total = (q_end - head_lo + kKeys - 1) / kKeys;
+  const auto key0_of = [&](int j) { return head_lo + j * kKeys; };
+  const auto score = [&](int tile) {
+    bf16x8 k0[kSubs];
+#pragma unroll
+    for (int sub = 0; sub < kSubs; ++sub) k0[sub] = at.key(tile, 0, sub);
+    score_tile(tile, qf, at, s, k0);
+  };
+  // The reference of the rows that need it goes up to their maximum, and o and sum with it; P anew.  A row's result is its own
+  // whatever its neighbours hold.  (A row without a reference has gathered nothing of its own: o may be NaN.)
+  const auto raise_to_max = [&](bool raise, Probs& p) {
+    const float top = half_max(raise ? 1.f : 0.f) > 0.f ? vmax(m, tile_max(s)) : m;
+    const bool fresh = m == -__builtin_inff();
+    const float alpha = fresh ? 0.f : fast_exp2((m - top) * a.c);
+    sum *= alpha;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] = fresh ? 0.f : o[db][i] * alpha;
+    m = top;
+    return form_tile(s, a.c, top == -__builtin_inff() ? 0.f : top * a.c, p);
+  };
+  K.fetch(key0_of(0), kst(0), w);
+  if (total > 1) K.fetch(key0_of(1), kst(1), w);
+  if (T == 0) {
+    V.fetch(key0_of(0), vst(0), w);
+    if (total > 1) V.fetch(key0_of(1), vst(1), w);
+  }
+  wait_dma();
+  __syncthreads();
+  score(kst(0));
   if (T > 0) {
     // Step j: K(j+1) and V(j-1) have landed; K(j+2) and V(j) go into the stages that step j-1 has done with.  P(j) is formed from
     // the scores in registers, against the standing reference, beside V(j-1) P(j-1); then the scores of j+1.
@@ -323,8 +375,8 @@ __global__ __launch_bounds__(kThreads, 2) void packed_attn(PackedArgs a) {
       constexpr int P = decltype(parity)::value;
       wait_dma();
       __syncthreads();
-      if (j + 2 < T) K.fetch(head_lo + (j + 2) * kKeys, kst(P), w);
-      V.fetch(head_lo + j * kKeys, vst(P), w);
+      if (j + 2 < total) K.fetch(key0_of(j + 2), kst(P), w);
+      V.fetch(key0_of(j), vst(P), w);
       bf16x8 k0[kSubs];
 #pragma unroll
       for (int sub = 0; sub < kSubs; ++sub) k0[sub] = at.key(kst(1 - P), 0, sub);
@@ -337,36 +389,16 @@ __global__ __launch_bounds__(kThreads, 2) void packed_attn(PackedArgs a) {
       for (int sub = 0; sub < kSubs; ++sub) asm volatile("" ::"v"(pn[sub][0]), "v"(pn[sub][1]));
       asm volatile("" ::"v"(ts));
       const bool raise = !(ts <= kSumLimit) || m == -__builtin_inff();
-      if (__ballot(raise)) {  // of the rows that need it, so that a row's result is its own whatever its neighbours hold
-        const float top = half_max(raise ? 1.f : 0.f) > 0.f ? vmax(m, tile_max(s)) : m;
-        const float alpha = m == -__builtin_inff() ? 0.f : fast_exp2((m - top) * a.c);
-        sum *= alpha;
-#pragma unroll
-        for (int db = 0; db < 4; ++db)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
-        m = top;
-        ts = form_tile(s, a.c, top == -__builtin_inff() ? 0.f : top * a.c, pn);
-      }
+      if (__ballot(raise)) ts = raise_to_max(raise, pn);
       sum += ts;
       __builtin_amdgcn_s_setprio(0);
 #pragma unroll
       for (int sub = 0; sub < kSubs; ++sub) asm volatile("" ::"v"(k0[sub]));
       __builtin_amdgcn_iglp_opt(0);
-      score_tile(kst(1 - P), qf, at, s, k0);  // of the last step: a stage that no load goes to, and never used
+      score_tile(kst(1 - P), qf, at, s, k0);
     };
     using Even = std::integral_constant<int, 0>;
     using Odd = std::integral_constant<int, 1>;
-    K.fetch(head_lo, kst(0), w);
-    if (T > 1) K.fetch(head_lo + kKeys, kst(1), w);
-    wait_dma();
-    __syncthreads();
-    {
-      bf16x8 k0[kSubs];
-#pragma unroll
-      for (int sub = 0; sub < kSubs; ++sub) k0[sub] = at.key(kst(0), 0, sub);
-      score_tile(kst(0), qf, at, s, k0);
-    }
     Probs pa, pz;
     step(0, Even{}, std::true_type{}, pz, pa);
     int j = 1;
@@ -374,63 +406,56 @@ __global__ __launch_bounds__(kThreads, 2) void packed_attn(PackedArgs a) {
       step(j, Odd{}, std::false_type{}, pa, pz);
       step(j + 1, Even{}, std::false_type{}, pz, pa);
     }
+    // the last whole tile's V meets its P while the first edge tile's is under way (its K has been scored)
     if (j < T) {
       step(j, Odd{}, std::false_type{}, pa, pz);
       wait_dma();
       __syncthreads();
+      V.fetch(key0_of(T), vst(0), w);
       add_values(vst(1), at, pz, o);
+      __syncthreads();
+      if (T + 1 < total) V.fetch(key0_of(T + 1), vst(1), w);
     } else {
       wait_dma();
       __syncthreads();
+      V.fetch(key0_of(T), vst(1), w);
       add_values(vst(0), at, pa, o);
+      __syncthreads();
+      if (T + 1 < total) V.fetch(key0_of(T + 1), vst(0), w);
     }
-    __syncthreads();  // the rings are free
     if (lo != head_lo) {  // a row of another sequence starts anew
       m = -__builtin_inff();
       sum = 0.f;
     }
   }
-
-  const int edges = (q_end - kd + kKeys - 1) / kKeys;
-  for (int t = 0; t < edges; ++t) {
-    if (t == 0 || t == 2) {  // two tiles at a time
-      if (t == 2) __syncthreads();
-      for (int x = t; x < t + 2 && x < edges; ++x) {
-        K.fetch(kd + x * kKeys, kst(x & 1), w);
-        V.fetch(kd + x * kKeys, vst(x & 1), w);
-      }
-      wait_dma();
-      const bool odd = odd_values(vst(0), w, l) || (t + 1 < edges && odd_values(vst(1), w, l));
-      if (l == 0) odd_wave[w] = odd;
-      __syncthreads();
-    }
-    const int key0 = kd + t * kKeys;
-    if (__ballot(covered && lo < key0 + kKeys && row >= key0) == 0) continue;  // no row of this wave sees the tile
-    {
-      bf16x8 k0[kSubs];
-#pragma unroll
-      for (int sub = 0; sub < kSubs; ++sub) k0[sub] = at.key(kst(t & 1), 0, sub);
-      score_tile(kst(t & 1), qf, at, s, k0);
-    }
-#pragma unroll
-    for (int sub = 0; sub < kSubs; ++sub)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = key_of(key0, sub, i, l);
-        if (key < lo || key > row) s[sub][i] = -__builtin_inff();
-      }
-    const float top = vmax(m, tile_max(s));
-    const bool fresh = m == -__builtin_inff();
-    const float alpha = fresh ? 0.f : fast_exp2((m - top) * a.c);
-    m = top;
-#pragma unroll
-    for (int db = 0; db < 4; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[db][i] = fresh ? 0.f : o[db][i] * alpha;  // (fresh: of rows not its own, perhaps NaN)
+  int odd = 0;  // an edge tile of V was not all finite
+  // Edge tile j: its scores are in registers and V(j) and K(j+1) under way (of the first one V(j+1), too).
+  for (int j = T; j < total; ++j) {
+    const int key0 = key0_of(j), P = j & 1;
+    const bool seen = __ballot(covered && lo < key0 + kKeys && row >= key0) != 0;  // by a row of this wave
     Probs p;
-    sum = sum * alpha + form_tile(s, a.c, top == -__builtin_inff() ? 0.f : top * a.c, p);
-    if (uniform(odd_wave[0] | odd_wave[1] | odd_wave[2] | odd_wave[3]) == 0) add_values(vst(t & 1), at, p, o);
-    else add_mixed_values(vst(t & 1), at, p, key0, lo, row, l, o);
+    if (seen) {
+#pragma unroll
+      for (int sub = 0; sub < kSubs; ++sub)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = key_of(key0, sub, i, l);
+          if (key < lo || key > row) s[sub][i] = -__builtin_inff();
+        }
+      float ts = form_tile(s, a.c, m == -__builtin_inff() ? 0.f : m * a.c, p);
+      const bool raise = !(ts <= kSumLimit) || m == -__builtin_inff();
+      if (__ballot(raise)) ts = raise_to_max(raise, p);
+      sum += ts;
+    }
+    if (j == T && j + 1 < total) wait_dma_but4();
+    else wait_dma();
+    if (!only_finite(vst(P), w, l)) odd = 1;
+    if (l == 0) odd_wave[w] = odd;
+    __syncthreads();  // V(j) and K(j+1) are there, the stages of K(j) and V(j-1) free
+    if (j + 2 < total) K.fetch(key0_of(j + 2), kst(P), w);
+    if (j > T && j + 1 < total) V.fetch(key0_of(j + 1), vst(1 - P), w);
+    if (seen) add_values(vst(P), at, p, o);
+    if (j + 1 < total && __ballot(covered && lo < key0 + 2 * kKeys && row >= key0 + kKeys) != 0) score(kst(1 - P));
   }
 
   // A row sees itself, so its sum is 0 only where all its scores are -infinity: then 0 / 0 is NaN, as the softmax is.
@@ -446,6 +471,8 @@ __global__ __launch_bounds__(kThreads, 2) void packed_attn(PackedArgs a) {
         *reinterpret_cast<bf16x4*>(dst + 32 * db + 8 * i) = bf16x4{x[0], x[1], y[0], y[1]};
       }
   }
+  if (uniform(odd_wave[0] | odd_wave[1] | odd_wave[2] | odd_wave[3]) != 0)  // written before the last tile's barrier
+    add_infinities(a, head, key0_of(T), q0 + 32 * w, lo, covered, l);
 #endif  // __HIP_DEVICE_COMPILE__
 }
 
