@@ -273,6 +273,13 @@ __device__ __forceinline__ void add_infinities(const PackedArgs& a, int head, in
   }
 }
 
+// Waits until at most N loads of this wave are under way; kLoads make a tile.
+template <int N>
+__device__ __forceinline__ void wait_but() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 7 << 4 | 15 << 8);
+}
+constexpr int kLoads = kKeys / 16;
+
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 #endif  // __HIP_DEVICE_COMPILE__
@@ -365,7 +372,10 @@ __global__ __launch_bounds__(kThreads, 2) void packed_attn(PackedArgs a) {
     V.fetch(key0_of(0), vst(0), w);
     if (total > 1) V.fetch(key0_of(1), vst(1), w);
   }
-  wait_dma();
+  // (only the first tile's keys are needed yet)
+  if (T > 0) wait_but<kLoads>();
+  else if (total > 1) wait_but<3 * kLoads>();
+  else wait_but<kLoads>();
   __syncthreads();
   score(kst(0));
   if (T > 0) {
@@ -383,13 +393,16 @@ __global__ __launch_bounds__(kThreads, 2) void packed_attn(PackedArgs a) {
       __builtin_amdgcn_s_setprio(1);
       const float mc = m == -__builtin_inff() ? 0.f : m * a.c;
       float ts;
-      if constexpr (decltype(first)::value) ts = form_tile(s, a.c, mc, pn);
-      else ts = form_beside_values(s, a.c, mc, pn, vst(1 - P), at, pp, o);
+      if constexpr (decltype(first)::value) {
+        ts = raise_to_max(true, pn);
+      } else {
+        ts = form_beside_values(s, a.c, mc, pn, vst(1 - P), at, pp, o);
 #pragma unroll
-      for (int sub = 0; sub < kSubs; ++sub) asm volatile("" ::"v"(pn[sub][0]), "v"(pn[sub][1]));
-      asm volatile("" ::"v"(ts));
-      const bool raise = !(ts <= kSumLimit) || m == -__builtin_inff();
-      if (__ballot(raise)) ts = raise_to_max(raise, pn);
+        for (int sub = 0; sub < kSubs; ++sub) asm volatile("" ::"v"(pn[sub][0]), "v"(pn[sub][1]));
+        asm volatile("" ::"v"(ts));
+        const bool raise = !(ts <= kSumLimit) || m == -__builtin_inff();
+        if (__ballot(raise)) ts = raise_to_max(raise, pn);
+      }
       sum += ts;
       __builtin_amdgcn_s_setprio(0);
 #pragma unroll
@@ -442,12 +455,17 @@ __global__ __launch_bounds__(kThreads, 2) void packed_attn(PackedArgs a) {
           const int key = key_of(key0, sub, i, l);
           if (key < lo || key > row) s[sub][i] = -__builtin_inff();
         }
-      float ts = form_tile(s, a.c, m == -__builtin_inff() ? 0.f : m * a.c, p);
-      const bool raise = !(ts <= kSumLimit) || m == -__builtin_inff();
-      if (__ballot(raise)) ts = raise_to_max(raise, p);
+      float ts;
+      if (j == 0) {
+        ts = raise_to_max(true, p);
+      } else {
+        ts = form_tile(s, a.c, m == -__builtin_inff() ? 0.f : m * a.c, p);
+        const bool raise = !(ts <= kSumLimit) || m == -__builtin_inff();
+        if (__ballot(raise)) ts = raise_to_max(raise, p);
+      }
       sum += ts;
     }
-    if (j == T && j + 1 < total) wait_dma_but4();
+    if (j == T && j + 1 < total) wait_but<kLoads>();
     else wait_dma();
     if (!only_finite(vst(P), w, l)) odd = 1;
     if (l == 0) odd_wave[w] = odd;
