@@ -500,15 +500,21 @@ crisp_status crisp_cache_weights(const crisp_cache_shape* cache, const crisp_cac
                                  int32_t width, const int32_t* held, void* workspace, size_t workspace_bytes,
                                  crisp_stream stream);
 
+/* Host only.  Bytes of workspace (256-byte aligned, any contents) of crisp_cache_keep, 0 up to width 16384; in_place: new_weights is
+ * weights. */
+crisp_status crisp_cache_keep_workspace_size(int32_t n_seqs, int32_t n_kv_heads, int32_t width, int32_t in_place,
+                                             size_t* bytes);
+
 /* For each sequence of n = seq_len[s] <= width tokens with 0 < keep[s] < n and keep[s] <= cap, and each KV head, the m = keep[s]
  * positions that stay: the last min(recent, m), the first min(sink, what is left of m), and of those between the ones with the
  * largest weights (ties: the lowest position; NaN below all).  kept int32[n_seqs][H_kv][cap] receives them in ascending order, -1 behind them;
  * count[s] = m.  Other sequences stay as they are: count 0, kept -1.  new_weights_or_null float[n_seqs][H_kv][width] receives the
  * weights of the positions that stay in places 0 .. m - 1, the rest of it stays as it was; it may be weights, or does not overlap
- * it.  width and cap in [1, 2^30]; n_kv_heads <= 65535, sink and recent >= 0. */
+ * it.  width and cap in [1, 2^28], n_seqs H_kv <= 2^20, n_seqs H_kv width <= 2^34; sink and recent >= 0. */
 crisp_status crisp_cache_keep(int32_t n_seqs, int32_t n_kv_heads, int32_t width, const float* weights, const int32_t* held,
                               const int32_t* seq_len, const int32_t* keep, int32_t sink, int32_t recent, int32_t cap,
-                              int32_t* kept, int32_t* count, float* new_weights_or_null, crisp_stream stream);
+                              int32_t* kept, int32_t* count, float* new_weights_or_null, void* workspace,
+                              size_t workspace_bytes, crisp_stream stream);
 
 /* The kept tokens of each sequence, KV head by KV head, to pages of their own: position i < min(count[s], cap) of the row of new_table
  * (int32[n_seqs][new_pages]) becomes what position kept[s][g][i] of the row of table holds, as if its cached K and V were

@@ -105,7 +105,8 @@ def _load(path: str = _LIB_PATH):
         "crisp_packed_attn": (ctypes.c_int, [ps, F, P, P, I64, I64, P, I64, I64, P, I64, I64, P, I64, I64, P]),
         "crisp_cache_weights_workspace_size": (ctypes.c_int, [cs, cb, I32, ctypes.POINTER(SZ)]),
         "crisp_cache_weights": (ctypes.c_int, [cs, cb, I32, F, P, P, P, P, P, P, I64, I64, P, P, I32, P, P, SZ, P]),
-        "crisp_cache_keep": (ctypes.c_int, [I32, I32, I32, P, P, P, P, I32, I32, I32, P, P, P, P]),
+        "crisp_cache_keep_workspace_size": (ctypes.c_int, [I32, I32, I32, I32, ctypes.POINTER(SZ)]),
+        "crisp_cache_keep": (ctypes.c_int, [I32, I32, I32, P, P, P, P, I32, I32, I32, P, P, P, P, SZ, P]),
         "crisp_cache_gather": (ctypes.c_int, [cs, cb, P, P, P, P, I32, P, P, I32, P]),
         "crisp_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "crisp_last_error": (ctypes.c_char_p, []),
@@ -124,7 +125,8 @@ EXPORTED = ("crisp_params_default", "crisp_col_capacity", "crisp_workspace_size"
             "crisp_cache_bytes", "crisp_cache_append", "crisp_cache_attn_workspace_size", "crisp_cache_attn",
             "crisp_cache_copy", "crisp_pool_words", "crisp_pool_init", "crisp_pool_reserve", "crisp_pool_fork",
             "crisp_pool_free", "crisp_pool_compact", "crisp_rope_init", "crisp_rope", "crisp_packed_attn",
-            "crisp_cache_weights_workspace_size", "crisp_cache_weights", "crisp_cache_keep", "crisp_cache_gather")
+            "crisp_cache_weights_workspace_size", "crisp_cache_weights", "crisp_cache_keep_workspace_size", "crisp_cache_keep",
+            "crisp_cache_gather")
 
 # route_mode / vs_mode values (include/crisp.h)
 ROUTE_BY_CSTRUCT, ROUTE_BY_JSD = 0, 1
@@ -602,8 +604,16 @@ def crisp_cache_weights(cache: Cache, table: torch.Tensor, seq_len: torch.Tensor
     return out
 
 
+def cache_keep_workspace(weights: torch.Tensor, in_place: bool = False) -> Optional[torch.Tensor]:
+    """A workspace for crisp_cache_keep on such weights (in_place: new_weights is weights too); None where it needs none."""
+    n = ctypes.c_size_t()
+    _check(lib.crisp_cache_keep_workspace_size(*weights.shape, in_place, ctypes.byref(n)), "crisp_cache_keep_workspace_size")
+    return torch.empty(int(n.value), dtype=torch.uint8, device=weights.device) if n.value else None
+
+
 def crisp_cache_keep(weights: torch.Tensor, held: torch.Tensor, seq_len: torch.Tensor, keep: torch.Tensor, cap: int,
-                     sink: int = 4, recent: int = 64, new_weights: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+                     sink: int = 4, recent: int = 64, new_weights: Optional[torch.Tensor] = None,
+                     ws: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The keep[s] < seq_len[s] positions of each sequence and KV head that stay: the last `recent`, the first `sink`, and those with
     the largest weights -> (kept int32 [n_seqs, H_kv, cap], ascending, -1 behind them; count int32 [n_seqs], 0 for a sequence that
     stays as it is).  new_weights (weights itself, or another) receives their weights."""
@@ -616,11 +626,15 @@ def crisp_cache_keep(weights: torch.Tensor, held: torch.Tensor, seq_len: torch.T
         _i32_of(t, name, (n_seqs,), gpu)
     if new_weights is not None:
         _f32(new_weights, "new_weights", weights.shape, gpu)
+    if ws is None:
+        ws = cache_keep_workspace(weights, new_weights is not None and new_weights.data_ptr() == weights.data_ptr()) if n_seqs else None
+    elif ws.dtype is not torch.uint8 or ws.get_device() != gpu or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous uint8 tensor on cuda:{gpu}, got {ws.dtype} on {ws.device}")
     kept = torch.empty((n_seqs, heads, max(cap, 0)), dtype=torch.int32, device=weights.device)
     count = torch.empty(n_seqs, dtype=torch.int32, device=weights.device)
     _call(gpu, "crisp_cache_keep", lib.crisp_cache_keep, n_seqs, heads, wide, weights.data_ptr(), held.data_ptr(),
           seq_len.data_ptr(), keep.data_ptr(), sink, recent, cap, kept.data_ptr(), count.data_ptr(),
-          None if new_weights is None else new_weights.data_ptr())
+          None if new_weights is None else new_weights.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel())
     return kept, count
 
 

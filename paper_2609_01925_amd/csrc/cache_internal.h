@@ -69,7 +69,9 @@ struct KeepArgs {
   int32_t* kept;         // [n_seqs][hkv][cap]
   int32_t* count;
   float* new_weights;    // as weights, which it may be; or null
+  char* ws;              // cache_keep_bytes
 };
+size_t cache_keep_bytes(int64_t heads, int width, bool in_place);
 hipError_t launch_cache_keep(const KeepArgs& a, hipStream_t stream);
 
 struct GatherArgs {

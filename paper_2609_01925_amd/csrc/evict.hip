@@ -6,9 +6,10 @@ namespace crisp {
 namespace {
 
 constexpr int kKeepThreads = 1024, kKeepWaves = kKeepThreads / kWave;
-constexpr int kBins = 2048, kCopies = 8;               // of a digit of 11 bits (the last has 10)
-constexpr int kEach = 16, kSpan = kEach * kKeepThreads;  // tokens of a thread and of the workgroup at a time
-__device__ __forceinline__ int padded(int i) { return i + i / kEach; }  // neighbours of threads that have some each fall on different banks
+constexpr int kBins = 2048, kCopies = 8;              // of a digit of 11 bits (the last has 10)
+constexpr int kMost = 16;                             // tokens of a thread where one workgroup chooses
+constexpr int kPart = 8, kChunk1 = kPart * kKeepThreads;  // tokens of a thread and a workgroup where several do
+constexpr int kList = 16384;                          // weights that share the first digit of the limit, if no more do
 
 // An unsigned order of floats: NaN lowest, -0 equal to 0.
 __device__ __forceinline__ uint32_t order_of(float x) {
@@ -16,174 +17,338 @@ __device__ __forceinline__ uint32_t order_of(float x) {
   return x != x ? 0u : (b >> 31) ? ~b : b | 0x80000000u;
 }
 
-// One workgroup a sequence and KV head.  The k-th largest weight is found by three digits of its bits, from the top, a histogram in LDS
-// for each; what is above it stays, and of its equals the first.  Up to kSpan tokens are read once and stay in LDS; of more, the
-// weights that share the digits so far are listed there as soon as they fit.  Then the tokens go by in order, each wave counting its own
-// by ballots, so that what stays is written in ascending order and, since a span is in LDS before any of it is written,
-// also over the weights that it was read from.  Weights share few exponents, so lanes add to eight copies of the bins.
-__global__ __launch_bounds__(kKeepThreads) void cache_keep(KeepArgs a) {
-  __shared__ __attribute__((aligned(16))) int hist[kBins][kCopies];
-  __shared__ uint32_t raw[kSpan + kSpan / kEach];
-  __shared__ int sums[kKeepWaves], found[3], n_few;
-  __shared__ int sums2[2][kKeepWaves];
-  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int s = blockIdx.x / a.hkv, h = blockIdx.x % a.hkv;
-  const int n = a.seq_len[s], m = a.keep[s], held = a.held[s];
-  int32_t* kept = a.kept + (int64_t)blockIdx.x * a.cap;
-  const bool chosen = n <= a.width && m > 0 && m < n && m <= a.cap;
-  if (h == 0 && tid == 0) a.count[s] = chosen ? m : 0;
-  for (int i = (chosen ? m : 0) + tid; i < a.cap; i += kKeepThreads) kept[i] = -1;
-  if (!chosen) return;
+// What a sequence and KV head is to keep: the positions below lo and from hi on, and `wanted` of those between.
+struct Choice {
+  int n, m, held, lo, hi, wanted;
+  bool any;
+  __device__ __forceinline__ Choice(const KeepArgs& a, int s) : n(a.seq_len[s]), m(a.keep[s]), held(a.held[s]) {
+    any = n <= a.width && m > 0 && m < n && m <= a.cap;
+    const int recent = min(a.recent, m), sink = min(a.sink, m - recent);
+    lo = sink;
+    hi = n - recent;
+    wanted = m - recent - sink;
+  }
+  __device__ __forceinline__ bool between(int j) const { return j >= lo && j < hi; }
+};
+
+// The limit: all weights above it stay, and `ties` of its equals.  It is found digit by digit, from the top: `prefix` holds the digits
+// so far, and `ties` of the weights that share them are still wanted.
+struct Limit {
+  uint32_t prefix, value;
+  int ties, among;  // how many share the digits so far
+  static __device__ __forceinline__ int shift(int digit) { return digit == 0 ? 21 : digit == 1 ? 10 : 0; }
+  static __device__ __forceinline__ int bits(int digit) { return digit < 2 ? 11 : 10; }
+  // Whether they all stay: then all above value - 1 do, and no further digit is needed.
+  __device__ __forceinline__ bool all_stay() const { return ties == among && value > 0; }
+  __device__ __forceinline__ void close() {
+    if (all_stay()) {
+      --value;
+      ties = 0;
+    }
+  }
+};
+
+// Weights share few exponents, so lanes add to eight copies of the bins.
+struct KeepLds {
+  __attribute__((aligned(16))) int hist[kBins][kCopies];
+  int sums[kKeepWaves], found[3];
+};
+
+__device__ __forceinline__ void clear(KeepLds& l) {  // ends with a barrier
+  for (int i = threadIdx.x; i < kBins * kCopies / 4; i += kKeepThreads) reinterpret_cast<int4*>(l.hist)[i] = make_int4(0, 0, 0, 0);
+  __syncthreads();
+}
+__device__ __forceinline__ void add(KeepLds& l, int digit, uint32_t prefix, uint32_t o) {
+  if ((uint64_t)o >> (Limit::shift(digit) + Limit::bits(digit)) == prefix)
+    atomicAdd(&l.hist[o >> Limit::shift(digit) & ((1u << Limit::bits(digit)) - 1)][threadIdx.x & (kCopies - 1)], 1);
+}
+__device__ __forceinline__ int bin(const KeepLds& l, int d) {
+  const int4* h = reinterpret_cast<const int4*>(l.hist[d]);
+  const int4 x = h[0], y = h[1];
+  return ((x.x + x.y) + (x.z + x.w)) + ((y.x + y.y) + (y.z + y.w));
+}
+// From the highest digit down, the one in which the count passes the ties that are still wanted; a0 and a1 are the counts of this thread's
+// digits 2047 - 2 tid and 2046 - 2 tid.  Barriers before and after what is shared.
+__device__ __forceinline__ void next_digit(KeepLds& l, int digit, int a0, int a1, Limit& x) {
+  const int d = kBins - 1 - 2 * (int)threadIdx.x;
+  int total;
+  const int end = block_scan<int, kKeepWaves>(a0 + a1, l.sums, &total), begin = end - a0 - a1;
+  if (begin < x.ties && end >= x.ties) {
+    const bool first = begin + a0 >= x.ties;
+    l.found[0] = first ? d : d - 1;
+    l.found[1] = x.ties - (first ? begin : begin + a0);
+    l.found[2] = first ? a0 : a1;
+  }
+  __syncthreads();
+  x.prefix = x.prefix << Limit::bits(digit) | (uint32_t)l.found[0];
+  x.ties = l.found[1];
+  x.among = l.found[2];
+  x.value = x.prefix << Limit::shift(digit);
+}
+
+// This thread's `mine` <= N neighbouring tokens from `first` on, of weights x: those that stay are written behind `above` and, of the limit's
+// equals, min(equal, ties) that stay before them.  All of x is in registers, so the weights may go over those that they
+// were read from.
+template <int N>
+__device__ __forceinline__ void write_kept(const Choice& c, const Limit& limit, const float (&x)[N], int first, int mine, int above, int equal,
+                                           int* lds, int32_t* kept, float* moved) {
+  uint32_t up = 0, same = 0;  // bits of the tokens that stay whatever the equals do, and of those
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (i < mine) {
+      const int j = first + i;
+      const uint32_t o = order_of(x[i]);
+      const bool sure = !c.between(j) || o > limit.value;
+      up |= (j < c.n && sure ? 1u : 0u) << i;
+      same |= (j < c.n && !sure && o == limit.value ? 1u : 0u) << i;
+    }
+  const int own = __popc(up) | __popc(same) << 16;  // of 16384 tokens: the sums stay apart
+  int total;
+  const int before = block_scan<int, kKeepWaves>(own, lds, &total) - own;
+  int e = equal + (before >> 16), to = above + (before & 0xffff) + min(e, limit.ties);
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (i < mine && ((up | same) >> i & 1) && ((up >> i & 1) || e++ < limit.ties)) {
+      kept[to] = first + i;
+      if (moved) moved[to] = x[i];
+      ++to;
+    }
+}
+
+// One workgroup a sequence and KV head of up to 16384 tokens, whose weights stay in registers: 32 sequences of 700 to 4100 tokens, 8 heads.
+__device__ __forceinline__ void keep_alone(const KeepArgs& a, const Choice& c, KeepLds& l) {
+  const int tid = threadIdx.x, mine = (c.n + kKeepThreads - 1) / kKeepThreads, first = tid * mine;
   const float* weights = a.weights + (int64_t)blockIdx.x * a.width;
-  float* moved = a.new_weights ? a.new_weights + (int64_t)blockIdx.x * a.width : nullptr;
-  const int recent = min(a.recent, m), sink = min(a.sink, m - recent), lo = sink, hi = n - recent;
-  const bool whole = n <= kSpan;
-
-  // f(j0, x): this thread's weights of each span, positions j0 + 1024 i + tid, read while the span before is worked on.
-  const auto read = [&](int j0, float (&x)[kEach]) {
+  float x[kMost];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) x[i] = weights[min(j0 + i * kKeepThreads + tid, n - 1)];
-  };
-  const auto spans = [&](auto f) {
-    float x[kEach], next[kEach];
-    read(0, next);
-    for (int j0 = 0; j0 < n; j0 += kSpan) {
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int j = j0 + i * kKeepThreads + tid;
-        x[i] = j < held ? next[i] : 0.f;
-      }
-      if (j0 + kSpan < n) read(j0 + kSpan, next);
-      f(j0, x);
-    }
-  };
-  const auto each = [&](auto f) {  // f(weight) for the ones to choose from
-    spans([&](int j0, const float (&x)[kEach]) {
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        const int j = j0 + i * kKeepThreads + tid;
-        if (j >= lo && j < hi) f(order_of(x[i]));
-      }
-    });
-  };
-  const auto store = [&](const float (&x)[kEach]) {
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) raw[padded(i * kKeepThreads + tid)] = __float_as_uint(x[i]);
-  };
-  if (whole) spans([&](int, const float (&x)[kEach]) { store(x); });  // a thread's own places, until the next barrier
-
-  uint32_t limit = 0xffffffffu;  // the weight that the k-th largest has: all above it stay, and `ties` of its equals
-  int ties = m - recent - sink;
-  if (ties > 0) {
-    uint32_t prefix = 0;
-    int listed = -1;  // weights in the list, once there is one
+  for (int i = 0; i < kMost; ++i) {
+    x[i] = 0.f;
+    if (i < mine && first + i < min(c.n, c.held)) x[i] = weights[first + i];
+  }
+  Limit limit{0, 0xffffffffu, c.wanted, -1};
+  if (c.wanted > 0) {
 #pragma unroll 1
-    for (int digit = 0; digit < 3; ++digit) {
-      const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, bits = digit < 2 ? 11 : 10;
-      const uint64_t mask = (1u << bits) - 1;
-      const auto add = [&](uint32_t o) {
-        if ((uint64_t)o >> (shift + bits) == prefix) atomicAdd(&hist[o >> shift & mask][lane & (kCopies - 1)], 1);
-      };
-      for (int i = tid; i < kBins * kCopies / 4; i += kKeepThreads) reinterpret_cast<int4*>(hist)[i] = make_int4(0, 0, 0, 0);
-      if (tid == 0) n_few = 0;
+    for (int digit = 0; digit < 3 && !limit.all_stay(); ++digit) {
+      clear(l);
+#pragma unroll
+      for (int i = 0; i < kMost; ++i)
+        if (i < mine && c.between(first + i)) add(l, digit, limit.prefix, order_of(x[i]));
       __syncthreads();
-      if (listed >= 0) {
-        for (int i = tid; i < listed; i += kKeepThreads) add(raw[i]);
-      } else if (whole) {
-#pragma unroll 4
-        for (int j = tid; j < n; j += kKeepThreads)
-          if (j >= lo && j < hi) add(order_of(__uint_as_float(raw[padded(j)])));
-      } else {
-        each(add);
-      }
-      __syncthreads();
-      // from the highest digit down: the one in which the count passes the ties that are still wanted
       const int d = kBins - 1 - 2 * tid;
-      int a0 = 0, a1 = 0, total;
-#pragma unroll
-      for (int i = 0; i < kCopies; ++i) {
-        a0 += hist[d][i];
-        a1 += hist[d - 1][i];
-      }
-      const int end = block_scan<int, kKeepWaves>(a0 + a1, sums, &total), begin = end - a0 - a1;
-      if (begin < ties && end >= ties) {
-        const bool first = begin + a0 >= ties;
-        found[0] = first ? d : d - 1;
-        found[1] = ties - (first ? begin : begin + a0);
-        found[2] = first ? a0 : a1;
-      }
-      __syncthreads();
-      prefix = prefix << bits | (uint32_t)found[0];
-      ties = found[1];
-      const int among = found[2];
-      limit = prefix << shift;
-      if (ties == among && limit > 0) {  // all that share the digits so far stay
-        --limit;
-        ties = 0;
-        break;
-      }
-      if (digit < 2 && !whole && listed < 0 && among <= kSpan) {
-        spans([&](int j0, const float (&x)[kEach]) {
-          uint32_t hit = 0;
-#pragma unroll
-          for (int i = 0; i < kEach; ++i) {
-            const int j = j0 + i * kKeepThreads + tid;
-            hit |= (j >= lo && j < hi && order_of(x[i]) >> shift == prefix ? 1u : 0u) << i;
-          }
-          const int end = wave_scan(__popc(hit));
-          int to = 0;
-          if (lane == kWave - 1) to = atomicAdd(&n_few, end);
-          to = __builtin_amdgcn_readlane(to, kWave - 1) + end - __popc(hit);
-#pragma unroll
-          for (int i = 0; i < kEach; ++i)
-            if (hit >> i & 1) raw[to++] = order_of(x[i]);
-        });
-        listed = among;
-        __syncthreads();
-      }
+      next_digit(l, digit, bin(l, d), bin(l, d - 1), limit);
     }
-  }
-  int above = 0, equal = 0, turn = 0;  // of the spans before
-  const auto write = [&](int j0) {
-    // a thread has `each` neighbouring tokens; bits of `up` stay whatever their equals do, those of `same` are equal to the limit
-    const int mine = (min(n - j0, kSpan) + kKeepThreads - 1) / kKeepThreads, first = tid * mine;
-    uint32_t up = 0, same = 0;
-#pragma unroll 4
-    for (int i = 0; i < mine; ++i) {
-      const int j = j0 + first + i;
-      const uint32_t o = order_of(__uint_as_float(raw[padded(first + i)]));
-      const bool sure = j < lo || j >= hi || o > limit;
-      up |= (j < n && sure ? 1u : 0u) << i;
-      same |= (j < n && !sure && o == limit ? 1u : 0u) << i;
-    }
-    const int own = __popc(up) | __popc(same) << 16;  // of 16384 tokens: the sums stay apart
-    int total;
-    const int before = block_scan<int, kKeepWaves>(own, sums2[turn], &total) - own;
-    int to = above + (before & 0xffff), e = equal + (before >> 16);
-    to += min(e, ties);
-    for (uint32_t todo = up | same; todo != 0; todo &= todo - 1) {
-      const int i = __ffs(todo) - 1;
-      if ((up >> i & 1) || e++ < ties) {
-        kept[to] = j0 + first + i;
-        if (moved) moved[to] = __uint_as_float(raw[padded(first + i)]);
-        ++to;
-      }
-    }
-    above += total & 0xffff;
-    equal += total >> 16;
-    turn ^= 1;
-  };
-  if (whole) {
+    limit.close();
     __syncthreads();
-    write(0);
-  } else {
-    spans([&](int j0, const float (&x)[kEach]) {
-      __syncthreads();  // the list, or the span before, is done with
-      store(x);
-      __syncthreads();
-      write(j0);
-    });
   }
+  write_kept<kMost>(c, limit, x, first, mine, 0, 0, l.sums, a.kept + (int64_t)blockIdx.x * a.cap,
+                    a.new_weights ? a.new_weights + (int64_t)blockIdx.x * a.width : nullptr);
+}
+
+// The places behind the last that stays.
+__device__ __forceinline__ void fill_rest(const KeepArgs& a, const Choice& c, int part, int parts) {
+  int32_t* kept = a.kept + (int64_t)blockIdx.x * a.cap;
+  for (int i = (c.any ? c.m : 0) + part * kKeepThreads + (int)threadIdx.x; i < a.cap; i += parts * kKeepThreads) kept[i] = -1;
+  if (part == 0 && blockIdx.x % a.hkv == 0 && threadIdx.x == 0) a.count[blockIdx.x / a.hkv] = c.any ? c.m : 0;
+}
+
+__global__ __launch_bounds__(kKeepThreads) void cache_keep(KeepArgs a) {
+  __shared__ KeepLds l;
+  const Choice c(a, blockIdx.x / a.hkv);
+  fill_rest(a, c, 0, 1);
+  if (c.any) keep_alone(a, c, l);
+}
+
+// Where the weights' rows are longer, three launches: each workgroup has kChunk1 tokens of a sequence and KV head (one of up to 16384 is
+// the first launch's alone).  1: the first digit's bins of each chunk.  2: their sums give the digit; each chunk counts its weights
+// above it and lists those that share it.  3: every workgroup finds the other digits from the list, counts what stays in the chunks
+// before its own, and writes its own.  (Where too many share the digit, the weights themselves are gone over in place of a list.)
+struct KeepSpace {
+  int chunks;
+  int* hist;      // [chunks][kBins], a head
+  int* above;     // [chunks]
+  int* info;      // weights listed, and what 2 has found: digit, ties, among
+  uint2* list;    // (weight, chunk)
+  float* copy;    // [width]: of the weights, where they are written over
+  static size_t bytes(int width, bool in_place) {
+    const size_t chunks = ((size_t)width + kChunk1 - 1) / kChunk1;
+    return (chunks * (kBins + 1) * 4 + 16 + (size_t)kList * 8 + (in_place ? (size_t)width * 4 : 0) + 255) & ~(size_t)255;
+  }
+  __device__ __forceinline__ KeepSpace(const KeepArgs& a, bool in_place) {
+    chunks = (a.width + kChunk1 - 1) / kChunk1;
+    const size_t each = ((size_t)chunks * (kBins + 1) * 4 + 16 + (size_t)kList * 8 + (in_place ? (size_t)a.width * 4 : 0) + 255) & ~(size_t)255;
+    char* p = a.ws + (size_t)blockIdx.x * each;
+    list = reinterpret_cast<uint2*>(p);
+    info = reinterpret_cast<int*>(list + kList);
+    hist = info + 4;
+    above = hist + (size_t)chunks * kBins;
+    copy = reinterpret_cast<float*>(above + chunks);
+  }
+};
+
+__device__ __forceinline__ int chunks_of(const Choice& c) { return (c.n + kChunk1 - 1) / kChunk1; }
+
+// f(position, order of the weight) for this thread's tokens of a chunk.
+template <typename F>
+__device__ __forceinline__ void each_weight(const Choice& c, const float* weights, int chunk, F f) {
+  float x[kPart];
+#pragma unroll
+  for (int i = 0; i < kPart; ++i) {
+    const int j = chunk * kChunk1 + i * kKeepThreads + (int)threadIdx.x;
+    x[i] = j < min(c.n, c.held) ? weights[j] : 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < kPart; ++i) {
+    const int j = chunk * kChunk1 + i * kKeepThreads + (int)threadIdx.x;
+    if (j < c.n) f(j, x[i]);
+  }
+}
+
+// The workgroup's sum, on every thread; ends with lds in use.
+__device__ __forceinline__ int block_sum(int x, int* lds) {
+  int total;
+  block_scan<int, kKeepWaves>(x, lds, &total);
+  return total;
+}
+
+__global__ __launch_bounds__(kKeepThreads) void keep_count(KeepArgs a) {
+  __shared__ KeepLds l;
+  const Choice c(a, blockIdx.x / a.hkv);
+  const int chunk = blockIdx.y, tid = threadIdx.x;
+  const bool alone = !c.any || c.n <= kMost * kKeepThreads;
+  const int parts = alone ? 1 : chunks_of(c);
+  if (chunk >= parts) return;
+  fill_rest(a, c, chunk, parts);
+  if (!c.any) return;
+  if (alone) return keep_alone(a, c, l);
+  const bool in_place = a.new_weights == a.weights;
+  const KeepSpace w(a, in_place);
+  if (chunk == 0 && tid == 0) w.info[0] = 0;
+  clear(l);
+  each_weight(c, a.weights + (int64_t)blockIdx.x * a.width, chunk, [&](int j, float x) {
+    if (in_place) w.copy[j] = x;
+    if (c.between(j)) add(l, 0, 0, order_of(x));
+  });
+  __syncthreads();
+  reinterpret_cast<int2*>(w.hist + (size_t)chunk * kBins)[tid] = make_int2(bin(l, 2 * tid), bin(l, 2 * tid + 1));
+}
+
+__global__ __launch_bounds__(kKeepThreads) void keep_list(KeepArgs a) {
+  __shared__ KeepLds l;
+  const Choice c(a, blockIdx.x / a.hkv);
+  const int chunk = blockIdx.y, tid = threadIdx.x, lane = tid & 63;
+  if (!c.any || c.n <= kMost * kKeepThreads || chunk >= chunks_of(c)) return;
+  const KeepSpace w(a, a.new_weights == a.weights);
+  Limit limit{0, 0xffffffffu, c.wanted, -1};
+  if (c.wanted > 0) {
+    int2 sum = {0, 0};  // of digits 2046 - 2 tid and 2047 - 2 tid
+    const int n = chunks_of(c);
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const int2 x = reinterpret_cast<const int2*>(w.hist + (size_t)i * kBins)[kKeepThreads - 1 - tid];
+      sum.x += x.x;
+      sum.y += x.y;
+    }
+    next_digit(l, 0, sum.y, sum.x, limit);
+    if (chunk == 0 && tid == 0) {
+      w.info[1] = (int)limit.prefix;
+      w.info[2] = limit.ties;
+      w.info[3] = limit.among;
+    }
+  }
+  const bool open = c.wanted > 0 && !limit.all_stay();  // some of those that share the digit stay, some do not
+  limit.close();
+  int more = 0, hits = 0;
+  uint32_t o[kPart];
+  each_weight(c, a.weights + (int64_t)blockIdx.x * a.width, chunk, [&](int j, float x) {
+    const uint32_t y = order_of(x);
+    const bool shares = open && c.between(j) && y >> Limit::shift(0) == limit.prefix;
+    if (shares) {
+#pragma unroll
+      for (int i = 0; i < kPart; ++i)
+        if (i == hits) o[i] = y;
+      ++hits;
+    } else {
+      more += !c.between(j) || y > limit.value;
+    }
+  });
+  if (open && limit.among <= kList) {
+    const int end = wave_scan(hits);
+    int to = 0;
+    if (lane == kWave - 1 && end > 0) to = atomicAdd(&w.info[0], end);
+    to = __builtin_amdgcn_readlane(to, kWave - 1) + end - hits;
+#pragma unroll
+    for (int i = 0; i < kPart; ++i)
+      if (i < hits) w.list[to + i] = make_uint2(o[i], chunk);
+  }
+  __syncthreads();
+  more = block_sum(more, l.sums);
+  if (tid == 0) w.above[chunk] = more;
+}
+
+__global__ __launch_bounds__(kKeepThreads) void keep_write(KeepArgs a) {
+  __shared__ KeepLds l;
+  const Choice c(a, blockIdx.x / a.hkv);
+  const int chunk = blockIdx.y, tid = threadIdx.x;
+  if (!c.any || c.n <= kMost * kKeepThreads || chunk >= chunks_of(c)) return;
+  const bool in_place = a.new_weights == a.weights;
+  const KeepSpace w(a, in_place);
+  const float* weights = in_place ? w.copy : a.weights + (int64_t)blockIdx.x * a.width;
+  Limit limit{0, 0xffffffffu, c.wanted, -1};
+  int above = 0, equal = 0;
+  for (int i = tid; i < chunk; i += kKeepThreads) above += w.above[i];
+  if (c.wanted > 0) {
+    limit.prefix = (uint32_t)w.info[1];
+    limit.value = limit.prefix << Limit::shift(0);
+    limit.ties = w.info[2];
+    limit.among = w.info[3];
+    if (!limit.all_stay()) {
+      const bool listed = limit.among <= kList;
+      const int entries = listed ? limit.among : 0;
+      uint2 x[kList / kKeepThreads];
+#pragma unroll
+      for (int i = 0; i < kList / kKeepThreads; ++i)
+        if (i * kKeepThreads + tid < entries) x[i] = w.list[i * kKeepThreads + tid];
+      const auto each = [&](int end, auto f) {  // f(order, chunk) for those that share the first digit, of chunks below end
+        if (listed) {
+#pragma unroll
+          for (int i = 0; i < kList / kKeepThreads; ++i)
+            if (i * kKeepThreads + tid < entries) f(x[i].x, (int)x[i].y);
+        } else {
+          for (int i = 0; i < end; ++i)
+            each_weight(c, weights, i, [&](int j, float y) {
+              const uint32_t o = order_of(y);
+              if (c.between(j) && o >> Limit::shift(0) == (uint32_t)w.info[1]) f(o, i);
+            });
+        }
+      };
+#pragma unroll 1
+      for (int digit = 1; digit < 3 && !limit.all_stay(); ++digit) {
+        clear(l);
+        each(chunks_of(c), [&](uint32_t o, int) { add(l, digit, limit.prefix, o); });
+        __syncthreads();
+        const int d = kBins - 1 - 2 * tid;
+        next_digit(l, digit, bin(l, d), bin(l, d - 1), limit);
+      }
+      limit.close();
+      each(chunk, [&](uint32_t o, int of) {
+        above += of < chunk && o > limit.value;
+        equal += of < chunk && o == limit.value;
+      });
+    } else {
+      limit.close();
+    }
+  }
+  __syncthreads();
+  above = block_sum(above, l.sums);
+  __syncthreads();
+  equal = block_sum(equal, l.sums);
+  __syncthreads();
+  float x[kPart];
+  const int first = chunk * kChunk1 + tid * kPart;
+#pragma unroll
+  for (int i = 0; i < kPart; ++i) x[i] = first + i < min(c.n, c.held) ? weights[first + i] : 0.f;
+  write_kept<kPart>(c, limit, x, first, kPart, above, equal, l.sums, a.kept + (int64_t)blockIdx.x * a.cap,
+                    a.new_weights ? a.new_weights + (int64_t)blockIdx.x * a.width : nullptr);
 }
 
 // The smallest e >= kScaleExpMin with x 2^8 <= MAX 2^e, from a value of at most eight significant bits.
@@ -373,8 +538,20 @@ __global__ __launch_bounds__(256 * TILES) void cache_gather(GatherArgs a) {
 
 }  // namespace
 
+size_t cache_keep_bytes(int64_t heads, int width, bool in_place) {
+  return width <= kMost * kKeepThreads ? 0 : (size_t)heads * KeepSpace::bytes(width, in_place);
+}
+
 hipError_t launch_cache_keep(const KeepArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL(cache_keep, dim3((unsigned)(a.n_seqs * a.hkv)), dim3(kKeepThreads), 0, stream, a);
+  const unsigned heads = (unsigned)(a.n_seqs * a.hkv);
+  if (a.width <= kMost * kKeepThreads) {
+    hipLaunchKernelGGL(cache_keep, dim3(heads), dim3(kKeepThreads), 0, stream, a);
+  } else {
+    const dim3 grid(heads, (unsigned)((a.width + kChunk1 - 1) / kChunk1));
+    hipLaunchKernelGGL(keep_count, grid, dim3(kKeepThreads), 0, stream, a);
+    hipLaunchKernelGGL(keep_list, grid, dim3(kKeepThreads), 0, stream, a);
+    hipLaunchKernelGGL(keep_write, grid, dim3(kKeepThreads), 0, stream, a);
+  }
   return hipGetLastError();
 }
 

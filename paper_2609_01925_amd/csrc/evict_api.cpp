@@ -7,7 +7,8 @@ namespace crisp {
 namespace {
 
 constexpr int64_t kMaxHeads = (int64_t)1 << 20;  // sequences x KV heads, some workgroups each
-constexpr int kMaxWidth = 1 << 30;
+constexpr int kMaxWidth = 1 << 28;               // of the weights and lists: their chunks are a launch's second dimension
+constexpr int64_t kMaxWeights = (int64_t)1 << 34;  // all heads' widths: workgroups of 1024 threads and 8192 tokens, fewer than 2^32 threads
 
 crisp_status check_seq_heads(int64_t n_seqs, int64_t heads) {
   if (n_seqs * heads > kMaxHeads)
@@ -17,7 +18,17 @@ crisp_status check_seq_heads(int64_t n_seqs, int64_t heads) {
 
 crisp_status check_width(int width, const char* name) {
   if (width < 1) return fail(CRISP_EINVAL, "%s must be >= 1", name);
-  if (width > kMaxWidth) return fail(CRISP_EUNSUPPORTED, "%s %d above the supported 2^30", name, width);
+  if (width > kMaxWidth) return fail(CRISP_EUNSUPPORTED, "%s %d above the supported 2^28", name, width);
+  return CRISP_OK;
+}
+
+crisp_status check_keep(int n_seqs, int heads, int width) {
+  if (n_seqs < 0 || heads < 1) return fail(CRISP_EINVAL, "bad sizes: n_seqs=%d n_kv_heads=%d", n_seqs, heads);
+  if (heads > 65535) return fail(CRISP_EUNSUPPORTED, "n_kv_heads %d above the supported 65535", heads);
+  CHECK(check_seq_heads(n_seqs, heads));
+  CHECK(check_width(width, "width"));
+  if ((int64_t)n_seqs * heads * width > kMaxWeights)
+    return fail(CRISP_EUNSUPPORTED, "%d sequences of %d KV heads and width %d are above the supported 2^34 weights", n_seqs, heads, width);
   return CRISP_OK;
 }
 
@@ -75,13 +86,19 @@ crisp_status crisp_cache_weights(const crisp_cache_shape* cache, const crisp_cac
                     "crisp_cache_weights launch");
 }
 
+crisp_status crisp_cache_keep_workspace_size(int32_t n_seqs, int32_t n_kv_heads, int32_t width, int32_t in_place,
+                                             size_t* bytes) {
+  CHECK(check_keep(n_seqs, n_kv_heads, width));
+  if (!bytes) return fail(CRISP_EINVAL, "bytes is null");
+  *bytes = cache_keep_bytes((int64_t)n_seqs * n_kv_heads, width, in_place != 0);
+  return CRISP_OK;
+}
+
 crisp_status crisp_cache_keep(int32_t n_seqs, int32_t n_kv_heads, int32_t width, const float* weights, const int32_t* held,
                               const int32_t* seq_len, const int32_t* keep, int32_t sink, int32_t recent, int32_t cap,
-                              int32_t* kept, int32_t* count, float* new_weights_or_null, crisp_stream stream) {
-  if (n_seqs < 0 || n_kv_heads < 1) return fail(CRISP_EINVAL, "bad sizes: n_seqs=%d n_kv_heads=%d", n_seqs, n_kv_heads);
-  if (n_kv_heads > 65535) return fail(CRISP_EUNSUPPORTED, "n_kv_heads %d above the supported 65535", n_kv_heads);
-  CHECK(check_seq_heads(n_seqs, n_kv_heads));
-  CHECK(check_width(width, "width"));
+                              int32_t* kept, int32_t* count, float* new_weights_or_null, void* workspace,
+                              size_t workspace_bytes, crisp_stream stream) {
+  CHECK(check_keep(n_seqs, n_kv_heads, width));
   CHECK(check_width(cap, "cap"));
   if (sink < 0 || recent < 0) return fail(CRISP_EINVAL, "sink %d and recent %d must be >= 0", sink, recent);
   if (n_seqs == 0) return CRISP_OK;
@@ -92,8 +109,11 @@ crisp_status crisp_cache_keep(int32_t n_seqs, int32_t n_kv_heads, int32_t width,
   CHECK(check_ptr(kept, 4, "kept"));
   CHECK(check_ptr(count, 4, "count"));
   if (new_weights_or_null) CHECK(check_ptr(new_weights_or_null, 4, "new_weights"));
+  const size_t need = cache_keep_bytes((int64_t)n_seqs * n_kv_heads, width, new_weights_or_null == weights);
+  if (need > 0) CHECK(check_ptr(workspace, 256, "workspace"));
+  if (workspace_bytes < need) return fail(CRISP_EINVAL, "workspace too small: %zu < %zu", workspace_bytes, need);
   return hip_status(launch_cache_keep(KeepArgs{n_seqs, n_kv_heads, width, sink, recent, cap, weights, held, seq_len, keep, kept,
-                                               count, new_weights_or_null},
+                                               count, new_weights_or_null, (char*)workspace},
                                       (hipStream_t)stream),
                     "crisp_cache_keep launch");
 }

@@ -57,7 +57,7 @@ int main(void) {
   EXPECT(crisp_cache_weights_workspace_size(&cache, &batch, 4, &bytes) == CRISP_OK && bytes > 0);
   EXPECT(weights(&cache, &batch, 4, 384, 128, 256, bytes) == CRISP_EHIP);
   EXPECT(weights(&cache, &batch, 4, 384, 128, 256, bytes - 1) == CRISP_EINVAL);
-  EXPECT(crisp_cache_keep(2, 2, 256, P, P, P, P, 4, 8, 64, P, P, NULL, NULL) == CRISP_EHIP);
+  EXPECT(crisp_cache_keep(2, 2, 256, P, P, P, P, 4, 8, 64, P, P, NULL, NULL, 0, NULL) == CRISP_EHIP);
   EXPECT(crisp_cache_gather(&cache, &batch, P, P, P, P, 64, P, P, 1, NULL) == CRISP_EHIP);
 
   /* every field over the ends of its type */
@@ -94,8 +94,10 @@ int main(void) {
       EXPECT(known(weights(&cache, &b, ints[j], 384, 128, 256, SIZE_MAX)) && known(weights(&cache, &batch, 4, 384, 128, ints[i], SIZE_MAX)));
       EXPECT(known(crisp_cache_gather(&cache, &b, P, P, P, P, 64, P, P, ints[j], NULL)));
       EXPECT(known(crisp_cache_gather(&cache, &batch, P, P, P, P, ints[i], P, P, ints[j], NULL)));
-      EXPECT(known(crisp_cache_keep(ints[i], ints[j], 256, P, P, P, P, 4, 8, 64, P, P, P, NULL)));
-      EXPECT(known(crisp_cache_keep(2, 2, ints[i], P, P, P, P, ints[j], ints[i], ints[j], P, P, P, NULL)));
+      EXPECT(known(crisp_cache_keep(ints[i], ints[j], 256, P, P, P, P, 4, 8, 64, P, P, P, P, SIZE_MAX, NULL)));
+      EXPECT(known(crisp_cache_keep(2, 2, ints[i], P, P, P, P, ints[j], ints[i], ints[j], P, P, P, P, SIZE_MAX, NULL)));
+      s = crisp_cache_keep_workspace_size(ints[i], 2, ints[j], i & 1, &bytes);
+      EXPECT(known(s) && s != CRISP_EHIP);
     }
   }
   for (i = 0; i < N(reals); ++i)

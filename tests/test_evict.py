@@ -286,14 +286,43 @@ def test_keep_batch_of_all_kinds():
     _check_keep(C, rng.random((11, 2, 300)).astype(np.float32), [1000] * 11, lens, keep, 150, 4, 32)
 
 
-@pytest.mark.parametrize("n,m", [(16384, 5000), (16385, 16384), (40000, 1), (70001, 30000)])
+@pytest.mark.parametrize("n,m", [(16384, 5000), (16385, 16384), (40000, 1), (70001, 30000), (24576, 24575), (33000, 60)])
 def test_keep_long_sequences(n, m):
-    """More tokens than the workgroup holds at a time, also in place."""
+    """About as many tokens as one workgroup takes, and more; also in place."""
     C = _crisp()
     _say(f"keep n={n} m={m}")
     rng = np.random.default_rng(n)
     w = np.exp(3 * rng.standard_normal((1, 2, n))).astype(np.float32)
     _check_keep(C, w, [n], [n], [m], m, 4, 100)
+    _check_keep(C, w, [n - 9000], [n], [m], m, 0, 0)
+
+
+def test_keep_long_sequences_that_share_digits():
+    """So many weights alike that the list of those that share the limit's first digit does not hold them: all equal, few values, the last
+    bits apart, special values."""
+    C = _crisp()
+    _say("keep long sequences that share digits")
+    rng = np.random.default_rng(11)
+    n = 40000
+    for w in (np.full((1, 1, n), 0.25), rng.integers(0, 3, (1, 1, n)), (np.int32(0x3f000000) + rng.integers(0, 1 << 20, (1, 1, n)).astype(np.int32)).view(np.float32),
+              rng.choice(np.array([0.0, -0.0, 1.0, -1.0, np.inf, -np.inf, np.nan], dtype=np.float32), (1, 1, n))):
+        for m in (1, 9000, 39999):
+            _check_keep(C, w.astype(np.float32), [n], [n], [m], m, 2, 5)
+
+
+def test_keep_short_and_long_sequences_in_a_wide_buffer():
+    C = _crisp()
+    _say("keep short and long in a wide buffer")
+    rng = np.random.default_rng(12)
+    lens = [30000, 5, 16384, 16385, 0, 1, 700, 25000, 30001]
+    keep = [10000, 2, 100, 16000, 3, 1, 699, 25000, 5]
+    w = np.exp(2 * rng.standard_normal((9, 2, 30000))).astype(np.float32)
+    _check_keep(C, w, [1 << 20] * 9, lens, keep, 16000, 4, 64)
+    ws = C.cache_keep_workspace(_floats(w), in_place=True)
+    ws.fill_(0xff)
+    a = C.crisp_cache_keep(_floats(w), _ints(lens), _ints(lens), _ints(keep), 16000, 4, 64, ws=ws)
+    b = C.crisp_cache_keep(_floats(w), _ints(lens), _ints(lens), _ints(keep), 16000, 4, 64)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
 # ------------------------------------------------------------------ the move

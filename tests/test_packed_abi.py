@@ -38,8 +38,8 @@ def _weights(sh=None, b=(2, 4, 3), hq=4, scale=0.0, p=P, s=P, t=P, n=P, r=P, q=P
                                      ws, wsb, None)
 
 
-def _keep(seqs=2, heads=2, width=256, w=P, h=P, n=P, m=P, sink=4, recent=8, cap=64, k=P, c=P, o=P):
-    return C.lib.crisp_cache_keep(seqs, heads, width, w, h, n, m, sink, recent, cap, k, c, o, None)
+def _keep(seqs=2, heads=2, width=256, w=P, h=P, n=P, m=P, sink=4, recent=8, cap=64, k=P, c=P, o=P, ws=None, wsb=0):
+    return C.lib.crisp_cache_keep(seqs, heads, width, w, h, n, m, sink, recent, cap, k, c, o, ws, wsb, None)
 
 
 def _gather(sh=None, b=(2, 4, 0), p=P, s=P, t=P, k=P, cap=64, c=P, n=P, wide=1):
@@ -152,7 +152,7 @@ def test_weights_refusals():
     assert _weights(ws=None) == C.CRISP_EINVAL and _weights(ws=ctypes.c_void_p(0x100010)) == C.CRISP_EINVAL
     assert _weights(wsb=16) == C.CRISP_EINVAL and b"too small" in C.lib.crisp_last_error()
     assert _weights(hq=3) == C.CRISP_EINVAL and _weights(width=0) == C.CRISP_EINVAL
-    assert _weights(width=(1 << 30) + 1) == C.CRISP_EUNSUPPORTED
+    assert _weights(width=(1 << 28) + 1) == C.CRISP_EUNSUPPORTED
     for bad in (-1.0, math.nan, math.inf):
         assert _weights(scale=bad) == C.CRISP_EINVAL
     for bad in (-8, 4, 129):
@@ -176,8 +176,22 @@ def test_keep_refusals():
     assert _keep(o=ODD) == C.CRISP_EINVAL
     for change in (dict(seqs=-1), dict(heads=0), dict(width=0), dict(cap=0), dict(cap=-1), dict(sink=-1), dict(recent=-1)):
         assert _keep(**change) == C.CRISP_EINVAL, change
-    for change in (dict(width=(1 << 30) + 1), dict(cap=(1 << 30) + 1), dict(heads=65536), dict(seqs=(1 << 19) + 1)):
+    for change in (dict(width=(1 << 28) + 1), dict(cap=(1 << 28) + 1), dict(heads=65536), dict(seqs=(1 << 19) + 1),
+                   dict(width=1 << 28, seqs=33)):
         assert _keep(**change) == C.CRISP_EUNSUPPORTED, change
+    n = ctypes.c_size_t()
+    size = lambda *args: C.lib.crisp_cache_keep_workspace_size(*args, REF(n))  # noqa: E731
+    assert size(2, 2, 16384, 1) == C.CRISP_OK and n.value == 0
+    assert size(2, 2, 16385, 0) == C.CRISP_OK and n.value > 0
+    apart = n.value
+    assert size(2, 2, 16385, 1) == C.CRISP_OK and n.value >= apart + 4 * (4 * 16385 - 255)
+    assert size(-1, 2, 64, 0) == C.CRISP_EINVAL and size(2, 2, 0, 0) == C.CRISP_EINVAL
+    assert C.lib.crisp_cache_keep_workspace_size(2, 2, 64, 0, None) == C.CRISP_EINVAL
+    other = ctypes.c_void_p(0x900000)
+    for bad in (None, ctypes.c_void_p(0x100010)):
+        assert _keep(width=16385, ws=bad, wsb=1 << 40) == C.CRISP_EINVAL
+    assert _keep(width=16385, ws=other, wsb=apart - 1, o=other) == C.CRISP_EINVAL and b"too small" in C.lib.crisp_last_error()
+    assert _keep(width=16385, ws=other, wsb=apart) == C.CRISP_EINVAL  # in place it needs more
 
 
 def test_gather_refusals():
