@@ -384,6 +384,16 @@ def make_rope(rotary_dim: int = 128, layout: int = ROPE_HALF, base: float = 1000
     return table
 
 
+def _rows_out(out: Optional[torch.Tensor], name: str, heads: int, n: int, like: torch.Tensor):
+    """A packed output of that size, new and contiguous unless given, and its head and row stride."""
+    if out is None:
+        return torch.empty((heads, n, 128), dtype=torch.bfloat16, device=like.device), max(n, 1) * 128, 128
+    _, m, head, row = _rows(out, name, heads, like.get_device())
+    if m != n:
+        raise ValueError(f"{name} {tuple(out.shape)} must have {n} rows")
+    return out, head, row
+
+
 def crisp_rope(rope: CrispRopeTable, start: torch.Tensor, row_ptr: torch.Tensor, q: torch.Tensor,
                k: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
                k_out: Optional[torch.Tensor] = None):
@@ -394,15 +404,14 @@ def crisp_rope(rope: CrispRopeTable, start: torch.Tensor, row_ptr: torch.Tensor,
     if gpu < 0:
         raise ValueError(f"q must be a CUDA tensor, got one on {q.device}")
     heads, n, qh, qr = _rows(q, "q", None, gpu)
-    o = torch.empty((heads, n, 128), dtype=torch.bfloat16, device=q.device) if q_out is None else q_out
-    _, m, oh, orow = _rows(o, "q_out", heads, gpu)
-    kv, kh, kr, p, ph, pr = 0, 0, 0, None, 0, 0
+    o, oh, orow = _rows_out(q_out, "q_out", heads, n, q)
+    kv = kh = kr = ph = pr = 0
+    p = None
     if k is not None:
-        kv, mk, kh, kr = _rows(k, "k", None, gpu)
-        p = torch.empty((kv, n, 128), dtype=torch.bfloat16, device=q.device) if k_out is None else k_out
-        _, mp, ph, pr = _rows(p, "k_out", kv, gpu)
-    if m != n or (k is not None and (mk != n or mp != n)):
-        raise ValueError(f"q {tuple(q.shape)}, k and their outputs must have the same number of rows")
+        kv, m, kh, kr = _rows(k, "k", None, gpu)
+        if m != n:
+            raise ValueError(f"k {tuple(k.shape)} must have q's number of rows {n}")
+        p, ph, pr = _rows_out(k_out, "k_out", kv, n, q)
     n_seqs, = _i32(start, "start", 1, gpu)
     _i32_of(row_ptr, "row_ptr", (n_seqs + 1,), gpu)
     _call(gpu, "crisp_rope", lib.crisp_rope, CrispPackedShape(n_seqs, n, heads, kv, 128), rope, start.data_ptr(),
@@ -422,11 +431,9 @@ def crisp_packed_attn(row_ptr: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v
     heads, n, qh, qr = _rows(q, "q", None, gpu)
     kv, m, kh, kr = _rows(k, "k", None, gpu)
     _, m2, vh, vr = _rows(v, "v", kv, gpu)
-    o = torch.empty((heads, n, 128), dtype=torch.bfloat16, device=q.device) if out is None else out
-    _, m3, oh, orow = _rows(o, "out", heads, gpu)
-    if not n == m == m2 == m3:
-        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)} and out {tuple(o.shape)} must have the same "
-                         "number of rows")
+    if not n == m == m2:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} must have the same number of rows")
+    o, oh, orow = _rows_out(out, "out", heads, n, q)
     ends, = _i32(row_ptr, "row_ptr", 1, gpu)
     if ends < 1:
         raise ValueError("row_ptr must hold the sequences' n_seqs + 1 offsets")

@@ -306,19 +306,17 @@ __global__ __launch_bounds__(kThreads, 2) void packed_attn(PackedArgs a) {
     for (int kk = 0; kk < 8; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(src + 16 * kk);
   }
 
-  // The begin of the first row's sequence, then of this lane's: the last begin at or before its row.  Up to 63 sequences all
-  // of it comes from one load, a begin a lane.
-  const int n_seqs = a.d.n_seqs;
-  const bool few = n_seqs < kWave;
-  const int mine = few ? a.row_ptr[min(l, n_seqs)] : 0;
-  int s0, end, head_lo;
+  // The begin of the first row's sequence, then of this lane's: the last begin at or before its row.  Up to 64 sequences all
+  // of it comes from one round of loads, a begin a lane.
+  const int n_seqs = a.d.n_seqs, end = uniform(a.row_ptr[n_seqs]);
+  const bool few = n_seqs <= kWave;
+  const int mine = few ? a.row_ptr[min(l, n_seqs - 1)] : 0;
+  int s0, head_lo;
   if (few) {
-    s0 = __popcll(__ballot(l <= n_seqs && mine <= q0)) - 1;
-    end = __builtin_amdgcn_readlane(mine, n_seqs);
+    s0 = __popcll(__ballot(l < n_seqs && mine <= q0)) - 1;
     head_lo = __builtin_amdgcn_readlane(mine, max(s0, 0));
   } else {
     s0 = uniform(seq_of_row(a.row_ptr, n_seqs, q0));
-    end = uniform(a.row_ptr[n_seqs]);
     head_lo = uniform(a.row_ptr[max(s0, 0)]);
   }
   const int q_end = min(q0 + kRows, min(end, a.d.n_rows));

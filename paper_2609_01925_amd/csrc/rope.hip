@@ -37,22 +37,40 @@ __global__ __launch_bounds__(kThreads) void rope(RopeArgs a) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int row0 = (int)blockIdx.x * kRowsPerWg + w * kRowsPerWave, row = row0 + (lane >> 3), c = lane & 7;
   if (row0 >= a.d.n_rows) return;
-  // the row's sequence: the last that begins at or before the wave's first row, then those that begin among its eight
-  int s0 = seq_of_row(a.row_ptr, a.d.n_seqs, row0);
-  int seq = s0;
-  for (int from = s0 + 1; from <= a.d.n_seqs; from += kWave) {
-    const int i = from + lane;
-    const int begin = i <= a.d.n_seqs ? a.row_ptr[i] : 0x7fffffff;
-    unsigned long long last = 0;
+  // The row's sequence, the last that begins at or before it.  Up to 64 sequences their begins and positions come from one round of
+  // loads, a sequence a lane; of more, the wave's first row's is looked for, then those that begin among its eight.
+  const int end = a.row_ptr[a.d.n_seqs];
+  int seq, begin, start;
+  if (a.d.n_seqs <= kWave) {
+    const int last = a.d.n_seqs - 1, mine = a.row_ptr[min(lane, last)], first = a.start[min(lane, last)];
+    seq = -1;
 #pragma unroll
-    for (int r = 0; r < kRowsPerWave; ++r) {
-      last = __ballot(begin <= row0 + r);
-      if (r == (lane >> 3)) seq += __popcll(last);
+    for (int i = 0; i < kRowsPerWave; ++i) {
+      const int n = __popcll(__ballot(lane <= last && mine <= row0 + i));
+      if (i == (lane >> 3)) seq += n;
     }
-    if (~last != 0) break;
+    begin = __shfl(mine, max(seq, 0));
+    start = __shfl(first, max(seq, 0));
+  } else {
+    const int s0 = seq_of_row(a.row_ptr, a.d.n_seqs, row0);
+    seq = s0;
+    for (int from = s0 + 1; from <= a.d.n_seqs; from += kWave) {
+      const int i = from + lane;
+      const int b = i <= a.d.n_seqs ? a.row_ptr[i] : 0x7fffffff;
+      unsigned long long last = 0;
+#pragma unroll
+      for (int x = 0; x < kRowsPerWave; ++x) {
+        last = __ballot(b <= row0 + x);
+        if (x == (lane >> 3)) seq += __popcll(last);
+      }
+      if (~last != 0) break;
+    }
+    const int s = min(max(seq, 0), a.d.n_seqs - 1);
+    begin = a.row_ptr[s];
+    start = a.start[s];
   }
-  if (row >= a.d.n_rows || seq < 0 || seq >= a.d.n_seqs) return;
-  const double p = (double)((int64_t)a.start[seq] + row - a.row_ptr[seq]);
+  if (row >= min(end, a.d.n_rows) || seq < 0 || seq >= a.d.n_seqs) return;
+  const double p = (double)((int64_t)start + row - begin);
   const bool turned = c < a.t.dim / 16;
   float co[8], si[8];
 #pragma unroll

@@ -122,6 +122,7 @@ def test_packed_prompts(fused):
     # a second prompt for sequences that hold tokens: nothing changes and the result says so
     more = [50, 60, 0, 0, 0]
     kv.reserve(_ints(more))
+    kv.layers[0].pages[kv.table[1, 0].item()] = 0x55  # (new memory may hold what an earlier test stored)
     before = [(c.pages.clone(), c.scales.clone()) for c in kv.layers]
     q, k, v = _qkv(110, 9)
     o = kv.prefill_packed(0, _ptr(more), q, k, v)
