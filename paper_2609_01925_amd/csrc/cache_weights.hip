@@ -151,13 +151,23 @@ __device__ __forceinline__ void column(float& m, float& l) {
   for (int o = 16; o < kWave; o <<= 1) merge(m, l, __shfl_xor(m, o), __shfl_xor(l, o));
 }
 
-// Scores of a tile that the pairs from p0 on do not see become -infinity.
-__device__ __forceinline__ void mask_tile(const WeightArgs& a, const SeqRows& r, int t, int p0, int lane, acc4 (&s)[4]) {
-  if (t * kTile + kTile - 1 <= r.len + p0 / a.G) return;
-  const int see = r.len + (p0 + (lane & 15)) / a.G, first = t * kTile + 16 * (lane >> 4);
+// The last positions that 16 pairs from p0 on see: the first pair's, and this lane's.  (Divided once, not once a tile.)
+struct Sight {
+  int all, own;
+  __device__ __forceinline__ Sight() {}
+  __device__ __forceinline__ Sight(const WeightArgs& a, const SeqRows& r, int p0, int pairs)
+      : all(r.len + min(p0, pairs - 1) / a.G), own(r.len + min(p0 + (lane_id() & 15), pairs - 1) / a.G) {}
+  __device__ __forceinline__ bool whole(int t) const { return t * kTile + kTile - 1 <= all; }
+  // Whether this lane's pair does not see its e-th token of tile t.
+  __device__ __forceinline__ bool hides(int t, int e) const { return t * kTile + 16 * (lane_id() >> 4) + e > own; }
+};
+
+// Scores of a tile that the pairs do not see become -infinity.
+__device__ __forceinline__ void mask_tile(const Sight& see, int t, acc4 (&s)[4]) {
+  if (see.whole(t)) return;
 #pragma unroll
   for (int e = 0; e < 16; ++e)
-    if (first + e > see) s[e >> 2][e & 3] = -__builtin_inff();
+    if (see.hides(t, e)) s[e >> 2][e & 3] = -__builtin_inff();
 }
 
 struct Item {
@@ -168,28 +178,39 @@ __device__ __forceinline__ Item item_of(const WeightArgs& a, int each) {
   return Item{sh / a.c.hkv, sh % a.c.hkv, (int)blockIdx.x - sh * each};
 }
 
-// A column's reference m and sum l of exp2(x - m) with a tile's 16 of this lane's, x = s kc, -infinity where masked.  The sums are
-// 32-bit floats, so the reference need not be the maximum: it is raised to it where a sum passes 2^60 (or is not a number) and
-// where there is none yet, and no maximum is looked for otherwise.
-__device__ __forceinline__ void add_tile(const acc4 (&s)[4], float kc, float& m, float& l) {
-  const auto sum = [&](float ref) {
+// For each group, a column's reference m and sum l of exp2(x - m) with a tile's 16 of this lane's, x = s kc, -infinity where masked.  The
+// sums are 32-bit floats, so the reference need not be the maximum: it is raised to it where a sum passes 2^60 (or is not a
+// number) and where there is none yet, and no maximum is looked for otherwise.
+template <int NI>
+__device__ __forceinline__ void add_tiles(const acc4 (&s)[NI][4], float kc, float (&m)[NI], float (&l)[NI]) {
+  const auto sum = [&](int i, float ref) {
     float y[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 16; ++e) y[e & 3] += fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], kc, -ref));
+    for (int e = 0; e < 16; ++e) y[e & 3] += fast_exp2(__builtin_fmaf(s[i][e >> 2][e & 3], kc, -ref));
     return (y[0] + y[1]) + (y[2] + y[3]);
   };
-  float more = sum(m == -__builtin_inff() ? 0.f : m);
-  if (__ballot(!(more <= 0x1p60f) || m == -__builtin_inff())) {
-    float top = s[0][0];
+  float more[NI];
+  bool raise = false;
 #pragma unroll
-    for (int e = 1; e < 16; ++e) top = vmax(top, s[e >> 2][e & 3]);
-    top = vmax(m, top * kc);
-    const float ref = top == -__builtin_inff() ? 0.f : top;
-    l *= fast_exp2(m - ref);
-    m = top;
-    more = sum(ref);
+  for (int i = 0; i < NI; ++i) {
+    more[i] = sum(i, m[i] == -__builtin_inff() ? 0.f : m[i]);
+    raise = raise || !(more[i] <= 0x1p60f) || m[i] == -__builtin_inff();
   }
-  l += more;
+  if (__ballot(raise)) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      float top = s[i][0][0];
+#pragma unroll
+      for (int e = 1; e < 16; ++e) top = vmax(top, s[i][e >> 2][e & 3]);
+      top = vmax(m[i], top * kc);
+      const float ref = top == -__builtin_inff() ? 0.f : top;
+      l[i] *= fast_exp2(m[i] - ref);
+      m[i] = top;
+      more[i] = sum(i, ref);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NI; ++i) l[i] += more[i];
 }
 
 // Calls of few pairs a sequence, 16 at a time: a wave takes every fourth tile of the chunk, with q in registers.
@@ -212,12 +233,14 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_rows_few(WeightArgs a) {
     bf16x8 q[4];
     load_pair(a, r, it.head, p0 + (lane & 15), pairs, q);
     if (p0 == 0) slot = first_slot(a, it.seq, T, pairs);
-    float m = -__builtin_inff(), l = 0.f;
+    const Sight see(a, r, p0, pairs);
+    float m[1] = {-__builtin_inff()}, l[1] = {0.f};
     for (int t = t0 + w; t < t1; t += kWaves) {
       if (t + kWaves < t1) ok_next = tiles.load(a, it.head, t + kWaves, next, kc_next);
       keep_whole(raw);
       if (ok) {
-        acc4 s[4];
+        acc4 s1[1][4];
+        acc4(&s)[4] = s1[0];
         products<FMT>(raw, q, s);
         if (slot >= 0 && (lane & 15) < pairs) {
           f32x4* dst = reinterpret_cast<f32x4*>(
@@ -225,16 +248,16 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_rows_few(WeightArgs a) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) dst[e] = s[e] * kc;
         }
-        mask_tile(a, r, t, p0, lane, s);
-        add_tile(s, kc, m, l);
+        mask_tile(see, t, s);
+        add_tiles<1>(s1, kc, m, l);
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) raw[i] = next[i];
       kc = kc_next;
       ok = ok_next;
     }
-    column(m, l);
-    if (lane < kGroup) part[w][lane] = make_float2(m, l);
+    column(m[0], l[0]);
+    if (lane < kGroup) part[w][lane] = make_float2(m[0], l[0]);
     __syncthreads();
     if (tid < kGroup && p0 + tid < pairs) {
       float2 x = part[0][tid];
@@ -311,21 +334,23 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_rows(WeightArgs a) {
     by_groups((min(pairs - p0, kPairs) + kGroup - 1) / kGroup, [&](auto groups) {
       constexpr int NI = decltype(groups)::value;
       float m[NI], l[NI];
+      Sight see[NI];
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         m[i] = -__builtin_inff();
         l[i] = 0.f;
+        see[i] = Sight(a, r, p0 + (w + kWaves * i) * kGroup, pairs);
       }
       over_tiles<FMT, NI>(a, r, it, p0, pairs, t0, t1, kst, [&](int t, bool ok, float kc, const bf16x8 (&q)[NI][4], const bf16x8 (&k)[16][kWave]) {
         if (!ok) return;
         acc4 s[NI][4];
 #pragma unroll
         for (int i = 0; i < NI; ++i) products(k, q[i], lane, s[i]);
+        if (!see[0].whole(t)) {
 #pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          mask_tile(a, r, t, p0 + (w + kWaves * i) * kGroup, lane, s[i]);
-          add_tile(s[i], kc, m[i], l[i]);
+          for (int i = 0; i < NI; ++i) mask_tile(see[i], t, s[i]);
         }
+        add_tiles<NI>(s, kc, m, l);
       });
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
@@ -382,16 +407,14 @@ __device__ __forceinline__ float row_sums(const float (&acc)[16], int lane) {
   return sum;
 }
 
-// acc += the weights of a group of 16 pairs from pg on: products s, taken to the exponent by kc, each column's logarithm sub.
-__device__ __forceinline__ void add_weights(const WeightArgs& a, const SeqRows& r, const acc4 (&s)[4], float kc, float sub, int t, int pg,
-                                            int pairs, int lane, float (&acc)[16]) {
-  if (t * kTile + kTile - 1 > r.len + pg / a.G) {
-    const int first = t * kTile + 16 * (lane >> 4), see = r.len + min(pg + (lane & 15), pairs - 1) / a.G;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) acc[e] += first + e > see ? 0.f : fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], kc, -sub));
-  } else {
+// acc += the weights of a group of 16 pairs: products s, taken to the exponent by kc, each column's logarithm sub.
+__device__ __forceinline__ void add_weights(const Sight& see, const acc4 (&s)[4], float kc, float sub, int t, float (&acc)[16]) {
+  if (see.whole(t)) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) acc[e] += fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], kc, -sub));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[e] += see.hides(t, e) ? 0.f : fast_exp2(__builtin_fmaf(s[e >> 2][e & 3], kc, -sub));
   }
 }
 
@@ -419,8 +442,10 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_tokens(WeightArgs a) {
     by_groups((min(pairs - p0, kPairs) + kGroup - 1) / kGroup, [&](auto groups) {
       constexpr int NI = decltype(groups)::value;
       float sub[NI];
+      Sight see[NI];
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
+        see[i] = Sight(a, r, p0 + (w + kWaves * i) * kGroup, pairs);
         const int p = p0 + (w + kWaves * i) * kGroup + (lane & 15);
         sub[i] = p < pairs ? a.lse[pair_of(a, r, it.head, p)] : __builtin_inff();
       }
@@ -444,14 +469,14 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_tokens(WeightArgs a) {
           acc4 s[NI][4];
 #pragma unroll
           for (int i = 0; i < NI; ++i) products(k, q[i], lane, s[i]);
-          if (t * kTile + kTile - 1 <= r.len + p0 / a.G) {
+          if (see[0].whole(t)) {  // by the wave's first pairs, so by all: no branch between the groups
 #pragma unroll
             for (int i = 0; i < NI; ++i)
 #pragma unroll
               for (int e = 0; e < 16; ++e) acc[e] += fast_exp2(__builtin_fmaf(s[i][e >> 2][e & 3], kc, -sub[i]));
           } else {
 #pragma unroll
-            for (int i = 0; i < NI; ++i) add_weights(a, r, s[i], kc, sub[i], t, p0 + (w + kWaves * i) * kGroup, pairs, lane, acc);
+            for (int i = 0; i < NI; ++i) add_weights(see[i], s[i], kc, sub[i], t, acc);
           }
         }
         parts[(t - t0) & 1][w][lane] = row_sums(acc, lane);
@@ -539,7 +564,7 @@ __global__ __launch_bounds__(kThreads, SCORES ? 8 : 4) void weigh_tokens_few(Wei
       acc4 s[4];
       keep_whole(raw);
       products<FMT>(raw, q, s);
-      add_weights(a, r, s, kc, lse[lane & 15], t, p0, pairs, lane, acc);
+      add_weights(Sight(a, r, p0, pairs), s, kc, lse[lane & 15], t, acc);
     }
     const float sum = row_sums(acc, lane);
     if (at < end) a.out[row + at] = old + sum;
