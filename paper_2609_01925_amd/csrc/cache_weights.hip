@@ -52,9 +52,9 @@ __device__ __forceinline__ int tiles_of(const WeightArgs& a, const SeqRows& r) {
 }
 __device__ __forceinline__ int chunks_of(const WeightArgs& a, int tiles) { return min(a.chunks, (tiles + kWaves - 1) / kWaves); }
 
-// The first slot of a sequence's scores, -1 if they do not wait: the tiles of the sequences before it come first.
+// The first slot of a sequence's scores, -1 if they do not wait (or there are none): the tiles of the sequences before it come first.
 __device__ __forceinline__ int64_t first_slot(const WeightArgs& a, int seq, int tiles, int pairs) {
-  if (pairs > a.waiting) return -1;
+  if (pairs > a.waiting || tiles == 0) return -1;
   int64_t sum = 0;
   for (int i = lane_id(); i < seq; i += kWave) sum += tiles_of(a, seq_rows(a.s, a.b, a.c.B, i));
   sum = wave_scan(sum);

@@ -162,6 +162,25 @@ def test_weights_holes_and_bad_pages():
     _check_weights(C, c, oracle, table, [398, 129], [2, 1], 4, held=[300, 129], seed=4)
 
 
+def test_weights_and_moves_without_a_table():
+    """A table of no pages: nothing is seen, what is held stays, kept positions are zeros."""
+    C = _crisp()
+    _say("weights and gather, table without pages")
+    c, _ = _new(C, 3, 2, 64, O.E4M3)
+    empty = torch.empty(2, 0, dtype=torch.int32, device=DEV)
+    for rows in (1, 9):
+        w = torch.rand(2, 2, 100, device=DEV)
+        got = C.crisp_cache_weights(c, empty, _ints([70, 3]), _ints([0, rows, 2 * rows]), _rand(4, 2 * rows, 1).to(DEV), w, _ints([60, 100]),
+                                    out=torch.full_like(w, 7.0))
+        # no position is in the table's range: lengths are brought into it, only the rows' own positions are left
+        want = torch.full_like(w, 7.0)
+        want[0, :, :rows], want[1, :, :rows] = w[0, :, :rows], w[1, :, :rows]
+        assert torch.equal(got, want)
+    kept = torch.zeros(2, 2, 5, dtype=torch.int32, device=DEV)
+    C.crisp_cache_gather(c, empty, kept, _ints([5, 0]), _ints([[1], [2]]))
+    assert (c.pages[1] == 0).all() and (c.pages[2] == 0x7f).all() and (c.scales[1] == 2.0 ** -64).all()
+
+
 @pytest.mark.parametrize("gain,scale", [(30.0, 0.0), (1e-3, 0.0), (1.0, 3.0), (1.0, 1e-30)])
 def test_weights_sharp_and_flat_scores(gain, scale):
     C = _crisp()
