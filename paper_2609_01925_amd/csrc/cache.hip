@@ -341,7 +341,7 @@ __global__ __launch_bounds__(256 * TILES) void cache_append_few(AppendArgs a) {
     for (int n = a.b.n_seqs; n > 1;) {
       const int step = (n + kWave - 1) / kWave, probe = lane * step;
       const unsigned long long ok = __ballot(probe < n && a.s.row_ptr[seq + min(probe, n - 1)] <= row);
-      const int k = max(__popcll(ok) - 1, 0);
+      const int k = max((int)__popcll(ok) - 1, 0);  // (its type is unsigned)
       seq += k * step;
       n = min(step, n - k * step);
     }

@@ -190,6 +190,25 @@ def test_append_extreme_values(fmt, rows_a_call):
     _check_written(c, oracle)
 
 
+@pytest.mark.parametrize("n_seqs", [65, 130, 5000])
+def test_append_with_rows_before_the_first_sequence(n_seqs):
+    """More sequences than one look holds, and rows that lie before all of them: those are stored nowhere."""
+    C = _crisp()
+    _say(f"append n_seqs={n_seqs}, rows before the first")
+    counts = [1 + s % 2 for s in range(n_seqs)]
+    n = sum(counts)
+    k, v = _rand(2, n + 40, n_seqs), _rand(2, n + 40, n_seqs + 1)
+    table = _ints(np.arange(n_seqs)[:, None])
+    sides = []
+    for lead in (0, 37):
+        c, _ = _new(C, n_seqs + 1, 2, 64, O.E4M3, junk=False)
+        C.crisp_cache_append(c, table, _ints([3] * n_seqs), _ints(_ptr(counts) + lead), k[:, 37 - lead:].contiguous().to(DEV),
+                             v[:, 37 - lead:].contiguous().to(DEV))
+        sides.append(c)
+    assert torch.equal(sides[0].pages, sides[1].pages) and torch.equal(sides[0].scales, sides[1].scales)
+    assert (sides[0].pages[:n_seqs].flatten(1) != 0).any(1).all() and (sides[0].pages[n_seqs] == 0).all()
+
+
 def test_append_leaves_the_rest():
     """Other pages, other tokens of the page, and rows of no page stay as they were; positions past the
     table and in holes are dropped."""
