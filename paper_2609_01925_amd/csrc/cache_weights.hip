@@ -380,7 +380,7 @@ __global__ __launch_bounds__(kThreads) void weigh_join(WeightArgs a) {
     for (int n = a.b.n_seqs; n > 1;) {
       const int step = (n + kWave - 1) / kWave, probe = lane * step;
       const unsigned long long ok = __ballot(probe < n && a.s.row_ptr[s + min(probe, n - 1)] <= row);
-      const int k = max(__popcll(ok) - 1, 0);
+      const int k = max((int)__popcll(ok) - 1, 0);  // (its type is unsigned)
       s += k * step;
       n = min(step, n - k * step);
     }

@@ -162,6 +162,49 @@ def test_weights_holes_and_bad_pages():
     _check_weights(C, c, oracle, table, [398, 129], [2, 1], 4, held=[300, 129], seed=4)
 
 
+@pytest.mark.parametrize("n_seqs,rows", [(3, 40), (70, 9), (70, 1), (3, 2)])
+def test_weights_with_rows_before_the_first_sequence(n_seqs, rows):
+    """Rows that lie before all sequences, or behind them, weigh nothing."""
+    C = _crisp()
+    _say(f"weights n_seqs={n_seqs} rows={rows}, rows before the first")
+    c, oracle, table, _ = _filled(C, [100] * n_seqs, 1, 64, O.E4M3, n_seqs)
+    ends = _ptr([rows] * n_seqs)
+    q = _rand(4, int(ends[-1]) + 60, 1)
+    args = (c, _ints(table), _ints([100 - rows] * n_seqs))
+    w, held = torch.rand(n_seqs, 1, 128, device=DEV), _ints([7] * n_seqs)
+    got = [C.crisp_cache_weights(*args, _ints(ends + lead), q[:, 37 - lead:].contiguous().to(DEV), w, held, out=torch.zeros_like(w))
+           for lead in (0, 37)]
+    assert torch.equal(*got) and got[0].isfinite().all()
+
+
+def test_weights_values_out_of_range_stay_within_the_buffers():
+    """Lengths, offsets of rows and what is held are brought into range; offsets that do not ascend change nothing elsewhere."""
+    C = _crisp()
+    _say("weights out of range")
+    c, oracle, table, _ = _filled(C, [250, 190, 60], 2, 64, O.E4M3, 9)
+    t = _ints(table)
+    for hq, n in ((4, 6), (8, 100)):
+        q = _rand(hq, n, 1).to(DEV)
+        w = torch.rand(3, 2, 256, device=DEV)
+        big = torch.full((3, 3, 2, 256), 7.0, device=DEV)
+        out = big[1]
+
+        def run(lens, ends, held):
+            big.fill_(7.0)
+            C.crisp_cache_weights(c, t, _ints(lens), _ints(ends), q, w, _ints(held), out=out)
+            assert (big[0] == 7.0).all() and (big[2] == 7.0).all()
+            return out.clone()
+
+        lowest, highest = -(1 << 31), (1 << 31) - 1
+        for first in (1 << 30, 200):  # (rows of the first and the last see places that nothing was stored in: NaN here)
+            got = run([first, -7, 40], [lowest, 2, 4, highest], [highest, lowest, 5])
+            want = run([min(first, 256), 0, 40], [0, 2, 4, n], [256, 0, 5])
+            assert torch.equal(torch.nan_to_num(got, nan=-1.0), torch.nan_to_num(want, nan=-1.0))
+            assert first > 256 or not got[:2].isnan().any()
+        run([100, 100, 40], [5, 1, 6, 3], [1, 2, 3])
+        run([100, 100, 40], [highest, lowest, highest, 0], [1, 2, 3])
+
+
 def test_weights_and_moves_without_a_table():
     """A table of no pages: nothing is seen, what is held stays, kept positions are zeros."""
     C = _crisp()
