@@ -492,7 +492,7 @@ crisp_status crisp_cache_weights_workspace_size(const crisp_cache_shape* cache, 
  *   out[s][g][j] = (j < held[s] ? weights[s][g][j] : 0) + sum_{h of g, rows r with j <= t(r)} softmax_j(softmax_scale q[h][r] . k_j),
  * the rows and the positions that they see being crisp_cache_attn's (appended before; the sum of a position without a page is 0).  All in
  * 32 bits and in a fixed order.  out may be weights, or does not overlap it; positions behind stay as they were.  A row of q that is not
- * finite makes the sums of what it sees NaN.  Afterwards seq_len[s] + its rows is the next call's held[s]. */
+ * finite makes the sums of what it sees NaN.  Without rows (q and workspace may then be null) what is held goes to out all the same.  Afterwards seq_len[s] + its rows is the next call's held[s]. */
 crisp_status crisp_cache_weights(const crisp_cache_shape* cache, const crisp_cache_batch* batch, int32_t n_q_heads,
                                  float softmax_scale, const uint8_t* pages, const float* scales, const int32_t* table,
                                  const int32_t* seq_len, const int32_t* row_ptr, const crisp_bf16* q,

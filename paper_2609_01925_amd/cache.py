@@ -134,7 +134,8 @@ class KVCache:
                out: Optional[torch.Tensor] = None, weigh: bool = False) -> torch.Tensor:
         """One layer of a step: rows row_ptr[s] .. row_ptr[s + 1] of k and v behind sequence s's tokens, then q's
         rows over all of them -> o.  Rows of a sequence without room are not stored and get 0; of more rows than
-        its room the ones behind it get no defined result.  With weigh the attention that each token gets is added to its weight."""
+        its room the ones behind it get no defined result.  With weigh the attention that each token gets is added to its
+        weight (a sequence's weights are not defined after more rows than its room)."""
         cache = self.layers[layer]
         if weigh:
             self._need_weights()

@@ -626,8 +626,10 @@ hipError_t launch_cache_weights(const CacheDims& c, const BatchDims& b, const Se
     if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_tokens<kCacheE4M3>), tokens, threads, 0, stream, a);
     else hipLaunchKernelGGL((weigh_tokens<kCacheInt8>), tokens, threads, 0, stream, a);
   } else {
-    if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_rows_few<kCacheE4M3>), rows, threads, 0, stream, a);
-    else hipLaunchKernelGGL((weigh_rows_few<kCacheInt8>), rows, threads, 0, stream, a);
+    if (b.n_rows > 0 && hq > 0) {
+      if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_rows_few<kCacheE4M3>), rows, threads, 0, stream, a);
+      else hipLaunchKernelGGL((weigh_rows_few<kCacheInt8>), rows, threads, 0, stream, a);
+    }
     if (p.waiting > 0) {
       if (c.fmt == kCacheE4M3) hipLaunchKernelGGL((weigh_tokens_few<kCacheE4M3, true>), tokens, threads, 0, stream, a);
       else hipLaunchKernelGGL((weigh_tokens_few<kCacheInt8, true>), tokens, threads, 0, stream, a);

@@ -69,15 +69,15 @@ crisp_status crisp_cache_weights(const crisp_cache_shape* cache, const crisp_cac
   if (!(softmax_scale >= 0.f) || !isfinite(softmax_scale))
     return fail(CRISP_EINVAL, "softmax_scale must be finite and >= 0");
   CHECK(check_strides(q_head_stride, q_row_stride, false, n_q_heads, b.n_rows, "q"));
-  if (empty(b) || n_q_heads == 0) return CRISP_OK;
+  if (b.n_seqs == 0) return CRISP_OK;  // (without rows the weights that are held still go to out)
   CHECK(check_pages(pages, scales));
   CHECK(check_seqs(b, table, seq_len, row_ptr));
-  CHECK(check_ptr(q, 16, "q"));
+  if (b.n_rows > 0 && n_q_heads > 0) CHECK(check_ptr(q, 16, "q"));
   CHECK(check_ptr(weights, 4, "weights"));
   CHECK(check_ptr(out, 4, "out"));
   CHECK(check_ptr(held, 4, "held"));
-  CHECK(check_ptr(workspace, 256, "workspace"));
   const size_t need = cache_weights_bytes(c, b, n_q_heads);
+  if (need > 0) CHECK(check_ptr(workspace, 256, "workspace"));
   if (workspace_bytes < need) return fail(CRISP_EINVAL, "workspace too small: %zu < %zu", workspace_bytes, need);
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)kHeadDim);
   return hip_status(launch_cache_weights(c, b, Seqs{table, seq_len, row_ptr}, n_q_heads, scale, q,

@@ -162,6 +162,51 @@ def test_weights_holes_and_bad_pages():
     _check_weights(C, c, oracle, table, [398, 129], [2, 1], 4, held=[300, 129], seed=4)
 
 
+@pytest.mark.parametrize("hq", [0, 4])
+def test_weights_without_rows(hq):
+    """No row in the whole call: what is held goes to out, the positions behind it become 0."""
+    C = _crisp()
+    _say(f"weights without rows hq={hq}")
+    c, oracle, table, _ = _filled(C, [200, 131], 2, 64, O.E4M3, 1)
+    _check_weights(C, c, oracle, table, [198, 130], [0, 0], 4, held=[50, 130], seed=1)
+    w, out = torch.rand(2, 2, 256, device=DEV), torch.full((2, 2, 256), 7.0, device=DEV)
+    rows = torch.zeros(hq, 0 if hq else 3, 128, dtype=torch.bfloat16, device=DEV)
+    C.crisp_cache_weights(c, _ints(table), _ints([198, 130]), _ints([0, 0, 0]), rows, w, _ints([50, 200]), out=out)
+    want = torch.full_like(out, 7.0)
+    want[0, :, :198], want[0, :, :50], want[1, :, :130] = 0.0, w[0, :, :50], w[1, :, :130]
+    assert torch.equal(out, want)
+
+
+def test_weights_of_forks():
+    """Sequences that share all their pages: more tiles together than the cache has, so that some sequences' scores wait and others' do not."""
+    C = _crisp()
+    _say("weights of forks")
+    c, oracle, table, _ = _filled(C, [300], 2, 64, O.E4M3, 6)
+    _check_weights(C, c, oracle, np.repeat(table, 9, 0), [299] * 9, [1] * 9, 8, held=[299, 0, 5] * 3, seed=6)
+    _check_weights(C, c, oracle, np.repeat(table, 9, 0), [298, 1, 250, 64, 299, 0, 127, 298, 60], [1, 2, 0, 1, 1, 1, 1, 2, 1], 8,
+                   held=[0] * 9, seed=7)
+
+
+def test_weights_of_many_sequences():
+    """More of them than scores are kept for."""
+    C = _crisp()
+    _say("weights of 1030 sequences")
+    rng = np.random.default_rng(8)
+    lens, counts = rng.integers(0, 140, 1030).tolist(), rng.integers(0, 3, 1030).tolist()
+    c, oracle, table, _ = _filled(C, [a + b for a, b in zip(lens, counts)], 1, 64, O.INT8, 8)
+    _check_weights(C, c, oracle, table, lens, counts, 3, held=lens, seed=8)
+
+
+def test_weights_of_a_few_rows_beside_many():
+    """Few rows a sequence on average, one sequence with many; and the other way round."""
+    C = _crisp()
+    _say("weights of mixed rows")
+    for counts, seed in (([1] * 30 + [90] + [1] * 9, 1), ([100, 1, 0, 140], 2)):
+        lens = [70 + 13 * (s % 7) for s in range(len(counts))]
+        c, oracle, table, _ = _filled(C, [a + b for a, b in zip(lens, counts)], 2, 64, O.E4M3, seed)
+        _check_weights(C, c, oracle, table, lens, counts, 8, held=lens, seed=seed)
+
+
 @pytest.mark.parametrize("n_seqs,rows", [(3, 40), (70, 9), (70, 1), (3, 2)])
 def test_weights_with_rows_before_the_first_sequence(n_seqs, rows):
     """Rows that lie before all sequences, or behind them, weigh nothing."""
@@ -515,7 +560,96 @@ def test_gather_of_a_batch_equals_appending_the_kept_values():
                 assert (b[one[s, p]] == b[two[s, p]]).all()
 
 
+# ------------------------------------------------------------------ far offsets
+
+
+def test_pages_past_32_bits():
+    """The same tokens in a small cache and in the last pages of one of more than 2^32 bytes."""
+    C = _crisp()
+    _say("pages past 32 bits")
+    heads, lens, far = 8, [200, 130], 33000
+    small, big = C.make_cache(12, heads, 64, C.CACHE_E4M3, DEV), C.make_cache(far + 12, heads, 64, C.CACHE_E4M3, DEV)
+    assert big.pages.numel() > 1 << 32
+    table, new = _ints([[3, 0, 5, 1], [2, 4, 6, -1]]), _ints([[7, 8], [9, 10]])
+    k, v, q = _rand(heads, 330, 1).to(DEV), _rand(heads, 330, 2).to(DEV), _rand(2 * heads, 2, 3).to(DEV)
+    got = []
+    for c, at in ((small, 0), (big, far)):
+        c.pages.zero_()
+        c.scales.fill_(1.0)
+        t, nt = torch.where(table < 0, table, table + at), new + at
+        C.crisp_cache_append(c, t, _ints([0, 0]), _ints([0, 200, 330]), k, v)
+        w = C.crisp_cache_weights(c, t, _ints([n - 1 for n in lens]), _ints([0, 1, 2]), q, torch.zeros(2, heads, 256, device=DEV), _ints([0, 0]))
+        many = C.crisp_cache_weights(c, t, _ints([100, 100]), _ints([0, 100, 130]), k[:, :130].repeat(2, 1, 1), torch.zeros_like(w), _ints([0, 0]))
+        kept, count = C.crisp_cache_keep(w, _ints(lens), _ints(lens), _ints([100, 70]), 128)
+        C.crisp_cache_gather(c, t, kept, count, nt)
+        got.append((w, many, kept, c.pages[at:at + 11], c.scales[at:at + 11]))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert (big.pages[:12] == 0).all()
+
+
+def test_weights_and_lists_past_32_bits():
+    """Buffers of the largest width, whose last head begins behind 2^31 values, against ones of the usual width."""
+    C = _crisp()
+    _say("weights and lists past 32 bits")
+    heads, n, m, wide = 9, 20000, 100, 1 << 28
+    rng = np.random.default_rng(1)
+    table, n_pages = _table([n], 64, rng, extra=4)
+    c = C.make_cache(n_pages, heads, 64, C.CACHE_E4M3, DEV)
+    k, q = _rand(heads, n, 1).to(DEV), _rand(heads, 20, 2).to(DEV)
+    C.crisp_cache_append(c, _ints(table), _ints([0]), _ints([0, n]), k, k)
+    new = _ints(_new_pages(table, n_pages, 2))
+    first = torch.from_numpy(np.exp(rng.standard_normal((1, heads, n)))).float().to(DEV)
+    got = []
+    for width in (n, wide):
+        w = torch.empty(1, heads, width, device=DEV)
+        w[:, :, :n] = first
+        for rows in (1, 20):
+            C.crisp_cache_weights(c, _ints(table), _ints([n - rows]), _ints([0, rows]), q[:, :rows], w, _ints([n]))
+        before = w[:, :, :n].clone()
+        cap = m if width == n else wide
+        kept, count = C.crisp_cache_keep(w, _ints([n]), _ints([n]), _ints([m]), cap, 4, 16, w)
+        assert (kept[0, heads - 1, m:] == -1).all()
+        c.pages[new.long()] = 0
+        C.crisp_cache_gather(c, _ints(table), kept, count, new)
+        got.append((before, w[:, :, :n].clone(), kept[:, :, :m].clone(), c.pages[new.long()], c.scales[new.long()]))
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+
+
 # ------------------------------------------------------------------ together
+
+
+def test_long_choices_in_a_graph():
+    """The choice from more tokens than one workgroup takes, captured with a workspace: replays follow the device's lengths and budgets."""
+    C = _crisp()
+    _say("long choices in a graph")
+    w = torch.rand(2, 2, 40000, device=DEV)
+    n, keep, held = _ints([40000, 300]), _ints([5000, 100]), _ints([40000, 40000])
+    ws = C.cache_keep_workspace(w, in_place=True)
+    kept_of = []
+
+    def once():
+        kept_of[:] = C.crisp_cache_keep(w, held, n, keep, 20000, 4, 64, w, ws)
+
+    once()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        once()
+    captured = list(kept_of)
+    for i, (lens, budget) in enumerate((([40000, 300], [5000, 100]), ([20000, 17000], [20000, 16999]), ([16384, 40000], [16000, 1]),
+                                        ([30001, 39999], [0, 20001]))):
+        x = torch.rand(2, 2, 40000, generator=torch.Generator().manual_seed(i)).to(DEV)
+        n.copy_(_ints(lens))
+        keep.copy_(_ints(budget))
+        w.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (*captured, w)]
+        w.copy_(x)
+        once()
+        for a, b in zip(got, (*kept_of, w)):
+            assert torch.equal(a, b)
 
 
 def test_evicting_steps_in_a_graph():

@@ -319,6 +319,42 @@ def test_packed_long_prompt():
             assert (np.abs(got[h, r] - want) <= tol).all()
 
 
+def test_packed_rows_past_32_bits():
+    """Rows whose elements lie further apart than 2^31 from the first to the last."""
+    C = _crisp()
+    _say("packed rows past 32 bits")
+    n, ptr = 300, _ints([0, 40, 300])
+    qkv = [_rand(1, n, seed).to(DEV) for seed in (1, 2, 3)]
+
+    def spread(stride):
+        return torch.empty(n * stride, dtype=torch.bfloat16, device=DEV).as_strided((1, n, 128), (128, stride, 1))
+
+    far = [spread((1 << 23) + 8), spread((1 << 23) - 8), spread((1 << 23) - 8)]
+    for a, b in zip(far, qkv):
+        a.copy_(b)
+    out = spread((1 << 23) + 16)
+    want = C.crisp_packed_attn(ptr, *qkv)
+    assert torch.equal(C.crisp_packed_attn(ptr, *far, out=out), want) and torch.equal(out, want)
+    table, start = C.make_rope(), _ints([7, 100])
+    turned = C.crisp_rope(table, start, ptr, qkv[0], qkv[1])
+    C.crisp_rope(table, start, ptr, far[0], far[1], out, far[1])
+    assert torch.equal(out, turned[0]) and torch.equal(far[1], turned[1])
+
+
+def test_row_ptr_that_does_not_ascend_stays_within_the_buffers():
+    C = _crisp()
+    _say("packed row_ptr that does not ascend")
+    n = 300
+    big = torch.full((3, n + 200, 128), 7.0, dtype=torch.bfloat16, device=DEV)
+    q, k, v = _rand(1, n, 1).to(DEV), _rand(1, n, 2).to(DEV), _rand(1, n, 3).to(DEV)
+    rng = np.random.default_rng(1)
+    for ends in ([0, 200, 100, 300], [300, 0], [250, 10, 260, 20, 300], [0, (1 << 31) - 1, -(1 << 31), 150], rng.integers(0, 300, 90).tolist()):
+        big.fill_(7.0)
+        C.crisp_packed_attn(_ints(ends), q, k, v, out=big[1:2, :n])
+        C.crisp_rope(C.make_rope(), _ints([0] * (len(ends) - 1)), _ints(ends), q, q_out=big[2:3, :n])
+        assert (big[0] == 7.0).all() and (big[1:, n:] == 7.0).all()
+
+
 def test_ropes_and_attention_on_another_stream_and_in_a_graph():
     """A captured call follows the device values of its replay: lengths that move within the same rows, other tensors' contents."""
     C = _crisp()

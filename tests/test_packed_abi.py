@@ -160,6 +160,13 @@ def test_weights_refusals():
     assert C.lib.crisp_cache_weights_workspace_size(REF(_cache()), REF(C.CrispCacheBatch(2, 4, 3)), 4, None) == C.CRISP_EINVAL
 
 
+def test_weights_without_rows_need_the_rest():
+    """The weights that are held go to out all the same: q and the workspace alone may be missing."""
+    for change in (dict(b=(2, 4, 0)), dict(hq=0)):
+        for name in "pstnrwoh":
+            assert _weights(**change, **{name: None}) == C.CRISP_EINVAL, name
+
+
 def test_weights_workspace_is_enough_for_fewer_rows():
     sizes = []
     for rows in list(range(0, 2000, 7)) + [1 << k for k in range(11, 25)]:
@@ -204,9 +211,7 @@ def test_gather_refusals():
 
 def test_eviction_nothing_to_do():
     none = dict(p=None, s=None, t=None)
-    for b in ((0, 4, 3), (2, 4, 0)):
-        assert _weights(b=b, n=None, r=None, q=None, w=None, o=None, h=None, ws=None, wsb=0, **none) == C.CRISP_OK
-    assert _weights(hq=0, n=None, r=None, q=None, w=None, o=None, h=None, ws=None, wsb=0, **none) == C.CRISP_OK
+    assert _weights(b=(0, 4, 3), n=None, r=None, q=None, w=None, o=None, h=None, ws=None, wsb=0, **none) == C.CRISP_OK
     assert _keep(seqs=0, w=None, h=None, n=None, m=None, k=None, c=None, o=None) == C.CRISP_OK
     assert _gather(b=(0, 4, 0), k=None, c=None, n=None, **none) == C.CRISP_OK
     assert _gather(wide=0, k=None, c=None, n=None, **none) == C.CRISP_OK
