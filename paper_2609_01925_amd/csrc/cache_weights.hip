@@ -302,13 +302,16 @@ __device__ __forceinline__ void over_tiles(const WeightArgs& a, const SeqRows& r
   __syncthreads();
 }
 
+// A staged tile's products: a lane's rows are 16 consecutive tokens and its column a pair, or (TURNED) its rows are pairs 4 (lane / 16) + [0, 4)
+// and its columns the tokens 16 (c / 4) + 4 t + c % 4, c = lane % 16, so that sums over pairs stay within the lane.
+template <bool TURNED = false>
 __device__ __forceinline__ void products(const bf16x8 (&k)[16][kWave], const bf16x8 (&q)[4], int lane, acc4 (&s)[4]) {
 #pragma unroll
   for (int t = 0; t < 4; ++t) s[t] = acc4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-    for (int t = 0; t < 4; ++t) s[t] = mfma16(k[4 * t + kk][lane], q[kk], s[t]);
+    for (int t = 0; t < 4; ++t) s[t] = TURNED ? mfma16(q[kk], k[4 * t + kk][lane], s[t]) : mfma16(k[4 * t + kk][lane], q[kk], s[t]);
 }
 
 // fn(std::integral_constant of the groups that a wave has), 1 .. kOwn.
@@ -392,6 +395,17 @@ __global__ __launch_bounds__(kThreads) void weigh_join(WeightArgs a) {
   }
 }
 
+// x[g] summed over the four lanes of a column, on the one of group g.
+__device__ __forceinline__ float group_sums(const float (&x)[4]) {
+  typedef __attribute__((__vector_size__(2 * sizeof(unsigned)))) unsigned u32x2;
+  const auto halves = [](float a, float b) {  // (a below and above lane 32 together, b's on the lanes above)
+    const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  };
+  const u32x2 r = __builtin_amdgcn_permlane16_swap(__float_as_uint(halves(x[0], x[2])), __float_as_uint(halves(x[1], x[3])), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // A tile's sums over the lanes of a row of 16; lane c of them takes token c.
 __device__ __forceinline__ float row_sums(const float (&acc)[16], int lane) {
   float sum = 0.f;
@@ -424,6 +438,8 @@ template <int FMT>
 __global__ __launch_bounds__(kThreads, 2) void weigh_tokens(WeightArgs a) {
   __shared__ bf16x8 kst[2][16][kWave];
   __shared__ float parts[2][kWaves][kTile];
+  __shared__ __attribute__((aligned(16))) int sight[kPairs];  // the last positions that the pass's pairs see
+  static_assert(kPairs == kThreads);
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Item it = item_of(a, a.token_wgs);
   const SeqRows r = seq_rows(a.s, a.b, a.c.B, it.seq);
@@ -441,14 +457,16 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_tokens(WeightArgs a) {
   for (int p0 = 0; p0 < pairs; p0 += kPairs)
     by_groups((min(pairs - p0, kPairs) + kGroup - 1) / kGroup, [&](auto groups) {
       constexpr int NI = decltype(groups)::value;
-      float sub[NI];
-      Sight see[NI];
+      sight[tid] = r.len + min(p0 + tid, pairs - 1) / a.G;  // (the pass before has ended with a barrier, its first tile begins with one)
+      float sub[NI][4];  // this lane's pairs' logarithms
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        see[i] = Sight(a, r, p0 + (w + kWaves * i) * kGroup, pairs);
-        const int p = p0 + (w + kWaves * i) * kGroup + (lane & 15);
-        sub[i] = p < pairs ? a.lse[pair_of(a, r, it.head, p)] : __builtin_inff();
-      }
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int p = p0 + (w + kWaves * i) * kGroup + 4 * (lane >> 4) + e;
+          sub[i][e] = p < pairs ? a.lse[pair_of(a, r, it.head, p)] : __builtin_inff();
+        }
+      const Sight see(a, r, p0 + w * kGroup, pairs);
       float old = 0.f;
       const auto start = [&](int t) {  // of a tile that this wave writes
         const int at = t * kTile + lane;
@@ -462,24 +480,29 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_tokens(WeightArgs a) {
       over_tiles<FMT, NI>(a, r, it, p0, pairs, t0, t1, kst, [&](int t, bool ok, float kc, const bf16x8 (&q)[NI][4], const bf16x8 (&k)[16][kWave]) {
         if (t > t0 && w == ((t - 1) & 3)) write(t - 1);
         if (w == (t & 3)) start(t);
-        float acc[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[e] = 0.f;
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};  // of the four columns
         if (ok) {
           acc4 s[NI][4];
 #pragma unroll
-          for (int i = 0; i < NI; ++i) products(k, q[i], lane, s[i]);
-          if (see[0].whole(t)) {  // by the wave's first pairs, so by all: no branch between the groups
+          for (int i = 0; i < NI; ++i) products<true>(k, q[i], lane, s[i]);
+          if (see.whole(t)) {  // by the wave's first pairs, so by all: no branch between the groups
 #pragma unroll
             for (int i = 0; i < NI; ++i)
 #pragma unroll
-              for (int e = 0; e < 16; ++e) acc[e] += fast_exp2(__builtin_fmaf(s[i][e >> 2][e & 3], kc, -sub[i]));
+              for (int e = 0; e < 16; ++e) acc[e >> 2] += fast_exp2(__builtin_fmaf(s[i][e >> 2][e & 3], kc, -sub[i][e & 3]));
           } else {
+            const int first = t * kTile + 16 * ((lane & 15) >> 2) + (lane & 3);
 #pragma unroll
-            for (int i = 0; i < NI; ++i) add_weights(see[i], s[i], kc, sub[i], t, acc);
+            for (int i = 0; i < NI; ++i) {
+              const int4 x = *reinterpret_cast<const int4*>(&sight[(w + kWaves * i) * kGroup + 4 * (lane >> 4)]);
+              const int own[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                acc[e >> 2] += first + 4 * (e >> 2) > own[e & 3] ? 0.f : fast_exp2(__builtin_fmaf(s[i][e >> 2][e & 3], kc, -sub[i][e & 3]));
+            }
           }
         }
-        parts[(t - t0) & 1][w][lane] = row_sums(acc, lane);
+        parts[(t - t0) & 1][w][16 * ((lane & 15) >> 2) + 4 * (lane >> 4) + (lane & 3)] = group_sums(acc);
       });
       if (w == ((t1 - 1) & 3)) write(t1 - 1);
       __syncthreads();
