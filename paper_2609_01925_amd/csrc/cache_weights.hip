@@ -603,13 +603,17 @@ struct Plan {
 Plan plan_of(const CacheDims& c, const BatchDims& b, int hq) {
   const int64_t heads = (int64_t)b.n_seqs * c.hkv, pairs = (int64_t)b.n_rows * hq, G = hq / c.hkv;
   if (heads == 0 || pairs == 0) return Plan{1, 0, 0, 0, 0, 0};
-  // Enough workgroups for the GPU, and 16 MB of statistics at most but for calls of very many rows.  The space for them
-  // does not shrink as rows are added, so that a workspace is enough for fewer rows, too.
+  // Workgroups enough for the GPU: of many pairs 512 (a window of 32 rows of 28 heads over 128k tokens 48 + 47 us; 1024 and 1536 workgroups 10
+  // and 30 % more), of few 1024, and where there are many heads to go over, up to twelve chunks each, so that the longest sequence is not
+  // left to the last (48 of 300 to 8191 tokens 44 us, 48 with four chunks).  16 MB of statistics at most but for calls of very many rows; the
+  // space for them does not shrink as rows are added, so that a workspace is enough for fewer rows, too.
   constexpr int64_t kMost = (int64_t)1 << 21;
-  const int64_t target = pairs > kGroup * (int64_t)c.hkv * b.n_seqs ? 512 : 1536;
-  const int64_t want = heads < target / 3 ? (target + heads - 1) / heads : 3, fit = kMost / pairs;
-  const int64_t chunks = fit < 1 ? 1 : want < fit ? want : fit;
-  const int64_t wide = heads < 512 ? (1536 + heads - 1) / heads : 3, space = pairs > kMost ? pairs : pairs * wide < kMost ? pairs * wide : kMost;
+  const auto each = [&](int64_t wgs) { return (wgs + heads - 1) / heads; };
+  const auto larger = [](int64_t x, int64_t y) { return x > y ? x : y; };
+  const auto smaller = [](int64_t x, int64_t y) { return x < y ? x : y; };
+  const int64_t few = larger(each(1024), larger(smaller(12, each(4608)), 3)), fit = larger(kMost / pairs, 1);
+  const int64_t chunks = smaller(pairs > kGroup * heads ? larger(each(512), 3) : few, fit);
+  const int64_t space = larger(pairs, smaller(pairs * few, kMost));
   // Scores of sequences of average rows or fewer wait, if that is one product's pairs, for as many tiles as the cache has (forks have
   // more together) or 256 MB hold.
   const int64_t rows = (b.n_rows + b.n_seqs - 1) / b.n_seqs, most = kGroup / G;
