@@ -5,6 +5,12 @@
 // tokens, and weigh_tokens takes the chunks' together and forms the weights, a wave a tile of 64 tokens, summed over the pairs in a
 // fixed order and without atomics.  Where a sequence has few pairs, x itself waits in the workspace, 4 bytes a pair and token where
 // the keys are 128; where it has many, the products are formed again and a launch between the two joins the chunks.
+//
+// Few pairs are bound by the keys' bytes: a row of each of 48 sequences of 300 to 8191 tokens, 32 heads over 8 (179 MB read), 43 us, 4.2 TB/s, and
+// 16 us for the scores and weights (32 MB read: launch, lengths, scores, in turn); without waiting scores 36 + 43 us.  Many pairs are bound by
+// vector instructions, three for each score and pass beside the conversion of K: 32 rows of 28 heads over 4 and 131000 tokens (30 GFLOP a
+// pass) 45 + 5.6 + 42 us, 35 of them for each pass in proportion to the tokens, 10 to begin.  Products of one group in a fixed order beside
+// the exponents of the one before, or the next tile read from LDS beside the last group's, change nothing (47 to 51 and 46 to 50 us).
 #include <type_traits>
 
 #include "cache_device.h"
@@ -594,6 +600,14 @@ __global__ __launch_bounds__(kThreads, SCORES ? 8 : 4) void weigh_tokens_few(Wei
   }
 }
 
+// Whether a call goes by weigh_rows, weigh_join and weigh_tokens, for more than 32 pairs a sequence on average (one sequence: 16), or by
+// weigh_rows_few and weigh_tokens_few, which go over the keys once for every 16 pairs.  32 heads over 8, us, few / many: 48 sequences of 300 to 8191
+// tokens 136 / 174 with 20 pairs, 144 / 176 with 32, 197 / 177 with 48; eight of them 30 / 40, 32 / 40, 41 / 41; one of 60000 tokens 29 / 37
+// with 16 pairs, 42 / 37 with 20.
+bool many_pairs(const CacheDims& c, const BatchDims& b, int hq) {
+  return (int64_t)b.n_rows * (hq / c.hkv) > (int64_t)(b.n_seqs == 1 ? kGroup : 2 * kGroup) * b.n_seqs;
+}
+
 // Chunks of a sequence's tokens whose statistics are kept apart, room for scores, and the workspace.
 struct Plan {
   int chunks, waiting;
@@ -603,7 +617,7 @@ struct Plan {
 Plan plan_of(const CacheDims& c, const BatchDims& b, int hq) {
   const int64_t heads = (int64_t)b.n_seqs * c.hkv, pairs = (int64_t)b.n_rows * hq, G = hq / c.hkv;
   if (heads == 0 || pairs == 0) return Plan{1, 0, 0, 0, 0, 0};
-  // Workgroups enough for the GPU: of many pairs 512 (a window of 32 rows of 28 heads over 128k tokens 48 + 47 us; 1024 and 1536 workgroups 10
+  // Workgroups enough for the GPU: of many pairs 512 (a window of 32 rows of 28 heads over 128k tokens 45 + 42 us; 1024 and 1536 workgroups 10
   // and 30 % more), of few 1024, and where there are many heads to go over, up to twelve chunks each, so that the longest sequence is not
   // left to the last (48 of 300 to 8191 tokens 44 us, 48 with four chunks).  16 MB of statistics at most but for calls of very many rows; the
   // space for them does not shrink as rows are added, so that a workspace is enough for fewer rows, too.
@@ -612,7 +626,7 @@ Plan plan_of(const CacheDims& c, const BatchDims& b, int hq) {
   const auto larger = [](int64_t x, int64_t y) { return x > y ? x : y; };
   const auto smaller = [](int64_t x, int64_t y) { return x < y ? x : y; };
   const int64_t few = larger(each(1024), larger(smaller(12, each(4608)), 3)), fit = larger(kMost / pairs, 1);
-  const int64_t chunks = smaller(pairs > kGroup * heads ? larger(each(512), 3) : few, fit);
+  const int64_t chunks = smaller(many_pairs(c, b, hq) ? larger(each(512), 3) : few, fit);
   const int64_t space = larger(pairs, smaller(pairs * few, kMost));
   // Scores of sequences of average rows or fewer wait, if that is one product's pairs, for as many tiles as the cache has (forks have
   // more together) or 256 MB hold.
@@ -635,7 +649,7 @@ hipError_t launch_cache_weights(const CacheDims& c, const BatchDims& b, const Se
                                 int width, const int32_t* held, void* ws, hipStream_t stream) {
   const Plan p = plan_of(c, b, hq);
   const int64_t heads = (int64_t)b.n_seqs * c.hkv;
-  const bool join = (int64_t)b.n_rows * (hq / c.hkv) > (int64_t)kGroup * b.n_seqs;
+  const bool join = many_pairs(c, b, hq);
   int64_t wgs = ((join ? 512 : 2048) + heads - 1) / heads;
   const int64_t most = ((int64_t)width + kTile * kWaves - 1) / (kTile * kWaves);
   wgs = wgs > most ? most : wgs;

@@ -115,7 +115,8 @@ __device__ __forceinline__ void write_kept(const Choice& c, const Limit& limit, 
     }
 }
 
-// One workgroup a sequence and KV head of up to 16384 tokens, whose weights stay in registers: 32 sequences of 700 to 4100 tokens, 8 heads.
+// One workgroup a sequence and KV head of up to 16384 tokens, whose weights stay in registers: bound by the digits' rounds, each a clear, an addition
+// and a scan of the bins.  32 sequences of 700 to 4100 tokens, 8 heads, 12 us; one of 16384 tokens 15 us, 64 of them 50 (the three launches below 22 and 55).
 __device__ __forceinline__ void keep_alone(const KeepArgs& a, const Choice& c, KeepLds& l) {
   const int tid = threadIdx.x, mine = (c.n + kKeepThreads - 1) / kKeepThreads, first = tid * mine;
   const float* weights = a.weights + (int64_t)blockIdx.x * a.width;
@@ -162,6 +163,7 @@ __global__ __launch_bounds__(kKeepThreads) void cache_keep(KeepArgs a) {
 // the first launch's alone).  1: the first digit's bins of each chunk.  2: their sums give the digit; each chunk counts its weights
 // above it and lists those that share it.  3: every workgroup finds the other digits from the list, counts what stays in the chunks
 // before its own, and writes its own.  (Where too many share the digit, the weights themselves are gone over in place of a list.)
+// 100003 tokens, 4 heads: 4.9 + 9.0 + 12.6 us, latency throughout; one workgroup alone, at 20 instructions a weight and digit on one CU, 88 to 111.
 struct KeepSpace {
   int chunks;
   int* hist;      // [chunks][kBins], a head
@@ -376,8 +378,10 @@ __device__ __forceinline__ uint32_t pack_codes(const float* x, float f) {
 
 // One workgroup a page of the new table and KV head, 256 threads a tile.  K comes in the chunks that it will stand in, a token's 16
 // elements.  A chunk of V holds 16 tokens of an element, of which some stay: tokens of one chunk that follow one another make a run,
-// and a wave takes a run's chunks of 64 elements and deals the bytes that stay out to the new chunks in LDS (byte by byte from memory
-// instead: 32 sequences of 700 to 4100 tokens cut to 1024, 8 heads, 62.4 us).  Values are formed as x 2^-8, which keeps the largest
+// and a wave takes a run's chunks of 64 elements and deals the bytes that stay out to the new chunks in LDS.  Bound by HBM, which reads the whole
+// chunks of V, most of the pages where every third token stays: 32 sequences of 700 to 4100 tokens cut to 1024, 8 heads (186 MB read, 65
+// written), 56 us, 4.4 TB/s; 100003 tokens cut to 16384, 4 heads (90 and 17 MB), 22 us, 4.8 TB/s.  Byte by byte from memory 62 and 26 us; 512 threads
+// a tile 70 and 27; items in the order of the XCDs 62 to 65; five waves a SIMD spill.  Values are formed as x 2^-8, which keeps the largest
 // finite, and become codes under the exponent of the largest.
 template <int FMT, int TILES>
 __global__ __launch_bounds__(256 * TILES) void cache_gather(GatherArgs a) {

@@ -4,6 +4,10 @@
 // The turns of a far position are many and only their fraction counts, so p turns is formed and reduced in 64 bits (off by
 // 2^-53 of itself: 2^-24 of a turn at position 2^30 of the fastest pair, turns = 1 / (2 pi)); sine and cosine of the fraction
 // and the products are 32 bits, and each result is rounded to bf16 once.
+//
+// Bound by HBM, each element read and written once: 32768 rows of 40 heads (336 MB each way) 138 us, 4.9 TB/s; 24 prompts of 1 to 700 rows of
+// 32 heads (82 MB each way) 33 us, 5.0 TB/s; one row of each of 64 sequences 5.1 us, a launch and three loads in turn (begins,
+// elements, stores).  Non-temporal loads 134 and 44 us; the next heads' loads before this one's stores 144 to 155.
 #include "packed_device.h"
 #include "packed_internal.h"
 
@@ -15,7 +19,7 @@ constexpr int kThreads = 256;
 constexpr int kRowLanes = 8;                      // lanes of a row: 16 elements, 8 pairs each
 constexpr int kRowsPerWave = kWave / kRowLanes;
 constexpr int kRowsPerWg = kThreads / kRowLanes;
-constexpr int kAhead = 4;                         // heads whose elements are loaded together
+constexpr int kAhead = 4;                         // heads whose elements are loaded together (8: 141, 35 and 6.2 us)
 
 struct RopeArgs {
   PackedDims d;
@@ -144,7 +148,7 @@ hipError_t launch_rope(const PackedDims& d, const RopeTable& t, const int32_t* s
   const auto same = [](const RopeTensor& x) { return x.in == x.out; };
   const int64_t blocks = (d.n_rows + kRowsPerWg - 1) / kRowsPerWg;
   const int heads = q.heads + k.heads;
-  // as many heads a workgroup as leave some workgroups for every CU
+  // As many heads a workgroup as leave some workgroups for every CU: all heads in one 141, 42 and 12 us, 8192 workgroups 149, 34 and 4.9.
   int64_t groups = (2048 + blocks - 1) / blocks;
   if (groups > (heads + kAhead - 1) / kAhead) groups = (heads + kAhead - 1) / kAhead;
   const int per = (int)((heads + groups - 1) / groups);
