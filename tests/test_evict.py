@@ -393,6 +393,17 @@ def test_keep_batch_of_all_kinds():
     _check_keep(C, rng.random((11, 2, 300)).astype(np.float32), [1000] * 11, lens, keep, 150, 4, 32)
 
 
+@pytest.mark.parametrize("width", [1, 2, 300, 17000])
+def test_keep_lists_longer_than_the_buffer(width):
+    """More places in the list than the weights have, budgets above every length among them."""
+    C = _crisp()
+    _say(f"keep width={width}, longer lists")
+    rng = np.random.default_rng(width)
+    w = rng.random((3, 2, width)).astype(np.float32)
+    lens = [width, max(width // 2, 1), width]
+    _check_keep(C, w, [width] * 3, lens, [width - 1, width + 3, width + 70], width + 100, 1, 3)
+
+
 @pytest.mark.parametrize("n,m", [(16384, 5000), (16385, 16384), (40000, 1), (70001, 30000), (24576, 24575), (33000, 60)])
 def test_keep_long_sequences(n, m):
     """About as many tokens as one workgroup takes, and more; also in place."""

@@ -275,6 +275,27 @@ def test_evict_without_pages_and_of_granted_rows():
     assert (kv.attend(0, _ptr([1, 0, 0]), x, y, z) == 0).all()  # it takes rows again once some are granted
 
 
+def test_evict_lists_longer_than_the_table():
+    """A cap above what the table holds changes nothing but the lists' length."""
+    from paper_2609_01925_amd.cache import KVCache
+    _say("KVCache evict, cap above the table")
+    sides = []
+    for cap in (100, 5000):
+        kv = KVCache(2, 24, 2, 2, 320, device=DEV, weights=True)
+        n = torch.tensor([300, 170], dtype=torch.int32, device=DEV)
+        kv.reserve(n)
+        ptr = torch.tensor([0, 300, 470], dtype=torch.int32, device=DEV)
+        for layer in range(2):
+            kv.prefill_packed(layer, ptr, _rand(4, 470, layer).to(DEV), _rand(2, 470, 5).to(DEV), _rand(2, 470, 6).to(DEV), weigh=True)
+        kv.advance(n, weighed=True)
+        count = kv.evict(torch.tensor([100, 64], dtype=torch.int32, device=DEV), cap, 4, 16)
+        assert count.tolist() == [100, 64] and kv.seq_len.tolist() == [100, 64]
+        sides.append([kv.table.clone()] + [w[s, :, :m].clone() for w in kv.weights for s, m in ((0, 100), (1, 64))]
+                     + [c.pages[kv.table[kv.table >= 0].long()] for c in kv.layers])
+    for a, b in zip(*sides):
+        assert torch.equal(a, b)
+
+
 def test_steps_that_are_not_weighed():
     """Their tokens have weight 0, also where the buffer holds something else, until a step that is."""
     from paper_2609_01925_amd.cache import KVCache
