@@ -387,7 +387,7 @@ def make_rope(rotary_dim: int = 128, layout: int = ROPE_HALF, base: float = 1000
 def _rows_out(out: Optional[torch.Tensor], name: str, heads: int, n: int, like: torch.Tensor):
     """A packed output of that size, new and contiguous unless given, and its head and row stride."""
     if out is None:
-        return torch.empty((heads, n, 128), dtype=torch.bfloat16, device=like.device), max(n, 1) * 128, 128
+        return like.new_empty((heads, n, 128)), max(n, 1) * 128, 128
     _, m, head, row = _rows(out, name, heads, like.get_device())
     if m != n:
         raise ValueError(f"{name} {tuple(out.shape)} must have {n} rows")
@@ -637,8 +637,7 @@ def crisp_cache_keep(weights: torch.Tensor, held: torch.Tensor, seq_len: torch.T
         ws = cache_keep_workspace(weights, new_weights is not None and new_weights.data_ptr() == weights.data_ptr()) if n_seqs else None
     elif ws.dtype is not torch.uint8 or ws.get_device() != gpu or not ws.is_contiguous():
         raise ValueError(f"ws must be a contiguous uint8 tensor on cuda:{gpu}, got {ws.dtype} on {ws.device}")
-    kept = torch.empty((n_seqs, heads, max(cap, 0)), dtype=torch.int32, device=weights.device)
-    count = torch.empty(n_seqs, dtype=torch.int32, device=weights.device)
+    kept, count = keep.new_empty((n_seqs, heads, max(cap, 0))), keep.new_empty(n_seqs)
     _call(gpu, "crisp_cache_keep", lib.crisp_cache_keep, n_seqs, heads, wide, weights.data_ptr(), held.data_ptr(),
           seq_len.data_ptr(), keep.data_ptr(), sink, recent, cap, kept.data_ptr(), count.data_ptr(),
           None if new_weights is None else new_weights.data_ptr(), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel())
