@@ -571,7 +571,43 @@ def test_gather_of_a_batch_equals_appending_the_kept_values():
                 assert (b[one[s, p]] == b[two[s, p]]).all()
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("block", [64, 128])
+def test_gather_in_any_order(block, fmt):
+    """Positions that do not ascend, and the same one several times."""
+    C = _crisp()
+    _say(f"gather in any order block={block} fmt={fmt}")
+    rng = np.random.default_rng(21)
+    lens = [300, 90]
+    c, oracle, table, n_pages = _filled(C, lens, 2, block, fmt, 21, spread=2, extra=8)
+    kept = np.stack([np.stack([rng.permutation(n)[:70] if h == 0 else rng.integers(0, n // 10, 70) for h in range(2)]) for n in lens]).astype(np.int32)
+    kept[0, 1, 20:40] = kept[0, 1, 20]
+    kept[1, 0, ::-1].sort()
+    _check_gather(C, c, oracle, table, kept, [70, 65], _new_pages(table, n_pages, 2))
+
+
 # ------------------------------------------------------------------ far offsets
+
+
+def test_most_sequences_of_a_call():
+    """As many sequences times KV heads as a call takes, each with the same rows over the same pages."""
+    C = _crisp()
+    _say("2^20 heads")
+    n, heads = 1 << 17, 8
+    c, oracle = _new(C, 4, heads, 64, O.E4M3)
+    table, ones, rp = torch.zeros(n, 1, dtype=torch.int32, device=DEV), torch.ones(n, dtype=torch.int32, device=DEV), torch.arange(n + 1, dtype=torch.int32, device=DEV)
+    k = _rand(heads, 3, 1).to(DEV)
+    C.crisp_cache_append(c, table[:1], _ints([0]), _ints([0, 3]), k, k)
+    q = _rand(heads, 1, 2).to(DEV).expand(heads, n, 128)
+    w, held = torch.zeros(n, heads, 3, device=DEV), torch.zeros(n, dtype=torch.int32, device=DEV)
+    C.crisp_cache_weights(c, table, 2 * ones, rp, q, w, held)
+    assert torch.equal(w, w[:1].expand_as(w)) and (w.sum(-1) - 1).abs().max() < 2.0 ** -18
+    kept, count = C.crisp_cache_keep(w, 3 * ones, 3 * ones, 2 * ones, 2, 0, 1)
+    assert torch.equal(kept, kept[:1].expand_as(kept)) and (count == 2).all() and (kept[0, :, 1] == 2).all()
+    new = torch.full((n, 1), -1, dtype=torch.int32, device=DEV)
+    new[0], new[n - 1], new[n // 2] = 1, 2, 3
+    C.crisp_cache_gather(c, table, kept, count, new)
+    assert torch.equal(c.pages[1], c.pages[2]) and torch.equal(c.pages[1], c.pages[3]) and torch.equal(c.scales[1], c.scales[3])
 
 
 def test_pages_past_32_bits():

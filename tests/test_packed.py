@@ -319,6 +319,24 @@ def test_packed_long_prompt():
             assert (np.abs(got[h, r] - want) <= tol).all()
 
 
+def test_most_rows_and_sequences_of_a_call():
+    """2^24 prompts of one token each: attention gives v, turned rows are those of a call of the last few alone."""
+    C = _crisp()
+    _say("2^24 prompts")
+    n = 1 << 24
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randint(0, 1 << 16, (1, n, 128), generator=g, device=DEV, dtype=torch.int32).to(torch.int16).view(torch.bfloat16)
+    x = torch.where(x.isfinite() & (x.abs() < 2.0 ** 40), x, 1.0)
+    q = _rand(1, 1, 2).to(DEV).expand(1, n, 128)
+    ptr, start = torch.arange(n + 1, dtype=torch.int32, device=DEV), torch.arange(n, dtype=torch.int32, device=DEV)
+    assert torch.equal(C.crisp_packed_attn(ptr, q, q, x), x)
+    table = C.make_rope()
+    last = 1000
+    whole, _ = C.crisp_rope(table, start, ptr, x)
+    few, _ = C.crisp_rope(table, start[-last:], ptr[:last + 1], x[:, -last:])
+    assert torch.equal(whole[:, -last:], few)
+
+
 def test_packed_rows_past_32_bits():
     """Rows whose elements lie further apart than 2^31 from the first to the last."""
     C = _crisp()
