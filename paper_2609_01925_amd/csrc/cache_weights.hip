@@ -143,12 +143,17 @@ __device__ __forceinline__ int64_t pair_of(const WeightArgs& a, const SeqRows& r
   return (int64_t)(r.row0 + p / a.G) * a.hq + head * a.G + p % a.G;
 }
 
-// (m, l) of two disjoint sets of keys together.
+// (m, l) of two disjoint sets of keys together.  Of no keys they are (-infinity, 0); of keys whose scores are all -infinity l is positive:
+// beside a finite m it counts for nothing, and alone it makes the logarithm -infinity and so the weights NaN, as the softmax is.
 __device__ __forceinline__ void merge(float& m, float& l, float m2, float l2) {
   const float top = vmax(m, m2);
-  const float ref = top == -__builtin_inff() ? 0.f : top;
-  l = l * fast_exp2(m - ref) + l2 * fast_exp2(m2 - ref);
+  l = l * (m == top ? 1.f : fast_exp2(m - top)) + l2 * (m2 == top ? 1.f : fast_exp2(m2 - top));
   m = top;
+}
+
+// To be called of a lane's pair behind its keys, the first of them that have a page being tile `first`'s.
+__device__ __forceinline__ void mark_seen(float m, float& l, int first, int last_seen) {
+  if (m == -__builtin_inff() && l == 0.f && first <= last_seen / kTile) l = 1.f;
 }
 
 // The four lanes of a column together.
@@ -241,10 +246,12 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_rows_few(WeightArgs a) {
     if (p0 == 0) slot = first_slot(a, it.seq, T, pairs);
     const Sight see(a, r, p0, pairs);
     float m[1] = {-__builtin_inff()}, l[1] = {0.f};
+    int first = 0x7fffffff;
     for (int t = t0 + w; t < t1; t += kWaves) {
       if (t + kWaves < t1) ok_next = tiles.load(a, it.head, t + kWaves, next, kc_next);
       keep_whole(raw);
       if (ok) {
+        first = min(first, t);
         acc4 s1[1][4];
         acc4(&s)[4] = s1[0];
         products<FMT>(raw, q, s);
@@ -262,6 +269,7 @@ __global__ __launch_bounds__(kThreads, 4) void weigh_rows_few(WeightArgs a) {
       kc = kc_next;
       ok = ok_next;
     }
+    mark_seen(m[0], l[0], first, see.own);
     column(m[0], l[0]);
     if (lane < kGroup) part[w][lane] = make_float2(m[0], l[0]);
     __syncthreads();
@@ -344,6 +352,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_rows(WeightArgs a) {
       constexpr int NI = decltype(groups)::value;
       float m[NI], l[NI];
       Sight see[NI];
+      int first = 0x7fffffff;
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         m[i] = -__builtin_inff();
@@ -352,6 +361,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_rows(WeightArgs a) {
       }
       over_tiles<FMT, NI>(a, r, it, p0, pairs, t0, t1, kst, [&](int t, bool ok, float kc, const bf16x8 (&q)[NI][4], const bf16x8 (&k)[16][kWave]) {
         if (!ok) return;
+        first = min(first, t);
         acc4 s[NI][4];
 #pragma unroll
         for (int i = 0; i < NI; ++i) products(k, q[i], lane, s[i]);
@@ -363,6 +373,7 @@ __global__ __launch_bounds__(kThreads, 2) void weigh_rows(WeightArgs a) {
       });
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
+        mark_seen(m[i], l[i], first, see[i].own);
         column(m[i], l[i]);
         const int p = p0 + (w + kWaves * i) * kGroup + lane;
         if (lane < kGroup && p < pairs) a.stats[pair_of(a, r, it.head, p) * a.chunks + it.i] = make_float2(m[i], l[i]);

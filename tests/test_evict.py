@@ -294,6 +294,42 @@ def test_weights_not_finite():
         assert torch.equal(got, clean)
 
 
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("counts", [[2, 1, 1], [9, 1, 4], [12, 10, 12], [40, 3, 33]])
+def test_weights_of_rows_whose_scores_are_all_minus_infinity(counts, sign):
+    """A row of q that is not finite makes the sums of what it sees NaN, also where all its scores are -infinity: one that sees a single key,
+    one that sees many chunks with a hole; scores that wait, scores that do not, calls of many pairs.  What has no page has no sum."""
+    C = _crisp()
+    _say(f"weights all -infinity counts={counts} sign={sign}")
+    lens = [0, 3000, 130]
+    full = [a + b for a, b in zip(lens, counts)]
+    rng = np.random.default_rng(sum(counts))
+    table, n_pages = _table(full, 64, rng)
+    c, oracle = _new(C, n_pages, 2, 64, O.E4M3)
+    k = _rand(2, sum(full), 1)
+    k[:, :, 9] = sign * (0.5 + k[:, :, 9].abs())
+    _append(C, c, oracle, table, [0] * 3, full, k, _rand(2, sum(full), 2))
+    table[1, 2] = -1
+    table[2] = -1  # the third sequence's rows see nothing
+    ptr, width = _ptr(counts), table.shape[1] * 64
+    q = _rand(4, int(ptr[-1]), 3)
+    w, held = rng.random((3, 2, width)).astype(np.float32), lens
+    want, tol = R.cache_weights(oracle, table, lens, ptr, to_f64(q), 1 / math.sqrt(128), w.astype(np.float64), held)
+    last = counts[1] - 1
+    for row, h in ((0, 1), (int(ptr[1]) + last, 2), (int(ptr[2]), 0)):
+        q[h, row, 9] = -sign * math.inf
+    got = to_f64(C.crisp_cache_weights(c, _ints(table), _ints(lens), _ints(ptr), q.to(DEV), _floats(w), _ints(held),
+                                       out=torch.full((3, 2, width), 7.0, device=DEV)))
+    nan = np.zeros(want.shape, dtype=bool)
+    nan[0, 0, 0] = True
+    nan[1, 1, :3000 + counts[1]] = True
+    nan[1, 1, 128:192] = False
+    assert np.isnan(got[nan]).all()
+    live = ~np.isnan(want) & ~nan
+    assert (np.abs(got - want)[live] <= tol[live]).all()
+    assert (got[1, :, 128:192] == w[1, :, 128:192]).all() and (got[np.isnan(want)] == 7.0).all()
+
+
 def test_weights_strides_repeat_and_workspaces():
     C = _crisp()
     _say("weights strides, workspaces")
