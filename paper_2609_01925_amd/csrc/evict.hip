@@ -8,7 +8,8 @@ namespace {
 constexpr int kKeepThreads = 1024, kKeepWaves = kKeepThreads / kWave;
 constexpr int kBins = 2048, kCopies = 8;              // of a digit of 11 bits (the last has 10)
 constexpr int kMost = 16;                             // tokens of a thread where one workgroup chooses
-constexpr int kPart = 8, kChunk1 = kPart * kKeepThreads;  // tokens of a thread and a workgroup where several do
+constexpr int kPart = 8, kPiece = kPart * kKeepThreads;  // tokens of a thread and a workgroup, at a time, where several do
+constexpr int kMostChunks = 128;                      // workgroups of a head there
 constexpr int kList = 16384;                          // weights that share the first digit of the limit, if no more do
 
 // An unsigned order of floats: NaN lowest, -0 equal to 0.
@@ -88,9 +89,9 @@ __device__ __forceinline__ void next_digit(KeepLds& l, int digit, int a0, int a1
 
 // This thread's `mine` <= N neighbouring tokens from `first` on, of weights x: those that stay are written behind `above` and, of the limit's
 // equals, min(equal, ties) that stay before them.  All of x is in registers, so the weights may go over those that they
-// were read from.
+// were read from.  What the workgroup's tokens add to above, and 2^16 times what they add to equal.
 template <int N>
-__device__ __forceinline__ void write_kept(const Choice& c, const Limit& limit, const float (&x)[N], int first, int mine, int above, int equal,
+__device__ __forceinline__ int write_kept(const Choice& c, const Limit& limit, const float (&x)[N], int first, int mine, int above, int equal,
                                            int* lds, int32_t* kept, float* moved) {
   uint32_t up = 0, same = 0;  // bits of the tokens that stay whatever the equals do, and of those
 #pragma unroll
@@ -113,6 +114,7 @@ __device__ __forceinline__ void write_kept(const Choice& c, const Limit& limit, 
       if (moved) moved[to] = x[i];
       ++to;
     }
+  return total;
 }
 
 // One workgroup a sequence and KV head of up to 16384 tokens, whose weights stay in registers: bound by the digits' rounds, each a clear, an addition
@@ -159,11 +161,18 @@ __global__ __launch_bounds__(kKeepThreads) void cache_keep(KeepArgs a) {
   if (c.any) keep_alone(a, c, l);
 }
 
-// Where the weights' rows are longer, three launches: each workgroup has kChunk1 tokens of a sequence and KV head (one of up to 16384 is
-// the first launch's alone).  1: the first digit's bins of each chunk.  2: their sums give the digit; each chunk counts its weights
+// Where the weights' rows are longer, three launches: each workgroup has a chunk of a sequence and KV head (one of up to 16384 tokens is
+// the first launch's alone), a piece of 8192 tokens or, of more than 128 pieces, several, so that what every workgroup does for all chunks
+// grows no faster than the tokens.  1: the first digit's bins of each chunk.  2: their sums give the digit; each chunk counts its weights
 // above it and lists those that share it.  3: every workgroup finds the other digits from the list, counts what stays in the chunks
-// before its own, and writes its own.  (Where too many share the digit, the weights themselves are gone over in place of a list.)
+// before its own, and writes its own.  Where more than 16384 share the digit every workgroup goes over all weights in place of the list, three
+// times: 2^20 equal weights, 4 heads, 1.1 ms; 2^23 of them 8.5 (with a workgroup for each piece 62).
 // 100003 tokens, 4 heads: 4.9 + 9.0 + 12.6 us, latency throughout; one workgroup alone, at 20 instructions a weight and digit on one CU, 88 to 111.
+__host__ __device__ __forceinline__ int most_chunks(int width) {
+  const int pieces = (width + kPiece - 1) / kPiece;
+  return pieces < kMostChunks ? pieces : kMostChunks;
+}
+
 struct KeepSpace {
   int chunks;
   int* hist;      // [chunks][kBins], a head
@@ -172,11 +181,11 @@ struct KeepSpace {
   uint2* list;    // (weight, chunk)
   float* copy;    // [width]: of the weights, where they are written over
   static size_t bytes(int width, bool in_place) {
-    const size_t chunks = ((size_t)width + kChunk1 - 1) / kChunk1;
+    const size_t chunks = most_chunks(width);
     return (chunks * (kBins + 1) * 4 + 16 + (size_t)kList * 8 + (in_place ? (size_t)width * 4 : 0) + 255) & ~(size_t)255;
   }
   __device__ __forceinline__ KeepSpace(const KeepArgs& a, bool in_place) {
-    chunks = (a.width + kChunk1 - 1) / kChunk1;
+    chunks = most_chunks(a.width);
     const size_t each = ((size_t)chunks * (kBins + 1) * 4 + 16 + (size_t)kList * 8 + (in_place ? (size_t)a.width * 4 : 0) + 255) & ~(size_t)255;
     char* p = a.ws + (size_t)blockIdx.x * each;
     list = reinterpret_cast<uint2*>(p);
@@ -187,20 +196,30 @@ struct KeepSpace {
   }
 };
 
-__device__ __forceinline__ int chunks_of(const Choice& c) { return (c.n + kChunk1 - 1) / kChunk1; }
+// Tokens of a chunk, whole pieces, and the chunks of a sequence.
+__device__ __forceinline__ int chunk_tokens(const Choice& c) { return ((c.n - 1) / (kPiece * kMostChunks) + 1) * kPiece; }
+__device__ __forceinline__ int chunks_of(const Choice& c) { return (c.n - 1) / chunk_tokens(c) + 1; }
 
-// f(position, order of the weight) for this thread's tokens of a chunk.
+// fn(first token) of each piece of a chunk.
+template <typename Fn>
+__device__ __forceinline__ void each_piece(const Choice& c, int chunk, Fn fn) {
+  const int tokens = chunk_tokens(c), end = min((chunk + 1) * tokens, c.n);
+#pragma unroll 1
+  for (int first = chunk * tokens; first < end; first += kPiece) fn(first);
+}
+
+// f(position, weight) for this thread's tokens of the piece from `first` on.
 template <typename F>
-__device__ __forceinline__ void each_weight(const Choice& c, const float* weights, int chunk, F f) {
+__device__ __forceinline__ void each_weight(const Choice& c, const float* weights, int first, F f) {
   float x[kPart];
 #pragma unroll
   for (int i = 0; i < kPart; ++i) {
-    const int j = chunk * kChunk1 + i * kKeepThreads + (int)threadIdx.x;
+    const int j = first + i * kKeepThreads + (int)threadIdx.x;
     x[i] = j < min(c.n, c.held) ? weights[j] : 0.f;
   }
 #pragma unroll
   for (int i = 0; i < kPart; ++i) {
-    const int j = chunk * kChunk1 + i * kKeepThreads + (int)threadIdx.x;
+    const int j = first + i * kKeepThreads + (int)threadIdx.x;
     if (j < c.n) f(j, x[i]);
   }
 }
@@ -226,9 +245,11 @@ __global__ __launch_bounds__(kKeepThreads) void keep_count(KeepArgs a) {
   const KeepSpace w(a, in_place);
   if (chunk == 0 && tid == 0) w.info[0] = 0;
   clear(l);
-  each_weight(c, a.weights + (int64_t)blockIdx.x * a.width, chunk, [&](int j, float x) {
-    if (in_place) w.copy[j] = x;
-    if (c.between(j)) add(l, 0, 0, order_of(x));
+  each_piece(c, chunk, [&](int first) {
+    each_weight(c, a.weights + (int64_t)blockIdx.x * a.width, first, [&](int j, float x) {
+      if (in_place) w.copy[j] = x;
+      if (c.between(j)) add(l, 0, 0, order_of(x));
+    });
   });
   __syncthreads();
   reinterpret_cast<int2*>(w.hist + (size_t)chunk * kBins)[tid] = make_int2(bin(l, 2 * tid), bin(l, 2 * tid + 1));
@@ -259,29 +280,32 @@ __global__ __launch_bounds__(kKeepThreads) void keep_list(KeepArgs a) {
   }
   const bool open = c.wanted > 0 && !limit.all_stay();  // some of those that share the digit stay, some do not
   limit.close();
-  int more = 0, hits = 0;
-  uint32_t o[kPart];
-  each_weight(c, a.weights + (int64_t)blockIdx.x * a.width, chunk, [&](int j, float x) {
-    const uint32_t y = order_of(x);
-    const bool shares = open && c.between(j) && y >> Limit::shift(0) == limit.prefix;
-    if (shares) {
+  int more = 0;
+  each_piece(c, chunk, [&](int first) {
+    int hits = 0;
+    uint32_t o[kPart];
+    each_weight(c, a.weights + (int64_t)blockIdx.x * a.width, first, [&](int j, float x) {
+      const uint32_t y = order_of(x);
+      const bool shares = open && c.between(j) && y >> Limit::shift(0) == limit.prefix;
+      if (shares) {
+#pragma unroll
+        for (int i = 0; i < kPart; ++i)
+          if (i == hits) o[i] = y;
+        ++hits;
+      } else {
+        more += !c.between(j) || y > limit.value;
+      }
+    });
+    if (open && limit.among <= kList) {
+      const int end = wave_scan(hits);
+      int to = 0;
+      if (lane == kWave - 1 && end > 0) to = atomicAdd(&w.info[0], end);
+      to = __builtin_amdgcn_readlane(to, kWave - 1) + end - hits;
 #pragma unroll
       for (int i = 0; i < kPart; ++i)
-        if (i == hits) o[i] = y;
-      ++hits;
-    } else {
-      more += !c.between(j) || y > limit.value;
+        if (i < hits) w.list[to + i] = make_uint2(o[i], chunk);
     }
   });
-  if (open && limit.among <= kList) {
-    const int end = wave_scan(hits);
-    int to = 0;
-    if (lane == kWave - 1 && end > 0) to = atomicAdd(&w.info[0], end);
-    to = __builtin_amdgcn_readlane(to, kWave - 1) + end - hits;
-#pragma unroll
-    for (int i = 0; i < kPart; ++i)
-      if (i < hits) w.list[to + i] = make_uint2(o[i], chunk);
-  }
   __syncthreads();
   more = block_sum(more, l.sums);
   if (tid == 0) w.above[chunk] = more;
@@ -317,9 +341,11 @@ __global__ __launch_bounds__(kKeepThreads) void keep_write(KeepArgs a) {
             if (i * kKeepThreads + tid < entries) f(x[i].x, (int)x[i].y);
         } else {
           for (int i = 0; i < end; ++i)
-            each_weight(c, weights, i, [&](int j, float y) {
-              const uint32_t o = order_of(y);
-              if (c.between(j) && o >> Limit::shift(0) == (uint32_t)w.info[1]) f(o, i);
+            each_piece(c, i, [&](int first) {
+              each_weight(c, weights, first, [&](int j, float y) {
+                const uint32_t o = order_of(y);
+                if (c.between(j) && o >> Limit::shift(0) == (uint32_t)w.info[1]) f(o, i);
+              });
             });
         }
       };
@@ -345,12 +371,17 @@ __global__ __launch_bounds__(kKeepThreads) void keep_write(KeepArgs a) {
   __syncthreads();
   equal = block_sum(equal, l.sums);
   __syncthreads();
-  float x[kPart];
-  const int first = chunk * kChunk1 + tid * kPart;
+  each_piece(c, chunk, [&](int piece) {
+    float x[kPart];
+    const int first = piece + tid * kPart;
 #pragma unroll
-  for (int i = 0; i < kPart; ++i) x[i] = first + i < min(c.n, c.held) ? weights[first + i] : 0.f;
-  write_kept<kPart>(c, limit, x, first, kPart, above, equal, l.sums, a.kept + (int64_t)blockIdx.x * a.cap,
-                    a.new_weights ? a.new_weights + (int64_t)blockIdx.x * a.width : nullptr);
+    for (int i = 0; i < kPart; ++i) x[i] = first + i < min(c.n, c.held) ? weights[first + i] : 0.f;
+    const int total = write_kept<kPart>(c, limit, x, first, kPart, above, equal, l.sums, a.kept + (int64_t)blockIdx.x * a.cap,
+                                        a.new_weights ? a.new_weights + (int64_t)blockIdx.x * a.width : nullptr);
+    above += total & 0xffff;
+    equal += total >> 16;
+    __syncthreads();  // the sums are done with
+  });
 }
 
 // The smallest e >= kScaleExpMin with x 2^8 <= MAX 2^e, from a value of at most eight significant bits.
@@ -551,7 +582,7 @@ hipError_t launch_cache_keep(const KeepArgs& a, hipStream_t stream) {
   if (a.width <= kMost * kKeepThreads) {
     hipLaunchKernelGGL(cache_keep, dim3(heads), dim3(kKeepThreads), 0, stream, a);
   } else {
-    const dim3 grid(heads, (unsigned)((a.width + kChunk1 - 1) / kChunk1));
+    const dim3 grid(heads, (unsigned)most_chunks(a.width));
     hipLaunchKernelGGL(keep_count, grid, dim3(kKeepThreads), 0, stream, a);
     hipLaunchKernelGGL(keep_list, grid, dim3(kKeepThreads), 0, stream, a);
     hipLaunchKernelGGL(keep_write, grid, dim3(kKeepThreads), 0, stream, a);
