@@ -110,7 +110,8 @@ class KVCache:
     def prefill_packed(self, layer: int, row_ptr: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                        softmax_scale: float = 0.0, weigh: bool = False) -> torch.Tensor:
         """One layer of several prompts, rows row_ptr[s] .. row_ptr[s + 1] those of sequence s, which holds nothing yet: dense causal
-        attention of each over itself, then k and v into the cache -> o.  With weigh, all their rows count.  If a
+        attention of each over itself, then k and v into the cache -> o.  With weigh, all their rows count (which for long prompts takes 10
+        to 70 times what the attention takes; the last rows alone, as in prefill, take little).  If a
         sequence with rows holds tokens, nothing of it is stored and o's first row of it is NaN."""
         if weigh:
             self._need_weights()
@@ -135,7 +136,9 @@ class KVCache:
         """One layer of a step: rows row_ptr[s] .. row_ptr[s + 1] of k and v behind sequence s's tokens, then q's
         rows over all of them -> o.  Rows of a sequence without room are not stored and get 0; of more rows than
         its room the ones behind it get no defined result.  With weigh the attention that each token gets is added to its
-        weight (a sequence's weights are not defined after more rows than its room)."""
+        weight (a sequence's weights are not defined after more rows than its room), at once: rows that advance() then does not take, or
+        takes back later, leave in the weights of the tokens that stay what they added, and a layer's step that is run twice is
+        added twice.  The workspace of that, up to 256 MB with the cache's size, is allocated in the call."""
         cache = self.layers[layer]
         if weigh:
             self._need_weights()
@@ -167,7 +170,8 @@ class KVCache:
         that many, in every layer and KV head the last `recent`, the first `sink`, and those that had the most weight -> the number
         of tokens kept, int32 [max_seqs], 0 where nothing was done: also where the free pages do not suffice, since what stays
         goes to pages of its own (a fork keeps what it shares).  Rows that were granted to a sequence that is cut and not
-        taken are given back.  Positions go on as they were."""
+        taken are given back.  Positions go on as they were.  Tokens that advance() takes back later are the last places of each KV head: its
+        `recent` ones, and where those do not suffice older tokens that stayed, in each head its own."""
         self._need_weights()
         if cap < 1:
             raise ValueError(f"cap {cap} must be positive")

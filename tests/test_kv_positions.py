@@ -1,7 +1,10 @@
-"""KVCache after evictions: positions go on as they were, against a second cache that is given turned rows."""
+"""KVCache after evictions and with rows that do not stay: positions go on as they were, against a second cache that is given turned rows; what
+rows that are not taken, or taken back, leave in the weights, against counted sums; what a take-back after an eviction takes,
+against the 64-bit mirror."""
 import pytest
 import torch
 
+from tests import cache_oracle as O
 from tests import test_kv_evict as E
 from tests.test_kv_cache import _ints
 
@@ -73,3 +76,54 @@ def test_positions_go_on_after_evictions():
     pos[1] = lens[1] = 0
     step([0, 33, 0, 0], 8, "prefill_packed")
     step([1, 1, 1, 1], 9)
+
+
+def test_rows_that_are_not_taken_keep_what_they_weighed():
+    """advance() with fewer rows than were weighed, or negative: the tokens that stay keep the attention of the others.  A step that is weighed
+    twice counts twice."""
+    from paper_2609_01925_amd.cache import KVCache
+    E._say("KVCache rows not taken")
+    kv = KVCache(1, 10, 1, max_seqs=1, max_tokens=320, device=DEV, weights=True)
+    total = lambda n: kv.weights[0][0, 0, :n].double().sum().item()
+    near = lambda x, y: abs(x - y) <= 2.0 ** -13 * y  # as test_weights_sum_to_the_rows
+    kv.reserve(_ints([100]))
+    kv.prefill(0, 0, *E._qkv(100, 1, 2, 1), weigh=1)
+    kv.advance(_ints([100]), weighed=True)
+    assert near(total(100), 2)
+    kv.reserve(_ints([4]))
+    rows = E._qkv(4, 2, 2, 1)
+    kv.attend(0, E._ptr([4]), *rows, weigh=True)
+    assert near(total(104), 2 + 8)
+    left = kv.weights[0][0, 0].clone()
+    kv.advance(_ints([1]), weighed=True)  # three of them are not taken
+    assert kv.held.tolist() == [101] and torch.equal(kv.weights[0][0, 0, :101], left[:101])
+    assert total(101) > 2 + 4  # more than the one row's
+    had = total(101)
+    kv.reserve(_ints([2]))
+    rows = E._qkv(2, 3, 2, 1)
+    kv.attend(0, E._ptr([2]), *rows, weigh=True)
+    assert near(total(103), had + 4)
+    # once more: the tokens held before have it twice, the two rows' own weight, not held yet, starts anew
+    kv.attend(0, E._ptr([2]), *rows, weigh=True)
+    assert had + 4 < total(103) < had + 8
+    kv.advance(_ints([2]), weighed=True)
+    left = kv.weights[0][0, 0].clone()
+    kv.advance(_ints([-2]))
+    assert kv.held.tolist() == [101] and torch.equal(kv.weights[0][0, 0, :101], left[:101])
+
+
+@pytest.mark.parametrize("fmt,block", [(O.E4M3, 64), (O.INT8, 128)])
+def test_rows_taken_back_after_an_eviction(fmt, block):
+    """They are the last places of each KV head: the last `recent` tokens, then whatever else stayed."""
+    from paper_2609_01925_amd.cache import KVCache
+    E._say(f"KVCache rows taken back after an eviction fmt={fmt}")
+    kv = KVCache(2, 20, 2, max_seqs=1, max_tokens=640, block=block, fmt=fmt, device=DEV, weights=True)
+    mirror = E.Evicting(2, 2, block, fmt, 640 // block)
+    E._step(kv, mirror, [200], 1)
+    before = E._weights_of(kv)
+    assert kv.evict(_ints([80]), 80, 4, 8).tolist() == [80]
+    mirror.evict(before, [80], [80], 4, 8)
+    kv.advance(_ints([-20]))
+    mirror.len[0] -= 20
+    assert kv.seq_len.tolist() == [60] and kv.held.tolist() == [60] and kv.pos.tolist() == [180]
+    E._step(kv, mirror, [3], 2)
