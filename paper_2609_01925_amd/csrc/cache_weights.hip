@@ -9,8 +9,12 @@
 // Few pairs are bound by the keys' bytes: a row of each of 48 sequences of 300 to 8191 tokens, 32 heads over 8 (179 MB read), 43 us, 4.2 TB/s, and
 // 16 us for the scores and weights (32 MB read: launch, lengths, scores, in turn); without waiting scores 36 + 43 us.  Many pairs are bound by
 // vector instructions, three for each score and pass beside the conversion of K: 32 rows of 28 heads over 4 and 131000 tokens (30 GFLOP a
-// pass) 45 + 5.6 + 42 us, 35 of them for each pass in proportion to the tokens, 10 to begin.  Products of one group in a fixed order beside
+// pass) 44 + 5.5 + 42 us, 35 of them for each pass in proportion to the tokens, 10 to begin.  Products of one group in a fixed order beside
 // the exponents of the one before, or the next tile read from LDS beside the last group's, change nothing (47 to 51 and 46 to 50 us).
+//
+// Rows as many as tokens are not what this is made for: chunks are divided by slots and bounded by the space for statistics, and a pass of 256
+// pairs goes over tiles behind all of them, too.  Whole prompts, 32 heads over 8: 4096 rows 1.6 ms, 12000 rows 19 (among 64 slots 77), 32768 rows
+// 261, 10 to 70 times their attention.  One row over 128000 tokens 40 us, 159 where 63 further slots hold nothing.
 #include <type_traits>
 
 #include "cache_device.h"
@@ -630,7 +634,9 @@ Plan plan_of(const CacheDims& c, const BatchDims& b, int hq) {
   if (heads == 0 || pairs == 0) return Plan{1, 0, 0, 0, 0, 0};
   // Workgroups enough for the GPU: of many pairs 512 (a window of 32 rows of 28 heads over 128k tokens 45 + 42 us; 1024 and 1536 workgroups 10
   // and 30 % more), of few 1024, and where there are many heads to go over, up to twelve chunks each, so that the longest sequence is not
-  // left to the last (48 of 300 to 8191 tokens 44 us, 48 with four chunks).  16 MB of statistics at most but for calls of very many rows; the
+  // left to the last.  With four / twelve / 24 chunks, the whole call in us: 48 sequences of 300 to 8191 tokens, 8 heads, 75 / 70 / 79; 24 of 500
+  // to 16000, 4 heads, 50 / 47 / 45; 100 of 100 to 4000, 8 heads, 73 / 72 / 76; 200 of 100 to 3000, 2 heads, 40 / 42 / 49; 64 of 8000, 8
+  // heads, 161 / 145 / 140; 12 of 1000 to 60000, 8 heads, 116 / 112 / 109.  16 MB of statistics at most but for calls of very many rows; the
   // space for them does not shrink as rows are added, so that a workspace is enough for fewer rows, too.
   constexpr int64_t kMost = (int64_t)1 << 21;
   const auto each = [&](int64_t wgs) { return (wgs + heads - 1) / heads; };

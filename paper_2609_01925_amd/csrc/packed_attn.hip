@@ -10,10 +10,11 @@
 // come from LDS through the transposing read, as in the sparse prefill.
 //
 // Bound by the matrix units and, beside them, the softmax's vector instructions: three prompts of 5000 to 12000 tokens, 32 heads over 8
-// (2982 GFLOP), 2.58 to 2.65 ms, 1125 to 1155 TFLOP/s at a clock of 1.7 GHz, MFMA 64% of cycles, VALU 45%, both 21%.  Short prompts are bound by their
-// edges: 16 of 40 to 2500 tokens, 28 heads over 4 (252 GFLOP), 322 to 360 us, MFMA 40%; without the edge tiles' work 300 of the 360, without the whole tiles'
-// 165, without either 74 (q in and o out).  A dozen of 1 to 90 tokens 14 us, the chain of one block: begins, keys, scores, values.
-// Two query heads a workgroup, with the next one's q and keys under way, take 381 (four 464, 48 for the short ones).
+// (2982 GFLOP), 2.53 to 2.64 ms, 1128 to 1178 TFLOP/s at a clock of 1.7 GHz, MFMA 64% of cycles, VALU 45%, both 21%.  Short prompts are bound by their
+// edges: 16 of 40 to 2500 tokens, 28 heads over 4 (252 GFLOP), 322 to 338 us, MFMA 40%; without the edge tiles' work 282 of 333, without the whole tiles
+// 131, without either 102.  A wave all of whose rows begin anew in the block still takes part in the whole tiles' products (458 of that case's 8308
+// tiles of a wave).  A dozen of 1 to 90 tokens 14 us, the chain of one block: begins, keys, scores, values.
+// Two query heads a workgroup, with the next one's q and keys under way, took 381 where one took 360 (four 464, 48 for the short ones).
 #include <type_traits>
 
 #include "packed_device.h"
@@ -135,7 +136,8 @@ __device__ __forceinline__ float tile_max(const f32x16 (&s)[kSubs]) {
   return half_max(m);
 }
 
-// P = exp2(s c - mc), rounded to bf16, and the lane's sum of the rounded ones.
+// P = exp2(s c - mc), rounded to bf16, which the products with V take, and the lane's sum of the rounded ones, so that a row's weights still
+// add up to 1.  It puts a result 0.0020 from the 64-bit one, relative to all of them, where the result's own rounding alone is 0.0016.
 __device__ __forceinline__ float form_tile(const f32x16 (&s)[kSubs], float c, float mc, Probs& p) {
   float part[2] = {0.f, 0.f};
 #pragma unroll

@@ -109,6 +109,16 @@ def test_weights_of_many_rows(rows, block):
     _check_weights(C, c, oracle, table, lens, counts, 6, held=[70, 0, 5], seed=rows)
 
 
+@pytest.mark.parametrize("slots", [2, 40])
+def test_weights_of_whole_prompts(slots):
+    """All rows of prompts of some thousands, dozens of passes of 256 pairs; alone, and among slots that hold nothing."""
+    C = _crisp()
+    _say(f"weights of whole prompts, {slots} slots")
+    counts = [2100, 1333] + [0] * (slots - 2)
+    c, oracle, table, _ = _filled(C, counts, 1, 64, O.E4M3, 12)
+    _check_weights(C, c, oracle, table, [0] * slots, counts, 4, held=[0] * slots, seed=12)
+
+
 def test_weights_of_a_ragged_batch():
     """Sequences without rows, without tokens, more than a wave looks over; nothing held, some held, more held than there is."""
     C = _crisp()
